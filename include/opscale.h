@@ -297,6 +297,99 @@ opscale_status opscale_add_rmsnorm(const void* x, void* residual, const void* w,
                                    float eps, opscale_dtype dt, hipStream_t stream, opscale_timing* timing);
 
 /* ---------------------------------------------------------------------------
+ * The attention path of layers that differ from the plain one: norms of the
+ * query and key heads, other rotations, the tables of a step built on the GPU,
+ * and attention with score modifiers and masks.
+ * ------------------------------------------------------------------------- */
+
+/* How the rotation's frequencies are stretched for contexts longer than the
+ * original one.  f_i = theta^(-2i/rot), i < rot/2, turns f_i L / 2 pi times over
+ * the original length L. */
+typedef enum {
+  OPSCALE_ROPE_NONE = 0,   /* f_i */
+  OPSCALE_ROPE_LINEAR = 1, /* f_i / factor */
+  OPSCALE_ROPE_BANDS = 2,  /* f_i where it turns high times or more, f_i / factor where low or fewer, between them
+                              mixed by its turns */
+  OPSCALE_ROPE_RAMP = 3    /* the same, mixed by i between the pair indices that turn high and low times (rounded
+                              outwards); magnitude 0.1 ln(factor) + 1 */
+} opscale_rope_scaling;
+
+/*
+ * Host only (no device needed).  The rotation frequencies of a head whose first
+ * `rot` elements turn: inv_freq (HOST, rot / 2 doubles, radians a position) and
+ * *magnitude, the factor on sine and cosine (1 unless scaling says otherwise).
+ * A caller copies inv_freq to the device once, as a weight.  rot even, in
+ * [2, 256]; theta finite and > 1; where a scaling uses them: factor finite and
+ * >= 1, 0 < low < high, original_len >= 1.
+ */
+opscale_status opscale_rope_frequencies(double* inv_freq, float* magnitude, int32_t rot, double theta,
+                                        opscale_rope_scaling scaling, double factor, double low, double high,
+                                        int64_t original_len);
+
+/*
+ * RMS Norm of every query and key head, rotary position embedding and KV-cache
+ * write, in one pass (each step optional):
+ *   x <- x / sqrt(mean_D x^2 + eps) * w           (w = q_weight or k_weight, [D]; both NULL: no norm)
+ *   (a, b) <- m (a cos t - b sin t, b cos t + a sin t),  t = positions[t] * inv_freq[i],  i < rot / 2,
+ * where pair i is (x[i], x[i + rot/2]) (interleaved == 0) or (x[2i], x[2i + 1])
+ * (interleaved != 0), m is `magnitude` (not applied to elements rot .. D-1), and the
+ * result is rounded once.  The angle is formed and reduced modulo 2 pi in fp64.
+ * q: [T, Hq, D], k: [T, Hkv, D], token t, head h at q + t * q_row_stride + h * D
+ *   (elements; views into the QKV linear's output are fine).
+ * q_out, k_out: the results, with row strides of their own; q_out == q (same
+ *   stride) and k_out == k work in place.  An output overlaps nothing else.
+ * inv_freq: DEVICE fp64 [rot / 2] (opscale_rope_frequencies); rot == 0: no
+ *   rotation (inv_freq and positions may be NULL).
+ * k_cache, v_cache: NULL, or caches [num_blocks, block_size, Hkv, D] that also
+ *   receive row t of k_out and of v ([T, Hkv, D], v_row_stride) at cache row
+ *   slot_mapping[t]; a slot outside [0, num_blocks * block_size) is skipped
+ *   (padding).  Without caches v, slot_mapping and the block arguments are ignored.
+ *   Tokens sharing a slot race.
+ * D a multiple of 16 in [32, 256], rot a multiple of 16 up to D (else
+ * OPSCALE_ERR_UNSUPPORTED); tensors 16-byte aligned, strides multiples of 16
+ * bytes; eps finite and >= 0; magnitude finite.
+ */
+opscale_status opscale_qk_norm_rope(const void* q, const void* k, int64_t q_row_stride, int64_t k_row_stride,
+                                    void* q_out, void* k_out, int64_t q_out_row_stride, int64_t k_out_row_stride,
+                                    const void* q_weight, const void* k_weight, float eps, const int32_t* positions,
+                                    const double* inv_freq, int32_t rot, int32_t interleaved, float magnitude,
+                                    const void* v, int64_t v_row_stride, void* k_cache, void* v_cache,
+                                    const int32_t* slot_mapping, int32_t block_size, int64_t num_blocks, int64_t T,
+                                    int32_t Hq, int32_t Hkv, int32_t D, opscale_dtype dt, hipStream_t stream,
+                                    opscale_timing* timing);
+
+/*
+ * The tables of a step from its requests' lengths, in one launch without a host
+ * round trip: request b has context_lens[b] tokens in the cache and brings
+ * new_lens[b] more (negative counts as 0).
+ *   cu_seqlens[b]  = min(sum of new_lens before b, max_tokens), [B + 1]: request b's new tokens
+ *                    are cu_seqlens[b] .. cu_seqlens[b+1] - 1 (tokens past max_tokens are left for a later step);
+ *   positions[t]   = context_lens[b] + (t - cu_seqlens[b]),
+ *   slot_mapping[t]= block_table[b, p / block_size] * block_size + p % block_size for p = positions[t];
+ *   kv_lens[b]     = context_lens[b] + the request's new tokens (at most max_blocks_per_seq * block_size);
+ *   block_table[b, j], ceil(context_lens[b] / block_size) <= j < ceil(kv_lens[b] / block_size): taken from
+ *                    free_blocks[*free_begin], [*free_begin + 1], ..., in order of b, then j; the row's other
+ *                    entries are left as they were (those before are the request's pages and are read);
+ *   *free_next     = *free_begin + the pages taken.
+ * Tokens cu_seqlens[B] .. max_tokens - 1 are padding: position 0, slot -1.
+ * Where the free list ends early, the entries are -1 and so are their tokens'
+ * slots (*free_next > num_free says how many pages are missing); so are the slots
+ * of tokens past max_blocks_per_seq pages, and of pages that are negative.  The cache write
+ * skips such slots and attention such pages.
+ * All arrays DEVICE int32: context_lens, new_lens, kv_lens [B]; block_table [B,
+ * max_blocks_per_seq]; free_blocks [num_free]; free_begin, free_next [1];
+ * positions, slot_mapping [max_tokens].  An output overlaps nothing else.
+ * block_size a power of two in [1, 1024]; max_blocks_per_seq * block_size,
+ * num_free and max_tokens below 2^31.  B == 0: every token is padding.
+ */
+opscale_status opscale_block_tables(const int32_t* context_lens, const int32_t* new_lens, int32_t B,
+                                    int32_t* block_table, int32_t max_blocks_per_seq, int32_t block_size,
+                                    const int32_t* free_blocks, int64_t num_free, const int32_t* free_begin,
+                                    int64_t max_tokens, int32_t* cu_seqlens, int32_t* positions,
+                                    int32_t* slot_mapping, int32_t* kv_lens, int32_t* free_next, hipStream_t stream,
+                                    opscale_timing* timing);
+
+/* ---------------------------------------------------------------------------
  * Operator profiling (Section 4.2 "Operator Profiling": per-operator compute
  * time T_v and memory M_v; Appendix C "Dataflow Characteristics": the payload
  * an operator hands to the next one, the basis of C_v).

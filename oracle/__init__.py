@@ -13,13 +13,14 @@ add before each norm), evaluated in fp64 with no
 tiling, no online softmax and no split of the key range.  See `ops` for the
 per-function citations, `cost` for the algorithmic flop/byte closed forms and
 `spatial` for CU shares and the interference factor of Eq. 5, `moe` for
-top-k routing and the fused mixture-of-experts MLP.
+top-k routing and the fused mixture-of-experts MLP, `step` for the norms and
+rotations of the heads, a step's tables, and attention with score modifiers and masks.
 
 Parity status: every exported function has a named pin in the CPU tests
 (brute force, a hand-worked golden, a closed form or an invariant, plus planted
 mistakes each pin must catch): tests/test_oracle_pins.py for `ops` and `cost`,
 tests/test_oracle_moe.py for `moe`, tests/test_oracle_spatial.py for
-`spatial`.  The whole-layer dataflow is pinned by a two-token layer worked by
+`spatial`, tests/test_oracle_step.py for `step`.  The whole-layer dataflow is pinned by a two-token layer worked by
 hand (tests/golden/layer_two_tokens_hand.txt).
 """
 from .ops import (  # noqa: F401
@@ -29,3 +30,4 @@ from .ops import (  # noqa: F401
 from . import cost  # noqa: F401
 from . import spatial  # noqa: F401
 from . import moe  # noqa: F401
+from . import step  # noqa: F401

@@ -21,6 +21,7 @@ OPSCALE_F32, OPSCALE_BF16 = 0, 1
 (TUNE_GEMM_TILE, TUNE_GEMM_SKINNY, TUNE_GEMM_SPLITK, TUNE_GEMM_TAIL, TUNE_SKINNY_NG, TUNE_PREFILL_SCHEDULE,
  TUNE_MOE_FUSE, TUNE_GEMM_DECODE) = range(8)
 TUNE_AUTO = -1
+ROPE_SCALINGS = {"none": 0, "linear": 1, "bands": 2, "ramp": 3}  # opscale_rope_scaling
 
 c_i32, c_i64, c_f32, c_f64, c_vp, c_sz = (ctypes.c_int32, ctypes.c_int64, ctypes.c_float,
                                           ctypes.c_double, ctypes.c_void_p, ctypes.c_size_t)
@@ -152,6 +153,13 @@ EXPORTS = {
                                           c_i32, c_vp, ctypes.POINTER(Timing)]),
     "opscale_add_rmsnorm": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_i64, c_i64, c_f32, c_i32, c_vp,
                                     ctypes.POINTER(Timing)]),
+    "opscale_rope_frequencies": (c_i32, [ctypes.POINTER(c_f64), ctypes.POINTER(c_f32), c_i32, c_f64, c_i32, c_f64,
+                                         c_f64, c_f64, c_i64]),
+    "opscale_qk_norm_rope": (c_i32, [c_vp, c_vp, c_i64, c_i64, c_vp, c_vp, c_i64, c_i64, c_vp, c_vp, c_f32, c_vp,
+                                     c_vp, c_i32, c_i32, c_f32, c_vp, c_i64, c_vp, c_vp, c_vp, c_i32, c_i64, c_i64,
+                                     c_i32, c_i32, c_i32, c_i32, c_vp, ctypes.POINTER(Timing)]),
+    "opscale_block_tables": (c_i32, [c_vp, c_vp, c_i32, c_vp, c_i32, c_i32, c_vp, c_i64, c_vp, c_i64, c_vp, c_vp,
+                                     c_vp, c_vp, c_vp, c_vp, ctypes.POINTER(Timing)]),
     "opscale_moe_topk": (c_i32, [c_vp, c_vp, c_vp, c_i64, c_i32, c_i32, c_i32, c_vp, ctypes.POINTER(Timing)]),
     "opscale_fused_moe_workspace_size": (c_sz, [c_i64, c_i32, c_i32, c_i32, c_i32]),
     "opscale_fused_moe": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64, c_i32, c_i32, c_i32, c_i32, c_i32,
@@ -501,6 +509,153 @@ def opscale_add_rmsnorm(x, residual, w, y=None, eps: float = 1e-5, stream=None, 
     _check(lib.opscale_add_rmsnorm(_ptr(x), _ptr(residual), _ptr(w), _ptr(y), M, H, eps, _dt(x), _stream(stream),
                                    ctypes.byref(t) if t else None))
     return (y, t) if timed else y
+
+
+# ------------------------------------- norms of the heads, step tables --
+def opscale_rope_frequencies(rot: int, theta: float, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
+                             high: float = 4.0, original_len: int = 8192, device="cuda"):
+    """(inv_freq, magnitude) of a head whose first `rot` elements turn: a float64
+    tensor [rot / 2] on `device`, kept like a weight, and a number.  scaling:
+    "none", "linear", "bands" or "ramp"."""
+    import torch
+    if scaling not in ROPE_SCALINGS:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"scaling {scaling!r} (one of {', '.join(ROPE_SCALINGS)})")
+    f, m = (c_f64 * max(rot // 2, 1))(), c_f32()
+    _check(load().opscale_rope_frequencies(f, ctypes.byref(m), rot, float(theta), ROPE_SCALINGS[scaling],
+                                           float(factor), float(low), float(high), int(original_len)))
+    return torch.tensor(list(f), dtype=torch.float64, device=device), m.value
+
+
+_i32, _f64 = None, None  # torch's dtypes, filled on first use
+
+
+def _here(*named) -> None:
+    """Each (name, tensor) on the current device, where the call's kernels run."""
+    if _raw_stream is None:
+        _stream(None)
+    dev = _device()
+    for name, t_ in named:
+        if t_ is not None and t_.get_device() != dev:
+            raise OpscaleError(OPSCALE_ERR_INVALID_ARG,
+                               f"{name} is on {t_.device}: tensors must be on the GPU that is current (cuda:{dev})")
+
+
+def _ints(*named, size=None):
+    """Each (name, tensor) contiguous int32 on the current GPU, of `size` elements if given."""
+    global _i32
+    if _i32 is None:
+        import torch
+        _i32 = torch.int32
+    _here(*named)
+    for name, t_ in named:
+        if t_.dtype != _i32 or not t_.is_contiguous() or (size is not None and t_.numel() != size):
+            raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"{name} must be a contiguous int32 tensor"
+                               + ("" if size is None else f" of {size} elements"))
+
+
+def _rows(name, t_, T, H, D, dtype) -> int:
+    """The row stride of t_ [T, H, D] (heads contiguous; any of a single row's)."""
+    if t_.dtype != dtype or t_.dim() != 3 or t_.shape[0] != T:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"{name} must be {dtype} with {T} rows of heads")
+    _heads_view(name, t_, H, D)
+    return t_.stride(0) if T > 1 else H * D
+
+
+def _weight(name, t_, n, dtype):
+    if t_.dtype != dtype or t_.numel() != n or not t_.is_contiguous():
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"{name} must be contiguous {dtype} of {n} elements")
+
+
+def opscale_qk_norm_rope(q, k, positions=None, inv_freq=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                         interleaved: bool = False, magnitude: float = 1.0, v=None, k_cache=None, v_cache=None,
+                         slot_mapping=None, q_out=None, k_out=None, stream=None, timed: bool = False):
+    """RMS Norm of each head of q [T, Hq, D] and k [T, Hkv, D] (with q_weight and
+    k_weight [D]), rotation of its first 2 * len(inv_freq) elements, and with
+    caches [num_blocks, block_size, Hkv, D] the write of k and v [T, Hkv, D] to
+    the int32 slots: each step where its arguments are given.  In place, or to
+    q_out and k_out; the token dimension of each may be strided.
+    opscale_rope_frequencies makes inv_freq and magnitude.  Returns (q, k), the
+    results."""
+    global _f64
+    lib = load()
+    dt, dtype = _dt(q), q.dtype
+    if q.dim() != 3 or k.dim() != 3:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "q and k must be [T, heads, D]")
+    T, Hq, D = q.shape
+    Hkv = k.shape[1]
+    q_out = q if q_out is None else q_out
+    k_out = k if k_out is None else k_out
+    _here(("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out), ("inv_freq", inv_freq), ("q_weight", q_weight),
+          ("k_weight", k_weight))
+    qs, ks = _rows("q", q, T, Hq, D, dtype), _rows("k", k, T, Hkv, D, dtype)
+    qos = qs if q_out is q else _rows("q_out", q_out, T, Hq, D, dtype)
+    kos = ks if k_out is k else _rows("k_out", k_out, T, Hkv, D, dtype)
+    rot = 0
+    if inv_freq is not None:
+        if _f64 is None:
+            import torch
+            _f64 = torch.float64
+        _weight("inv_freq", inv_freq, inv_freq.numel(), _f64)
+        if positions is None:
+            raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "a rotation takes positions")
+        _ints(("positions", positions), size=T)
+        rot = 2 * inv_freq.numel()
+    else:
+        positions = None
+    if (q_weight is None) != (k_weight is None):
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "q_weight and k_weight are given both or neither")
+    if q_weight is not None:
+        _weight("q_weight", q_weight, D, dtype)
+        _weight("k_weight", k_weight, D, dtype)
+    bs = nb = vs = 0
+    if k_cache is None and v_cache is None:
+        v = slot_mapping = None
+    else:
+        if k_cache is None or v_cache is None or v is None or slot_mapping is None:
+            raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "a cache write takes k_cache, v_cache, v and slot_mapping")
+        _here(("v", v), ("k_cache", k_cache), ("v_cache", v_cache))
+        vs = _rows("v", v, T, Hkv, D, dtype)
+        _ints(("slot_mapping", slot_mapping), size=T)
+        nb, bs = k_cache.shape[0], k_cache.shape[1]
+        for n, t_ in (("k_cache", k_cache), ("v_cache", v_cache)):
+            if tuple(t_.shape) != (nb, bs, Hkv, D) or t_.dtype != dtype or not t_.is_contiguous():
+                raise OpscaleError(OPSCALE_ERR_INVALID_ARG,
+                                   f"{n} must be contiguous {dtype} [num_blocks, block_size, {Hkv}, {D}]")
+    t = Timing() if timed else None
+    _check(lib.opscale_qk_norm_rope(_ptr(q), _ptr(k), qs, ks, _ptr(q_out), _ptr(k_out), qos, kos, _ptr(q_weight),
+                                    _ptr(k_weight), eps, _ptr(positions), _ptr(inv_freq), rot, int(interleaved),
+                                    magnitude, _ptr(v), vs, _ptr(k_cache), _ptr(v_cache), _ptr(slot_mapping), bs, nb,
+                                    T, Hq, Hkv, D, dt, _stream(stream), ctypes.byref(t) if t else None))
+    return ((q_out, k_out), t) if timed else (q_out, k_out)
+
+
+def opscale_block_tables(context_lens, new_lens, block_table, free_blocks, free_begin, block_size: int,
+                         max_tokens: int, out=None, stream=None, timed: bool = False):
+    """The tables of a step: request b has context_lens[b] tokens in the cache and
+    brings new_lens[b]; pages are taken from free_blocks, from entry free_begin[0]
+    on, into block_table [B, max_blocks_per_seq] (updated in place).  All int32
+    GPU tensors.  Returns (cu_seqlens [B + 1], positions [max_tokens],
+    slot_mapping [max_tokens], kv_lens [B], free_next [1]); `out`: the same five,
+    to be filled.  Tokens past the last are padding (position 0, slot -1)."""
+    lib = load()
+    B, cols = block_table.shape
+    _ints(("context_lens", context_lens), ("new_lens", new_lens), size=B)
+    _ints(("block_table", block_table), ("free_blocks", free_blocks))
+    _ints(("free_begin", free_begin), size=1)
+    if out is None:
+        new = context_lens.new_empty
+        out = new(B + 1), new(max_tokens), new(max_tokens), new(B), new(1)
+    else:
+        for n, t_, size in zip(("cu_seqlens", "positions", "slot_mapping", "kv_lens", "free_next"), out,
+                               (B + 1, max_tokens, max_tokens, B, 1)):
+            _ints((n, t_), size=size)
+    cu, positions, slots, kv_lens, free_next = out
+    t = Timing() if timed else None
+    _check(lib.opscale_block_tables(_ptr(context_lens), _ptr(new_lens), B, _ptr(block_table), cols, block_size,
+                                    _ptr(free_blocks), free_blocks.numel(), _ptr(free_begin), max_tokens, _ptr(cu),
+                                    _ptr(positions), _ptr(slots), _ptr(kv_lens), _ptr(free_next), _stream(stream),
+                                    ctypes.byref(t) if t else None))
+    return (out, t) if timed else out
 
 
 def opscale_op_profile(desc: OpDesc, warmup: int = 5, iters: int = 20, flush=None, stream=None) -> Profile:

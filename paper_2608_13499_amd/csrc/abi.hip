@@ -173,6 +173,14 @@ Work work_add_rmsnorm(int64_t M, int64_t H, int s) {
   return {5.0 * M * H, (double)s * (4.0 * M * H + H), s * H, s * 4 * M * H, s * 2 * M * H};
 }
 
+Work work_qk_norm_rope(const opscale::QkNormRope& p, int s) {
+  const int64_t qk = p.T * (p.Hq + p.Hkv) * p.D, v = p.k_cache ? p.T * p.Hkv * p.D : 0;
+  const int64_t weight = (p.q_weight ? (int64_t)s * 2 * p.D : 0) + 4ll * p.rot;
+  const double flops = (p.q_weight ? 4.0 * qk : 0.0) + 3.0 * p.T * (p.Hq + p.Hkv) * p.rot;
+  return {flops, (double)s * (2.0 * qk + 3.0 * v) + weight + (p.rot ? 4.0 : 0.0) * p.T + (v ? 4.0 : 0.0) * p.T, weight,
+          s * (qk + 2 * v), s * (qk + v)};
+}
+
 // MoE: each valid (token, slot) pair does the two expert GEMMs (2 H 2F + 2 F H
 // flops, 6 H F) and the SwiGLU (6 F); x and out are read / written once and
 // the weights of every expert that receives a token are read once.
@@ -377,6 +385,128 @@ opscale_status check_cache_write(const void* k, const void* v, int64_t kvs, void
   return OPSCALE_OK;
 }
 
+// Do rows [0, T) of `wa` bytes every `sa` bytes from a share a byte with the rows
+// (T, wb, sb) of b?  Rows of one stride (views of one packed tensor) are
+// compared column by column, others by their whole extent.
+bool rows_overlap(const void* a, int64_t sa, int64_t wa, const void* b, int64_t sb, int64_t wb, int64_t T) {
+  if (!overlap(a, (T - 1) * sa + wa, b, (T - 1) * sb + wb)) return false;
+  if (sa != sb) return true;
+  const intptr_t d = (intptr_t)(reinterpret_cast<uintptr_t>(b) - reinterpret_cast<uintptr_t>(a));
+  const int64_t col = ((d % sa) + sa) % sa;  // b's first column as seen from a's
+  return col < wa || col + wb > sa;
+}
+
+opscale_status check_qk_norm_rope(const opscale::QkNormRope& p, int32_t bs, int64_t nb, opscale_dtype dt) {
+  const char* who = "qk_norm_rope";
+  if (!dtype_ok(dt)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, (int)dt);
+  if (p.T < 0 || p.T >= kMaxDim || p.Hq <= 0 || p.Hkv <= 0 || p.Hq > 65535 || p.Hkv > 65535 || p.D <= 0)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes T=%lld Hq=%d Hkv=%d D=%d", who, (long long)p.T, p.Hq, p.Hkv, p.D);
+  if (p.D < 32 || p.D > 256 || p.D % 16)
+    return fail(OPSCALE_ERR_UNSUPPORTED, "%s: head_dim %d (supported: multiples of 16 in [32, 256])", who, p.D);
+  if (p.rot < 0 || p.rot > p.D) return fail(OPSCALE_ERR_INVALID_ARG, "%s: rot=%d outside [0, %d]", who, p.rot, p.D);
+  if (p.rot % 16) return fail(OPSCALE_ERR_UNSUPPORTED, "%s: rot=%d is not a multiple of 16", who, p.rot);
+  if (!(p.eps >= 0.f) || std::isinf(p.eps)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: eps must be finite and >= 0", who);
+  if (!std::isfinite(p.magnitude)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: magnitude must be finite", who);
+  if (!p.q_weight != !p.k_weight)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: q_weight and k_weight are given both or neither", who);
+  if (!p.k_cache != !p.v_cache)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: k_cache and v_cache are given both or neither", who);
+  const bool cache = p.k_cache != nullptr;
+  if (cache && (bs < 1 || nb < 1 || nb >= ((int64_t)1 << 31) || nb * bs >= ((int64_t)1 << 31)))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: block_size=%d num_blocks=%lld", who, bs, (long long)nb);
+  if (p.T == 0) return OPSCALE_OK;
+  const int s = esize(dt);
+  const int64_t vec = 16 / s, wq = (int64_t)p.Hq * p.D, wk = (int64_t)p.Hkv * p.D, most = (int64_t)1 << 24;
+  for (const int64_t st : {p.q_stride, p.q_out_stride})
+    if (st < wq || st % vec || st > most)
+      return fail(OPSCALE_ERR_INVALID_ARG, "%s: q row stride %lld must cover the heads, be a multiple of %lld and at most 2^24",
+                  who, (long long)st, (long long)vec);
+  for (const int64_t st : {p.k_stride, p.k_out_stride, cache ? p.v_stride : p.k_stride})
+    if (st < wk || st % vec || st > most)
+      return fail(OPSCALE_ERR_INVALID_ARG, "%s: k or v row stride %lld must cover the heads, be a multiple of %lld and at most 2^24",
+                  who, (long long)st, (long long)vec);
+  if (!p.q || !p.k || !p.q_out || !p.k_out || (p.rot && (!p.positions || !p.inv_freq)) ||
+      (cache && (!p.v || !p.slots)))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: null pointer", who);
+  for (const void* t : {p.q, p.k, (const void*)p.q_out, (const void*)p.k_out, p.q_weight, p.k_weight})
+    if (!aligned16(t)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+  if (cache)
+    for (const void* t : {p.v, (const void*)p.k_cache, (const void*)p.v_cache})
+      if (!aligned16(t)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned", who);
+  if (((p.rot ? reinterpret_cast<uintptr_t>(p.positions) : 0) | (cache ? reinterpret_cast<uintptr_t>(p.slots) : 0)) & 3 ||
+      (p.rot && (reinterpret_cast<uintptr_t>(p.inv_freq) & 7)))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: positions and slots must be 4-byte aligned, inv_freq 8-byte", who);
+  struct Rows {
+    const void* p;
+    int64_t stride, width;
+  };
+  const Rows q{p.q, p.q_stride * s, wq * s}, k{p.k, p.k_stride * s, wk * s}, v{p.v, p.v_stride * s, wk * s};
+  const Rows qo{p.q_out, p.q_out_stride * s, wq * s}, ko{p.k_out, p.k_out_stride * s, wk * s};
+  const auto meet = [&](const Rows& a, const Rows& b) {
+    return rows_overlap(a.p, a.stride, a.width, b.p, b.stride, b.width, p.T);
+  };
+  const bool q_in_place = p.q_out == p.q && p.q_out_stride == p.q_stride;
+  const bool k_in_place = p.k_out == p.k && p.k_out_stride == p.k_stride;
+  bool bad = meet(qo, ko) || meet(qo, k) || meet(ko, q) || (!q_in_place && meet(qo, q)) || (!k_in_place && meet(ko, k));
+  const auto extent = [&](const Rows& r) { return (p.T - 1) * r.stride + r.width; };
+  const auto touches = [&](const void* t, int64_t n) {
+    return t && n && (overlap(t, n, qo.p, extent(qo)) || overlap(t, n, ko.p, extent(ko)));
+  };
+  bad = bad || touches(p.q_weight, (int64_t)p.D * s) || touches(p.k_weight, (int64_t)p.D * s);
+  if (p.rot) bad = bad || touches(p.positions, 4 * p.T) || touches(p.inv_freq, 4ll * p.rot);
+  if (cache) {
+    bad = bad || meet(qo, v) || meet(ko, v) || touches(p.slots, 4 * p.T);
+    const int64_t n = nb * bs * wk * s;
+    bad = bad || overlap(p.k_cache, n, p.v_cache, n);
+    for (const void* c : {(const void*)p.k_cache, (const void*)p.v_cache}) {
+      for (const Rows& r : {q, k, v, qo, ko}) bad = bad || overlap(c, n, r.p, extent(r));
+      bad = bad || overlap(c, n, p.slots, 4 * p.T);
+      if (p.q_weight) bad = bad || overlap(c, n, p.q_weight, (int64_t)p.D * s) || overlap(c, n, p.k_weight, (int64_t)p.D * s);
+      if (p.rot) bad = bad || overlap(c, n, p.positions, 4 * p.T) || overlap(c, n, p.inv_freq, 4ll * p.rot);
+    }
+  }
+  if (bad) return fail(OPSCALE_ERR_INVALID_ARG, "%s: an output overlaps another tensor (q_out == q and k_out == k are allowed)", who);
+  return OPSCALE_OK;
+}
+
+opscale_status check_block_tables(const int32_t* ctx, const int32_t* fresh, int32_t B, int32_t* table, int32_t max_blocks,
+                                  int32_t bs, const int32_t* free_blocks, int64_t num_free, const int32_t* begin,
+                                  int64_t max_tokens, int32_t* cu, int32_t* positions, int32_t* slots,
+                                  int32_t* kv_lens, int32_t* next) {
+  if (B < 0) return fail(OPSCALE_ERR_INVALID_ARG, "block_tables: bad size B=%d", B);
+  if (bs < 1 || bs > 1024 || (bs & (bs - 1)))
+    return fail(OPSCALE_ERR_INVALID_ARG, "block_tables: block_size %d must be a power of two in [1, 1024]", bs);
+  if (max_blocks < 1 || (int64_t)max_blocks * bs >= kMaxDim || num_free < 0 || num_free >= kMaxDim || max_tokens < 0 ||
+      max_tokens >= kMaxDim)
+    return fail(OPSCALE_ERR_INVALID_ARG, "block_tables: max_blocks_per_seq=%d num_free=%lld max_tokens=%lld", max_blocks,
+                (long long)num_free, (long long)max_tokens);
+  if (!begin || !cu || !next || (B > 0 && (!ctx || !fresh || !table || !kv_lens)) || (num_free > 0 && !free_blocks) ||
+      (max_tokens > 0 && (!positions || !slots)))
+    return fail(OPSCALE_ERR_INVALID_ARG, "block_tables: null pointer");
+  struct Ints {
+    const int32_t* p;
+    int64_t n;
+  };
+  const Ints in[] = {{ctx, B}, {fresh, B}, {free_blocks, num_free}, {begin, 1}};
+  const Ints out[] = {{table, (int64_t)B * max_blocks}, {cu, (int64_t)B + 1}, {positions, max_tokens},
+                      {slots, max_tokens}, {kv_lens, B}, {next, 1}};
+  for (const Ints& o : out) {
+    if (o.n == 0) continue;
+    if (reinterpret_cast<uintptr_t>(o.p) & 3) return fail(OPSCALE_ERR_INVALID_ARG, "block_tables: arrays must be 4-byte aligned");
+    for (const Ints& i : in) {
+      if (i.n == 0) continue;
+      if (reinterpret_cast<uintptr_t>(i.p) & 3)
+        return fail(OPSCALE_ERR_INVALID_ARG, "block_tables: arrays must be 4-byte aligned");
+      if (overlap(o.p, 4 * o.n, i.p, 4 * i.n))
+        return fail(OPSCALE_ERR_INVALID_ARG, "block_tables: an output overlaps another array");
+    }
+    for (const Ints& u : out)
+      if (&u != &o && u.n && overlap(o.p, 4 * o.n, u.p, 4 * u.n))
+        return fail(OPSCALE_ERR_INVALID_ARG, "block_tables: an output overlaps another array");
+  }
+  return OPSCALE_OK;
+}
+
 opscale_status check_add_rmsnorm(const void* x, void* res, const void* w, void* y, int64_t M, int64_t H, float eps,
                                  opscale_dtype dt) {
   opscale_status st = check_rmsnorm(x, w, y, M, H, eps, dt);
@@ -430,6 +560,16 @@ opscale_status check_fused_moe(const void* x, const void* w1, const void* w2, co
   if (ws_bytes < need)
     return fail(OPSCALE_ERR_WORKSPACE, "fused_moe: workspace of %zu bytes, %zu needed", ws_bytes, need);
   return OPSCALE_OK;
+}
+
+opscale::QkNormRope qk_norm_rope_args(const void* q, const void* k, int64_t qs, int64_t ks, void* qo, void* ko,
+                                      int64_t qos, int64_t kos, const void* wq, const void* wk, float eps,
+                                      const int32_t* pos, const double* freq, int32_t rot, int32_t interleaved,
+                                      float magnitude, const void* v, int64_t vs, void* kc, void* vc,
+                                      const int32_t* slots, int32_t bs, int64_t nb, int64_t T, int32_t Hq,
+                                      int32_t Hkv, int32_t D) {
+  return {q, k, qs, ks, qo, ko, qos, kos, wq, wk, eps, pos, freq, rot, interleaved != 0, magnitude, v, vs, kc, vc,
+          slots, kc ? (int64_t)((uint64_t)nb * (uint64_t)bs) : 0, T, Hq, Hkv, D};
 }
 
 // Median with linear interpolation between the two middle values (the
@@ -730,6 +870,91 @@ opscale_status opscale_add_rmsnorm(const void* x, void* residual, const void* w,
     const Work wk = work_add_rmsnorm(M, H, esize(dt));
     timing->alg_flops = wk.flops;
     timing->alg_bytes = wk.bytes;
+  }
+  return st;
+}
+
+opscale_status opscale_rope_frequencies(double* inv_freq, float* magnitude, int32_t rot, double theta,
+                                        opscale_rope_scaling scaling, double factor, double low, double high,
+                                        int64_t original_len) {
+  const char* who = "rope_frequencies";
+  if (!inv_freq || !magnitude) return fail(OPSCALE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (rot < 2 || rot > 256 || rot % 2) return fail(OPSCALE_ERR_INVALID_ARG, "%s: rot=%d must be even, in [2, 256]", who, rot);
+  if (!(theta > 1.0) || !std::isfinite(theta)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: theta must be finite and > 1", who);
+  if (scaling != OPSCALE_ROPE_NONE && scaling != OPSCALE_ROPE_LINEAR && scaling != OPSCALE_ROPE_BANDS &&
+      scaling != OPSCALE_ROPE_RAMP)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: unknown scaling %d", who, (int)scaling);
+  if (scaling != OPSCALE_ROPE_NONE && (!(factor >= 1.0) || !std::isfinite(factor)))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: factor must be finite and >= 1", who);
+  const bool mixed = scaling == OPSCALE_ROPE_BANDS || scaling == OPSCALE_ROPE_RAMP;
+  if (mixed && (!(low > 0.0) || !(high > low) || !std::isfinite(high) || original_len < 1))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: 0 < low < high and original_len >= 1 required", who);
+  constexpr double two_pi = 6.283185307179586476925286766559;
+  const double len = (double)original_len;
+  // the pair index that turns `turns` times over the original length
+  const auto pair_at = [&](double turns) { return rot * std::log(len / (turns * two_pi)) / (2.0 * std::log(theta)); };
+  const double first = mixed ? std::max(std::floor(pair_at(high)), 0.0) : 0.0;
+  const double last = mixed ? std::min(std::ceil(pair_at(low)), rot - 1.0) : 0.0;
+  for (int i = 0; i < rot / 2; ++i) {
+    const double f = std::pow(theta, -2.0 * i / rot);
+    double kept = 1.0;  // share of the unscaled frequency
+    if (scaling == OPSCALE_ROPE_LINEAR) kept = 0.0;
+    if (scaling == OPSCALE_ROPE_BANDS) kept = std::clamp((len * f / two_pi - low) / (high - low), 0.0, 1.0);
+    if (scaling == OPSCALE_ROPE_RAMP) kept = 1.0 - std::clamp((i - first) / std::max(last - first, 1e-3), 0.0, 1.0);
+    inv_freq[i] = kept * f + (1.0 - kept) * f / (scaling == OPSCALE_ROPE_NONE ? 1.0 : factor);
+  }
+  *magnitude = scaling == OPSCALE_ROPE_RAMP ? (float)(0.1 * std::log(factor) + 1.0) : 1.f;
+  return OPSCALE_OK;
+}
+
+opscale_status opscale_qk_norm_rope(const void* q, const void* k, int64_t q_row_stride, int64_t k_row_stride,
+                                    void* q_out, void* k_out, int64_t q_out_row_stride, int64_t k_out_row_stride,
+                                    const void* q_weight, const void* k_weight, float eps, const int32_t* positions,
+                                    const double* inv_freq, int32_t rot, int32_t interleaved, float magnitude,
+                                    const void* v, int64_t v_row_stride, void* k_cache, void* v_cache,
+                                    const int32_t* slot_mapping, int32_t block_size, int64_t num_blocks, int64_t T,
+                                    int32_t Hq, int32_t Hkv, int32_t D, opscale_dtype dt, hipStream_t stream,
+                                    opscale_timing* timing) {
+  const opscale::QkNormRope p = qk_norm_rope_args(q, k, q_row_stride, k_row_stride, q_out, k_out, q_out_row_stride,
+                                                  k_out_row_stride, q_weight, k_weight, eps, positions, inv_freq, rot,
+                                                  interleaved, magnitude, v, v_row_stride, k_cache, v_cache,
+                                                  slot_mapping, block_size, num_blocks, T, Hq, Hkv, D);
+  opscale_status st = check_qk_norm_rope(p, block_size, num_blocks, dt);
+  if (st != OPSCALE_OK) return st;
+  zero_timing(timing);
+  if (T == 0) return OPSCALE_OK;
+  st = run_timed(stream, timing, "qk_norm_rope launch",
+                 [&] { return opscale::launch_qk_norm_rope(p, dt == OPSCALE_BF16, stream); });
+  if (st == OPSCALE_OK && timing) {
+    const Work wk = work_qk_norm_rope(p, esize(dt));
+    timing->alg_flops = wk.flops;
+    timing->alg_bytes = wk.bytes;
+  }
+  return st;
+}
+
+opscale_status opscale_block_tables(const int32_t* context_lens, const int32_t* new_lens, int32_t B,
+                                    int32_t* block_table, int32_t max_blocks_per_seq, int32_t block_size,
+                                    const int32_t* free_blocks, int64_t num_free, const int32_t* free_begin,
+                                    int64_t max_tokens, int32_t* cu_seqlens, int32_t* positions,
+                                    int32_t* slot_mapping, int32_t* kv_lens, int32_t* free_next, hipStream_t stream,
+                                    opscale_timing* timing) {
+  opscale_status st = check_block_tables(context_lens, new_lens, B, block_table, max_blocks_per_seq, block_size,
+                                         free_blocks, num_free, free_begin, max_tokens, cu_seqlens, positions,
+                                         slot_mapping, kv_lens, free_next);
+  if (st != OPSCALE_OK) return st;
+  zero_timing(timing);
+  st = run_timed(stream, timing, "block_tables launch", [&] {
+    return opscale::launch_block_tables(context_lens, new_lens, B, block_table, max_blocks_per_seq, block_size,
+                                        free_blocks, num_free, free_begin, max_tokens, cu_seqlens, positions,
+                                        slot_mapping, kv_lens, free_next, stream);
+  });
+  if (st == OPSCALE_OK && timing) {
+    std::vector<int32_t> begin, next;
+    if ((st = copy_ints(begin, free_begin, 1, stream)) != OPSCALE_OK) return st;
+    if ((st = copy_ints(next, free_next, 1, stream)) != OPSCALE_OK) return st;
+    timing->alg_flops = 0.0;  // (integers)
+    timing->alg_bytes = 4.0 * (4.0 * B + 3.0 + 2.0 * (double)max_tokens + 2.0 * ((double)next[0] - (double)begin[0]));
   }
   return st;
 }

@@ -119,6 +119,35 @@ hipError_t launch_cache_write(const void* k, const void* v, int64_t kv_stride, v
                               const int32_t* slots, int64_t T, int32_t Hkv, int32_t D, int64_t num_slots,
                               bool bf16, hipStream_t s);
 
+// Norm of the query and key heads, rotation and cache write (opscale_qk_norm_rope's
+// arguments; strides in elements, num_slots = num_blocks * block_size).
+struct QkNormRope {
+  const void *q, *k;
+  int64_t q_stride, k_stride;
+  void *q_out, *k_out;
+  int64_t q_out_stride, k_out_stride;
+  const void *q_weight, *k_weight;
+  float eps;
+  const int32_t* positions;
+  const double* inv_freq;
+  int32_t rot;
+  bool interleaved;
+  float magnitude;
+  const void* v;
+  int64_t v_stride;
+  void *k_cache, *v_cache;
+  const int32_t* slots;
+  int64_t num_slots, T;
+  int32_t Hq, Hkv, D;
+};
+hipError_t launch_qk_norm_rope(const QkNormRope& p, bool bf16, hipStream_t s);
+
+// The tables of a step (opscale_block_tables).
+hipError_t launch_block_tables(const int32_t* ctx, const int32_t* fresh, int32_t B, int32_t* table, int32_t max_blocks,
+                               int32_t block_size, const int32_t* free_blocks, int64_t num_free,
+                               const int32_t* free_begin, int64_t max_tokens, int32_t* cu, int32_t* positions,
+                               int32_t* slots, int32_t* kv_lens, int32_t* free_next, hipStream_t s);
+
 // residual <- x + residual; y <- rmsnorm(residual) * w.
 hipError_t launch_add_rmsnorm(const void* x, void* res, const void* w, void* y, int64_t M, int64_t H, float eps,
                               bool bf16, hipStream_t s);
