@@ -389,6 +389,37 @@ opscale_status opscale_block_tables(const int32_t* context_lens, const int32_t* 
                                     int32_t* slot_mapping, int32_t* kv_lens, int32_t* free_next, hipStream_t stream,
                                     opscale_timing* timing);
 
+/*
+ * Score modifiers and masks of attention.  For the query at local position i of
+ * prompt or sequence b, head h, and the key at j:
+ *   s = scale * q . k;  s <- softcap * tanh(s / softcap)  (softcap > 0);
+ *   s <- s - slopes[h] * |i - j|                          (slopes given).
+ * Key j is visible iff j < prefix_lens[b] (the prefix, seen by every token), or
+ *   j >= doc_starts[.] and |i - j| < window (window > 0) and j <= i (causal).
+ * A query that sees no key gets a zero row.
+ */
+typedef struct {
+  float softcap;              /* 0: none; finite and >= 0 */
+  int32_t window;             /* 0: none; >= 0 */
+  const float* slopes;        /* DEVICE fp32 [Hq], finite, or NULL */
+  const int32_t* prefix_lens; /* DEVICE int32 [B] or NULL (0); values outside [0, length] count as the nearer end */
+  const int32_t* doc_starts;  /* DEVICE int32, or NULL (0): the first key of the query's document, one for each
+                                 token in prefill ([total_tokens], local to its prompt), one for each
+                                 sequence in decode ([B]).  Values below 0 count as 0, values past the prompt
+                                 leave the query its prefix (padding). */
+} opscale_attn_mods;
+
+/*
+ * opscale_attn_prefill with score modifiers and masks (its arguments, layouts
+ * and conditions; mods NULL: none; o overlaps no input).  A masked key has no part
+ * in a row, whatever its K and V rows hold (infinities and NaN among it).
+ */
+opscale_status opscale_attn_prefill_mod(const void* q, const void* k, const void* v, int64_t q_row_stride,
+                                        int64_t kv_row_stride, void* o, const int32_t* cu_seqlens, int32_t B,
+                                        int64_t total_tokens, int32_t max_seqlen, int32_t Hq, int32_t Hkv, int32_t D,
+                                        float scale, int32_t causal, const opscale_attn_mods* mods, opscale_dtype dt,
+                                        hipStream_t stream, opscale_timing* timing);
+
 /* ---------------------------------------------------------------------------
  * Operator profiling (Section 4.2 "Operator Profiling": per-operator compute
  * time T_v and memory M_v; Appendix C "Dataflow Characteristics": the payload

@@ -86,6 +86,10 @@ class _FusedMoeArgs(ctypes.Structure):
                 ("workspace_bytes", c_sz)]
 
 
+class AttnMods(ctypes.Structure):
+    _fields_ = [("softcap", c_f32), ("window", c_i32), ("slopes", c_vp), ("prefix_lens", c_vp), ("doc_starts", c_vp)]
+
+
 class _OpUnion(ctypes.Union):
     _fields_ = [("rmsnorm", _RmsnormArgs), ("linear", _LinearArgs), ("swiglu", _SwigluArgs),
                 ("attn_prefill", _PrefillArgs), ("attn_decode", _DecodeArgs), ("rope", _RopeArgs),
@@ -153,6 +157,9 @@ EXPORTS = {
                                           c_i32, c_vp, ctypes.POINTER(Timing)]),
     "opscale_add_rmsnorm": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_i64, c_i64, c_f32, c_i32, c_vp,
                                     ctypes.POINTER(Timing)]),
+    "opscale_attn_prefill_mod": (c_i32, [c_vp, c_vp, c_vp, c_i64, c_i64, c_vp, c_vp, c_i32, c_i64, c_i32, c_i32, c_i32,
+                                         c_i32, c_f32, c_i32, ctypes.POINTER(AttnMods), c_i32, c_vp,
+                                         ctypes.POINTER(Timing)]),
     "opscale_rope_frequencies": (c_i32, [ctypes.POINTER(c_f64), ctypes.POINTER(c_f32), c_i32, c_f64, c_i32, c_f64,
                                          c_f64, c_f64, c_i64]),
     "opscale_qk_norm_rope": (c_i32, [c_vp, c_vp, c_i64, c_i64, c_vp, c_vp, c_i64, c_i64, c_vp, c_vp, c_f32, c_vp,
@@ -526,7 +533,7 @@ def opscale_rope_frequencies(rot: int, theta: float, scaling: str = "none", fact
     return torch.tensor(list(f), dtype=torch.float64, device=device), m.value
 
 
-_i32, _f64 = None, None  # torch's dtypes, filled on first use
+_i32, _f32, _f64 = None, None, None  # torch's dtypes, filled on first use
 
 
 def _here(*named) -> None:
@@ -627,6 +634,55 @@ def opscale_qk_norm_rope(q, k, positions=None, inv_freq=None, q_weight=None, k_w
                                     magnitude, _ptr(v), vs, _ptr(k_cache), _ptr(v_cache), _ptr(slot_mapping), bs, nb,
                                     T, Hq, Hkv, D, dt, _stream(stream), ctypes.byref(t) if t else None))
     return ((q_out, k_out), t) if timed else (q_out, k_out)
+
+
+def _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, rows):
+    """The score modifiers and masks of an attention call over B prompts or sequences."""
+    global _f32
+    if slopes is not None:
+        if _f32 is None:
+            import torch
+            _f32 = torch.float32
+        _here(("slopes", slopes))
+        _weight("slopes", slopes, Hq, _f32)
+    if prefix_lens is not None:
+        _ints(("prefix_lens", prefix_lens), size=B)
+    if doc_starts is not None:
+        _ints(("doc_starts", doc_starts), size=rows)
+    if not 0 <= window < 1 << 31:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"window {window} must be in [0, 2^31)")
+    return AttnMods(softcap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(doc_starts))
+
+
+def opscale_attn_prefill_mod(q, k, v, cu_seqlens, max_seqlen: int, scale: float, causal: bool = True,
+                             softcap: float = 0.0, slopes=None, window: int = 0, prefix_lens=None, doc_starts=None,
+                             out=None, stream=None, timed: bool = False):
+    """opscale_attn_prefill with score modifiers and masks: scores capped at
+    softcap by a tanh, lowered by slopes[h] (float32 [Hq]) a key of distance; a key
+    is seen in the prefix (prefix_lens int32 [B]), or in the query's document
+    (doc_starts int32 [T], its first key, local to the prompt), fewer than `window`
+    keys away and, causal, not ahead.  A query that sees no key gets zeros."""
+    lib = load()
+    dt, dtype = _dt(q), q.dtype
+    if q.dim() != 3 or k.dim() != 3:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "q and k must be [T, heads, D]")
+    T, Hq, D = q.shape
+    Hkv = k.shape[1]
+    if out is None:
+        out = q.new_empty((T, Hq, D))
+    _here(("q", q), ("k", k), ("v", v), ("out", out))
+    qs, ks, vs = _rows("q", q, T, Hq, D, dtype), _rows("k", k, T, Hkv, D, dtype), _rows("v", v, T, Hkv, D, dtype)
+    if ks != vs:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "k and v must share a row stride")
+    _weight("out", out, T * Hq * D, dtype)
+    B = cu_seqlens.numel() - 1
+    _ints(("cu_seqlens", cu_seqlens))
+    mods = _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, T)
+    t = Timing() if timed else None
+    _check(lib.opscale_attn_prefill_mod(_ptr(q), _ptr(k), _ptr(v), qs, ks, _ptr(out), _ptr(cu_seqlens), B, T,
+                                        max_seqlen, Hq, Hkv, D, scale, int(causal), ctypes.byref(mods), dt,
+                                        _stream(stream), ctypes.byref(t) if t else None))
+    return (out, t) if timed else out
 
 
 def opscale_block_tables(context_lens, new_lens, block_table, free_blocks, free_begin, block_size: int,

@@ -146,6 +146,25 @@ Work work_prefill(const std::vector<int32_t>& cu, int64_t Hq, int64_t Hkv, int64
   const int64_t tb = (int64_t)s * (2 * T * Hq * D + 2 * T * Hkv * D);
   return {4.0 * D * Hq * pairs, (double)tb, 0, tb, (int64_t)s * T * Hq * D};
 }
+// Keys of [0, n) that the query at i sees (start: of its document).
+int64_t keys_seen(int64_t i, int64_t n, bool causal, int64_t window, int64_t prefix, int64_t start) {
+  prefix = std::min(std::max<int64_t>(prefix, 0), n);
+  int64_t lo = std::max<int64_t>(start, 0), hi = causal ? i : n - 1;
+  if (window > 0) lo = std::max(lo, i - window + 1), hi = std::min(hi, i + window - 1);
+  return prefix + std::max<int64_t>(0, hi - std::max(lo, prefix) + 1);
+}
+Work work_prefill_mod(const std::vector<int32_t>& cu, const std::vector<int32_t>& prefix,
+                      const std::vector<int32_t>& starts, int64_t window, int64_t Hq, int64_t Hkv, int64_t D, int s,
+                      bool causal) {
+  double pairs = 0;
+  for (size_t b = 0; b + 1 < cu.size(); ++b)
+    for (int64_t i = 0, n = cu[b + 1] - cu[b]; i < n; ++i)
+      pairs += (double)keys_seen(i, n, causal, window, prefix.empty() ? 0 : prefix[b],
+                                 starts.empty() ? 0 : starts[(size_t)(cu[b] + i)]);
+  Work wk = work_prefill(cu, Hq, Hkv, D, s, causal);
+  wk.flops = 4.0 * D * Hq * pairs;
+  return wk;
+}
 Work work_decode(const std::vector<int32_t>& ctx, int64_t Hq, int64_t Hkv, int64_t D, int s, int64_t bs,
                  int64_t max_blocks) {
   double N = 0, nb = 0;
@@ -305,6 +324,32 @@ opscale_status check_prefill(const void* q, const void* k, const void* v, int64_
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(o) || (reinterpret_cast<uintptr_t>(cu) & 3))
     return fail(OPSCALE_ERR_INVALID_ARG, "attn_prefill: q, k, v, o must be 16-byte aligned, cu_seqlens 4-byte");
   if ((int64_t)B * Hkv * Hq >= kMaxDim) return fail(OPSCALE_ERR_UNSUPPORTED, "attn_prefill: batch too large");
+  return OPSCALE_OK;
+}
+
+opscale_status check_mods(const char* who, const opscale_attn_mods* m) {
+  if (!m) return OPSCALE_OK;
+  if (!(m->softcap >= 0.f) || !std::isfinite(m->softcap))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: softcap must be finite and >= 0", who);
+  if (m->window < 0) return fail(OPSCALE_ERR_INVALID_ARG, "%s: window %d must be >= 0", who, m->window);
+  if ((reinterpret_cast<uintptr_t>(m->slopes) | reinterpret_cast<uintptr_t>(m->prefix_lens) |
+       reinterpret_cast<uintptr_t>(m->doc_starts)) & 3)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: slopes, prefix_lens and doc_starts must be 4-byte aligned", who);
+  return OPSCALE_OK;
+}
+
+opscale_status check_prefill_mod(const void* q, const void* k, const void* v, int64_t qs, int64_t kvs, void* o,
+                                 const int32_t* cu, int32_t B, int64_t T, int32_t max_seqlen, int32_t Hq, int32_t Hkv,
+                                 int32_t D, float scale, const opscale_attn_mods* m, opscale_dtype dt) {
+  opscale_status st = check_prefill(q, k, v, qs, kvs, o, cu, B, T, max_seqlen, Hq, Hkv, D, scale, dt);
+  if (st == OPSCALE_OK) st = check_mods("attn_prefill_mod", m);
+  if (st != OPSCALE_OK || B == 0 || T == 0) return st;
+  const int s = esize(dt);
+  const int64_t no = T * Hq * D * s, nq = ((T - 1) * qs + (int64_t)Hq * D) * s, nkv = ((T - 1) * kvs + (int64_t)Hkv * D) * s;
+  if (overlap(o, no, q, nq) || overlap(o, no, k, nkv) || overlap(o, no, v, nkv) || overlap(o, no, cu, 4ll * (B + 1)) ||
+      (m && ((m->slopes && overlap(o, no, m->slopes, 4ll * Hq)) || (m->prefix_lens && overlap(o, no, m->prefix_lens, 4ll * B)) ||
+             (m->doc_starts && overlap(o, no, m->doc_starts, 4 * T)))))
+    return fail(OPSCALE_ERR_INVALID_ARG, "attn_prefill_mod: o must not overlap an input");
   return OPSCALE_OK;
 }
 
@@ -868,6 +913,34 @@ opscale_status opscale_add_rmsnorm(const void* x, void* residual, const void* w,
   });
   if (st == OPSCALE_OK && timing) {
     const Work wk = work_add_rmsnorm(M, H, esize(dt));
+    timing->alg_flops = wk.flops;
+    timing->alg_bytes = wk.bytes;
+  }
+  return st;
+}
+
+opscale_status opscale_attn_prefill_mod(const void* q, const void* k, const void* v, int64_t q_row_stride,
+                                        int64_t kv_row_stride, void* o, const int32_t* cu_seqlens, int32_t B,
+                                        int64_t total_tokens, int32_t max_seqlen, int32_t Hq, int32_t Hkv, int32_t D,
+                                        float scale, int32_t causal, const opscale_attn_mods* mods, opscale_dtype dt,
+                                        hipStream_t stream, opscale_timing* timing) {
+  opscale_status st = check_prefill_mod(q, k, v, q_row_stride, kv_row_stride, o, cu_seqlens, B, total_tokens,
+                                        max_seqlen, Hq, Hkv, D, scale, mods, dt);
+  if (st != OPSCALE_OK) return st;
+  zero_timing(timing);
+  if (B == 0 || total_tokens == 0) return OPSCALE_OK;
+  st = run_timed(stream, timing, "attn_prefill_mod launch", [&] {
+    return opscale::launch_attn_prefill_mod(q, k, v, q_row_stride, kv_row_stride, o, cu_seqlens, B, total_tokens,
+                                            max_seqlen, Hq, Hkv, D, scale, causal != 0, mods, dt == OPSCALE_BF16,
+                                            stream);
+  });
+  if (st == OPSCALE_OK && timing) {
+    std::vector<int32_t> cu, prefix, starts;
+    if ((st = copy_ints(cu, cu_seqlens, (int64_t)B + 1, stream)) != OPSCALE_OK) return st;
+    if (mods && mods->prefix_lens && (st = copy_ints(prefix, mods->prefix_lens, B, stream)) != OPSCALE_OK) return st;
+    if (mods && mods->doc_starts && (st = copy_ints(starts, mods->doc_starts, total_tokens, stream)) != OPSCALE_OK)
+      return st;
+    const Work wk = work_prefill_mod(cu, prefix, starts, mods ? mods->window : 0, Hq, Hkv, D, esize(dt), causal != 0);
     timing->alg_flops = wk.flops;
     timing->alg_bytes = wk.bytes;
   }

@@ -1,0 +1,67 @@
+// Score modifiers and masks of the attention kernels (opscale_attn_mods), as the
+// kernels take them.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "opscale.h"
+
+namespace opscale {
+
+// What a kernel is compiled for: 0 for plain attention, else kMod (masks, taken
+// from the arguments) with the modifiers that cost work per score.
+constexpr int kMod = 1, kCap = 2, kBias = 4;
+
+struct AttnMods {
+  const float* slopes;
+  const int32_t *prefix, *starts;
+  int32_t window;
+  float softcap;
+  // softcap * tanh(scale * x / softcap) of a raw score x = q . k, in log2 units:
+  // cap_log2 * tanh, e^2y = 2^(cap_rate x), and for |x| <= cap_bound
+  // x * P(x^2) with P of degree 3
+  float cap_log2, cap_rate, cap_bound, cap_poly[4];
+
+  __device__ __forceinline__ float capped_small(float x) const {
+    const float u = x * x;
+    return x * fmaf(u, fmaf(u, fmaf(u, cap_poly[3], cap_poly[2]), cap_poly[1]), cap_poly[0]);
+  }
+  // To a few steps of fp32 at cap_log2, any x (an infinity gives +-cap_log2).
+  __device__ __forceinline__ float capped(float x) const {
+    const float e = __builtin_amdgcn_exp2f(x * cap_rate);
+    return fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(1.f + e), cap_log2);
+  }
+
+  // A score on the fp32 path: x = scale * q . k, d = |i - j|.
+  __device__ __forceinline__ float score(float x, float slope, float d) const {
+    if (softcap > 0.f) x = softcap * tanhf(x / softcap);
+    return fmaf(-slope, d, x);
+  }
+};
+
+inline AttnMods make_attn_mods(const opscale_attn_mods* m, float scale) {
+  AttnMods a{};
+  if (!m) return a;
+  a.slopes = m->slopes, a.prefix = m->prefix_lens, a.starts = m->doc_starts;
+  a.window = m->window, a.softcap = m->softcap;
+  if (m->softcap > 0.f) {
+    constexpr double log2e = 1.4426950408889634;
+    // tanh(y) = y P(y^2) for |y| <= 1/2, to 5.5e-7 of itself (least largest
+    // relative error at this degree)
+    constexpr double p[4] = {0.99999946, -0.33326318, 0.13190297, -0.04440223};
+    const double cap = m->softcap, y = (double)scale / cap;  // y: of one raw unit
+    a.cap_log2 = (float)(cap * log2e);
+    a.cap_rate = (float)(2.0 * log2e * y);
+    a.cap_bound = (float)(0.5 / y);
+    double f = cap * log2e * y;
+    for (int i = 0; i < 4; ++i, f *= y * y) a.cap_poly[i] = (float)(p[i] * f);
+  }
+  return a;
+}
+
+// Whether the kernels have anything to do beyond plain attention, and what.
+inline int attn_mode(const opscale_attn_mods* m) {
+  return kMod | (m && m->softcap > 0.f ? kCap : 0) | (m && m->slopes ? kBias : 0);
+}
+
+}  // namespace opscale

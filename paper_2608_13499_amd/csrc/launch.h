@@ -97,6 +97,12 @@ hipError_t launch_attn_prefill(const void* q, const void* k, const void* v, int6
                                int64_t total_tokens, int32_t max_seqlen, int32_t Hq, int32_t Hkv,
                                int32_t D, float scale, bool causal, bool bf16, hipStream_t s);
 
+// The same with score modifiers and masks (m may be null).
+hipError_t launch_attn_prefill_mod(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride,
+                                   void* o, const int32_t* cu, int32_t B, int64_t total_tokens, int32_t max_seqlen,
+                                   int32_t Hq, int32_t Hkv, int32_t D, float scale, bool causal,
+                                   const opscale_attn_mods* m, bool bf16, hipStream_t s);
+
 // Balanced split-KV decode: workgroups of a launch (each takes an equal range
 // of the batch's 32-key tiles) and the workspace it needs (the tile prefix
 // sums, then (workgroups + B) x Hq partial results of D + 2 floats).

@@ -1,0 +1,314 @@
+"""GPU parity of attention with score modifiers and masks, prefill and paged
+decode, against the 64-bit definitions in oracle.step.
+
+Tolerance.  With p the probabilities and A = sum p |v| / sum p of an output element
+(the oracle's result with |v| for v):
+  * bf16: a probability is rounded to bf16 for its product with V and not for the
+    sum (2^-8 A), the result once (2^-8 |o|);
+  * a score's error e changes its probability by the factor 1 +- e, the quotient by
+    2 e A at most.  e counts, in u = 2^-24: the products' sum, D roundings of
+    scale |q| . |k| at worst; the cap's 5.5e-7 (10 u) and 6 roundings of the capped
+    score; the bias's 10 roundings of slope |i - j|, for the keys that count (a
+    score 30 below its row's largest does not);
+  * the sums over n keys, n u A each at worst.
+"""
+import math
+
+import numpy as np
+import pytest
+
+import workloads as wl
+from oracle import step
+from parity_util import cuda, f64, gen, say
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def ops():
+    import torch
+    assert torch.cuda.is_available()
+    import paper_2608_13499_amd as ops
+    ops.load()
+    return ops
+
+
+def i32(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, np.int32)).cuda()
+
+
+def f32(a):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(a, np.float32)).cuda()
+
+
+def tolerance(ref, weighted, dtype, D, n, dot, cap, bias):
+    """dot: the largest scale |q| . |k|; bias: the largest slope |i - j| that counts."""
+    e = D * U * dot + (16 * U * min(cap, dot) if cap else 2 * U * dot) + 10 * U * bias
+    tol = (2 * e + 2 * (n + 64) * U) * weighted
+    return tol + (2.0 ** -8 * (weighted + np.abs(ref)) if dtype == "bf16" else 2 * U * np.abs(ref)) + 1e-30
+
+
+def near(got, ref, tol, what):
+    got = np.asarray(got, np.float64)
+    assert np.isfinite(got).all(), f"{what}: not finite at {np.argwhere(~np.isfinite(got))[:4].tolist()}"
+    r = np.abs(got - ref) / tol
+    say(f"  {what}: {r.max():.3f} of the tolerance")
+    assert r.max() <= 1.0, f"{what}: {r.max():.3f} of the tolerance at {np.unravel_index(r.argmax(), r.shape)}"
+
+
+def slopes_of(H):
+    return np.float32(2.0 ** (-8.0 * (1 + np.arange(H)) / H))
+
+
+def rules(name, lens, Hq, seed=0):
+    """Named modifiers of a batch: (arguments of the oracle, causal)."""
+    rng = np.random.default_rng([seed, len(lens), int(np.sum(lens))])
+    n = int(max(lens, default=1))
+    starts = []
+    for L in lens:
+        s = np.zeros(L, np.int64)
+        for c in sorted(rng.integers(0, L + 1, 3)):
+            s[c:] = c
+        if L > 4:
+            s[L - 2:] = [L, 10 * L]  # padding: past the prompt
+        starts.append(s)
+    starts = np.concatenate(starts) if lens else np.zeros(0, np.int64)
+    prefix = np.array([rng.integers(-1, L + 3) for L in lens])
+    return {
+        "none": (dict(), True),
+        "cap": (dict(softcap=5.0), True),
+        "cap_wide": (dict(softcap=1000.0), True),
+        "bias": (dict(slopes=slopes_of(Hq)), True),
+        "cap_bias": (dict(softcap=8.0, slopes=slopes_of(Hq)), True),
+        "window1": (dict(window=1), True),
+        "window": (dict(window=max(1, n // 5), softcap=5.0), True),
+        "window_all": (dict(window=2 ** 31 - 1), True),
+        "prefix": (dict(prefix_lens=prefix, softcap=5.0), True),
+        "prefix_bias": (dict(prefix_lens=prefix, slopes=slopes_of(Hq)), True),
+        "docs": (dict(doc_starts=starts, slopes=slopes_of(Hq)), True),
+        "docs_prefix_window": (dict(doc_starts=starts, prefix_lens=prefix, window=max(1, n // 3), softcap=5.0,
+                                    slopes=slopes_of(Hq)), True),
+        "open": (dict(softcap=5.0), False),
+        "open_window_bias": (dict(window=max(1, n // 6), slopes=slopes_of(Hq)), False),
+        "open_docs_prefix": (dict(doc_starts=starts, prefix_lens=prefix), False),
+    }[name]
+
+
+RULES = ["none", "cap", "cap_wide", "bias", "cap_bias", "window1", "window", "window_all", "prefix", "prefix_bias",
+         "docs", "docs_prefix_window", "open", "open_window_bias", "open_docs_prefix"]
+
+
+def on_gpu(kw):
+    d = dict(kw)
+    for n in ("prefix_lens", "doc_starts"):
+        if d.get(n) is not None:
+            d[n] = i32(d[n])
+    if d.get("slopes") is not None:
+        d["slopes"] = f32(d["slopes"])
+    return d
+
+
+def heads(seed, T, Hq, Hkv, D, dtype, std=1.5):
+    """A packed QKV tensor and its views."""
+    qkv = gen(seed, "q", (T, (Hq + 2 * Hkv) * D), dtype, std)
+    return qkv, [qkv[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in
+                 ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv))]
+
+
+def counted(kw, n):
+    """The largest slope * distance whose key can count against one 30 higher."""
+    s = kw.get("slopes")
+    return 0.0 if s is None else float(min(n * np.max(s), 30 + n * np.max(s)))
+
+
+def check_prefill(ops, dtype, lens, Hq, Hkv, D, name, seed=61, rows=None, stream=None, std=1.5):
+    import torch
+    kw, causal = rules(name, lens, Hq, seed) if isinstance(name, str) else name
+    say(f"attn_prefill_mod {dtype} lens={lens if len(lens) < 9 else len(lens)} Hq={Hq} Hkv={Hkv} D={D} {name}")
+    T, cu = int(np.sum(lens)), wl.cu_seqlens(lens)
+    qkv, views = heads(seed, T, Hq, Hkv, D, dtype, std)
+    dev = cuda(qkv)
+    q, k, v = (dev[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+    scale = 1.0 / math.sqrt(D)
+    out = torch.full((T, Hq, D), float("nan"), dtype=dev.dtype, device="cuda")
+    ops.opscale_attn_prefill_mod(q, k, v, i32(cu), max(1, max(lens)), scale, causal, out=out, stream=stream, **on_gpu(kw))
+    torch.cuda.synchronize()
+    qh, kh, vh = (f64(t) for t in views)
+    if rows is not None:
+        rng = np.random.default_rng(seed)
+        rows = [(int(t), int(h)) for t, h in zip(np.r_[0, T - 1, rng.integers(0, T, rows)], rng.integers(0, Hq, rows + 2))]
+    ref, weighted = (step.attn_prefill_mod(qh, kh, x, cu, scale, causal, rows=rows, **kw) for x in (vh, np.abs(vh)))
+    got = f64(out.cpu())
+    got = got if rows is None else np.stack([got[t, h] for t, h in rows])
+    n = max(lens)
+    dot = scale * np.abs(qh).sum(-1).max() * np.abs(kh).max() if T else 0.0
+    near(got, ref, tolerance(ref, weighted, dtype, D, n, dot, kw.get("softcap"), counted(kw, n)), str(name)[:40])
+    return out
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", RULES)
+def test_prefill_rules(ops, dtype, name):
+    check_prefill(ops, dtype, [150, 0, 1, 67, 33], 8, 2, 128, name)
+    check_prefill(ops, dtype, [97, 40], 6, 6, 64, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("L", [1, 2, 31, 32, 33, 63, 64, 65, 127, 128, 129, 191, 193, 300])
+def test_prefill_lengths(ops, dtype, L):
+    for name in ("cap", "docs_prefix_window", "open_window_bias"):
+        check_prefill(ops, dtype, [L], 4, 1, 64, name)
+
+
+@pytest.mark.parametrize("Hq,Hkv,D", [(1, 1, 64), (3, 1, 128), (7, 1, 128), (28, 4, 64), (12, 6, 128), (16, 2, 64),
+                                      (24, 2, 128), (71, 1, 64)])
+def test_prefill_head_layouts(ops, Hq, Hkv, D):
+    for name in ("cap", "docs_prefix_window"):
+        check_prefill(ops, "bf16", [70, 5, 129], Hq, Hkv, D, name, rows=200)
+
+
+@pytest.mark.parametrize("schedule", [0, 1])
+@pytest.mark.parametrize("name", ["window", "prefix_bias", "docs_prefix_window", "open_docs_prefix"])
+def test_prefill_schedules(ops, tune, schedule, name):
+    tune(prefill_schedule=schedule)
+    for lens in ([300, 1], [130, 130], [65], [5, 0, 700, 64, 31]):
+        check_prefill(ops, "bf16", lens, 8, 2, 128, name, rows=300)
+
+
+def test_prefill_many_prompts_and_long_ones(ops):
+    rng = np.random.default_rng(5)
+    check_prefill(ops, "bf16", [int(x) for x in rng.integers(0, 9, 1500)], 4, 2, 64, "cap_bias", rows=300)
+    check_prefill(ops, "f32", [int(x) for x in rng.integers(0, 40, 300)], 4, 2, 64, "docs_prefix_window", rows=300)
+    check_prefill(ops, "bf16", [5000, 2300], 8, 2, 128, "window", rows=60)
+    check_prefill(ops, "bf16", [4099], 8, 8, 128, "docs_prefix_window", rows=60)
+    check_prefill(ops, "f32", [2100], 4, 1, 128, "prefix_bias", rows=60)
+
+
+@pytest.mark.parametrize("cap", [1e-3, 0.5, 30.0, 50.0, 1e6])
+def test_prefill_caps(ops, cap):
+    """Scores far past the cap, within half of it (the polynomial) and at its end."""
+    for std in (0.3, 1.5, 4.0, 30.0):
+        check_prefill(ops, "bf16", [200, 77], 4, 2, 64, (dict(softcap=cap), True), std=std, rows=200)
+
+
+def test_prefill_without_modifiers_is_the_plain_operator(ops):
+    import torch
+    lens, Hq, Hkv, D = [333, 64, 1], 8, 2, 128
+    qkv, _ = heads(62, sum(lens), Hq, Hkv, D, "bf16")
+    qkv = cuda(qkv)
+    q, k, v = (qkv[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in ((0, 8), (8, 10), (10, 12)))
+    cu = i32(wl.cu_seqlens(lens))
+    for causal in (True, False):
+        a = ops.opscale_attn_prefill(q, k, v, cu, 333, 0.09, causal)
+        b = ops.opscale_attn_prefill_mod(q, k, v, cu, 333, 0.09, causal)
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_prefill_masked_infinities_and_nan(ops, dtype, D):
+    """K and V rows that hold infinities and NaN reach the queries that see them and
+    no other."""
+    import torch
+    lens, Hq, Hkv = [300, 90], 4, 2
+    T, cu = sum(lens), wl.cu_seqlens(lens)
+    qkv, _ = heads(63, T, Hq, Hkv, D, dtype)
+    starts = np.concatenate([np.r_[np.zeros(100), np.full(190, 100), np.full(10, 300)], np.r_[np.zeros(80), np.full(10, 90)]])
+    bad = qkv.clone()
+    kcol, vcol = slice(Hq * D, (Hq + Hkv) * D), slice((Hq + Hkv) * D, None)
+    rng = np.random.default_rng(0)
+    for t in (*range(290, 300), *range(380, 390)):  # the padding: seen by none
+        bad[t, kcol] = float(rng.choice([np.inf, -np.inf, np.nan]))
+        bad[t, vcol] = float(rng.choice([np.inf, -np.inf, np.nan]))
+    bad[120, (Hq + Hkv) * D + 3] = float("inf")   # seen from 120 on in the document at 100 (KV head 0)
+    bad[130, (Hq + Hkv) * D + 3] = float("-inf")
+    bad[200, (Hq + Hkv) * D + 7] = float("nan")
+    dev = cuda(bad)
+    q, k, v = (dev[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in ((0, 4), (4, 6), (6, 8)))
+    for extra in (dict(), dict(softcap=9.0), dict(slopes=slopes_of(Hq)), dict(softcap=9.0, slopes=slopes_of(Hq))):
+        say(f"masked infinities {dtype} D={D} {list(extra)}")
+        kw = dict(extra, doc_starts=starts)
+        got = ops.opscale_attn_prefill_mod(q, k, v, i32(cu), 300, 0.1, True, **on_gpu(kw))
+        torch.cuda.synchronize()
+        got = f64(got.cpu())
+        assert (got[290:300] == 0).all() and (got[380:] == 0).all()
+        head0 = got[:, :2]
+        assert (head0[120:130, :, 3] == np.inf).all() and not np.isfinite(head0[130:290, :, 3]).any()
+        assert np.isnan(head0[200:290, :, 7]).all()
+        hit = np.zeros(got.shape, bool)
+        hit[120:290, :2, 3] = hit[200:290, :2, 7] = True
+        qh, kh, vh = (f64(t) for t in (qkv[:, :4 * D].unflatten(1, (-1, D)), qkv[:, kcol].unflatten(1, (-1, D)),
+                                       qkv[:, vcol].unflatten(1, (-1, D))))
+        ref, weighted = (step.attn_prefill_mod(qh, kh, x, cu, 0.1, True, **kw) for x in (vh, np.abs(vh)))
+        dot = 0.1 * np.abs(qh).sum(-1).max() * np.abs(kh).max()
+        tol = tolerance(ref, weighted, dtype, D, 300, dot, extra.get("softcap"), counted(extra, 300))
+        near(np.where(hit, ref, got), ref, tol, "the others")
+
+
+def test_prefill_offsets_past_32_bits(ops):
+    """Token rows 2^17 elements apart: 5 GB from the first to the last."""
+    import torch
+    T, Hq, Hkv, D, stride = 20000, 4, 2, 64, 1 << 17
+    say("attn_prefill_mod: rows 2^17 elements apart")
+    buf = torch.zeros((T - 1) * stride + (Hq + 2 * Hkv) * D, dtype=torch.bfloat16, device="cuda")
+    rows = buf.as_strided((T, (Hq + 2 * Hkv) * D), (stride, 1))
+    g = torch.Generator(device="cuda").manual_seed(3)
+    rows.copy_(torch.empty(rows.shape, dtype=torch.float32, device="cuda").normal_(0, 1.5, generator=g))
+    lens = [100] * 200
+    cu = wl.cu_seqlens(lens)
+    q, k, v = (rows[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in ((0, 4), (4, 6), (6, 8)))
+    out = ops.opscale_attn_prefill_mod(q, k, v, i32(cu), 100, 0.125, True, softcap=6.0, window=70)
+    dense = [t.contiguous() for t in (q, k, v)]
+    near_out = ops.opscale_attn_prefill_mod(*dense, i32(cu), 100, 0.125, True, softcap=6.0, window=70)
+    torch.cuda.synchronize()
+    assert torch.equal(out, near_out)
+    pick = [(T - 1, 3), (T - 50, 0), (0, 1), (T // 2, 2)]
+    ref = step.attn_prefill_mod(*(f64(t.cpu()) for t in dense), cu, 0.125, True, softcap=6.0, window=70, rows=pick)
+    got = f64(out.cpu())
+    for (t, h), r in zip(pick, ref):
+        assert np.abs(got[t, h] - r).max() <= 2.0 ** -6 * np.abs(r).max()
+
+
+def test_prefill_streams_and_graph(ops):
+    import torch
+    lens, Hq, Hkv, D = [200, 33, 64], 8, 2, 128
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    check_prefill(ops, "bf16", lens, Hq, Hkv, D, "docs_prefix_window", stream=s, rows=100)
+    kw, causal = rules("docs_prefix_window", lens, Hq)
+    d = on_gpu(kw)
+    x = cuda(heads(64, sum(lens), Hq, Hkv, D, "bf16")[0])
+    q, k, v = (x[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in ((0, 8), (8, 10), (10, 12)))
+    cu, out = i32(wl.cu_seqlens(lens)), torch.empty(sum(lens), Hq, D, dtype=x.dtype, device="cuda")
+    call = lambda o: ops.opscale_attn_prefill_mod(q, k, v, cu, 200, 0.09, causal, out=o, **d)
+    call(out)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(out)
+    for i in range(3):
+        x.copy_(heads(65 + i, sum(lens), Hq, Hkv, D, "bf16")[0])
+        d["prefix_lens"].fill_(10 * i)
+        out.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, call(torch.empty_like(out))), i
+
+
+def test_prefill_refuses_tensors(ops):
+    import torch
+    q = torch.zeros(8, 4, 64, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros(8, 2, 64, dtype=torch.bfloat16, device="cuda")
+    good = dict(q=q, k=k, v=k.clone(), cu_seqlens=i32([0, 8]), max_seqlen=8, scale=0.1)
+    ops.opscale_attn_prefill_mod(**good)
+    for bad in (dict(q=q.half()), dict(k=k.float()), dict(v=k.cpu()), dict(cu_seqlens=i32([0, 8]).long()),
+                dict(softcap=-1.0), dict(softcap=float("inf")), dict(softcap=float("nan")), dict(window=-1),
+                dict(window=1 << 31), dict(slopes=f32([1, 2, 3])), dict(slopes=f32([1, 2, 3, 4]).double()),
+                dict(prefix_lens=i32([1, 2])), dict(prefix_lens=i32([1]).long()), dict(doc_starts=i32([0] * 7)),
+                dict(doc_starts=torch.zeros(8, dtype=torch.int32)), dict(out=q), dict(out=torch.zeros_like(q).float()),
+                dict(v=k[:4]), dict(scale=0.0)):
+        with pytest.raises(ops.OpscaleError):
+            ops.opscale_attn_prefill_mod(**dict(good, **bad))

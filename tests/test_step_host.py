@@ -118,3 +118,33 @@ def test_block_tables_refusals(lib):
                 dict(kv=6 * G + 400), dict(slots=3 * G + 100)):
         assert _bt(lib, **bad) == 1, bad
         assert "block_tables" in _err(lib)
+
+
+# ----------------------------------------------- attention with modifiers ---
+PF = dict(q=G, k=2 * G, v=3 * G, qs=32 * 128, kvs=8 * 128, o=4 * G, cu=5 * G, B=2, T=100, ms=64, Hq=32, Hkv=8, D=128,
+          scale=0.08, causal=1, mods=None, dt=1)
+
+
+def _mods(softcap=0.0, window=0, slopes=None, prefix=None, starts=None):
+    import paper_2608_13499_amd as ops
+    return ctypes.byref(ops.AttnMods(softcap, window, slopes, prefix, starts))
+
+
+BAD_MODS = (dict(softcap=-1.0), dict(softcap=NAN), dict(softcap=INF), dict(window=-1), dict(slopes=6 * G + 2),
+            dict(prefix=6 * G + 1), dict(starts=6 * G + 3))
+
+
+def test_attn_prefill_mod_refusals(lib):
+    def call(**kw):
+        a = dict(PF, **kw)
+        return lib.opscale_attn_prefill_mod(*(a[n] for n in PF), None, None)
+
+    for bad in (dict(Hkv=5), dict(qs=100), dict(ms=0), dict(cu=None), dict(scale=NAN), dict(scale=0.0), dict(q=G + 8),
+                dict(dt=3), dict(B=-1), dict(T=-1), dict(o=G), dict(o=2 * G + 16), dict(o=3 * G), dict(o=5 * G),
+                dict(mods=_mods(slopes=4 * G)), dict(mods=_mods(prefix=4 * G + 64)), dict(mods=_mods(starts=4 * G))):
+        assert call(**bad) == 1, bad
+    for bad in BAD_MODS:
+        assert call(mods=_mods(**bad)) == 1, bad
+        assert "attn_prefill_mod" in _err(lib)
+    assert call(D=96) == 2
+    assert call(T=0) == 0 and call(B=0) == 0
