@@ -420,6 +420,22 @@ opscale_status opscale_attn_prefill_mod(const void* q, const void* k, const void
                                         float scale, int32_t causal, const opscale_attn_mods* mods, opscale_dtype dt,
                                         hipStream_t stream, opscale_timing* timing);
 
+/* Bytes of device workspace that opscale_attn_decode_mod needs for these sizes. */
+size_t opscale_attn_decode_mod_workspace_size(int32_t B, int32_t Hq, int32_t D, int32_t max_context_len);
+
+/*
+ * opscale_attn_decode with score modifiers and masks (its arguments, layouts and
+ * conditions; mods NULL: none; o and the workspace overlap nothing else), the query
+ * of sequence b at position context_lens[b] - 1.  Only 32-key tiles that hold a
+ * visible key are read.  Any Hq / Hkv on both paths.
+ */
+opscale_status opscale_attn_decode_mod(const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache,
+                                       const int32_t* block_table, const int32_t* context_lens, void* o, int32_t B,
+                                       int32_t Hq, int32_t Hkv, int32_t D, int32_t block_size,
+                                       int32_t max_blocks_per_seq, int64_t num_blocks, int32_t max_context_len,
+                                       float scale, const opscale_attn_mods* mods, opscale_dtype dt, void* workspace,
+                                       size_t workspace_bytes, hipStream_t stream, opscale_timing* timing);
+
 /* ---------------------------------------------------------------------------
  * Operator profiling (Section 4.2 "Operator Profiling": per-operator compute
  * time T_v and memory M_v; Appendix C "Dataflow Characteristics": the payload

@@ -11,7 +11,8 @@ from ._lib import (  # noqa: F401
     opscale_version, opscale_rmsnorm, opscale_linear, opscale_linear_workspace_size, opscale_swiglu,
     opscale_attn_prefill, opscale_set_tuning, opscale_get_tuning,
     opscale_rope, opscale_reshape_and_cache, opscale_add_rmsnorm,
-    opscale_rope_frequencies, opscale_qk_norm_rope, opscale_block_tables, opscale_attn_prefill_mod, AttnMods,
+    opscale_rope_frequencies, opscale_qk_norm_rope, opscale_block_tables, opscale_attn_prefill_mod,
+    opscale_attn_decode_mod_workspace_size, opscale_attn_decode_mod, AttnMods,
     opscale_attn_decode_workspace_size, opscale_attn_decode, opscale_op_profile,
     opscale_attn_decode_noalloc, opscale_attn_decode_noalloc_max_bytes,
     desc_rmsnorm, desc_linear, desc_swiglu, desc_attn_prefill, desc_attn_decode,

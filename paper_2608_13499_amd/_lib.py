@@ -160,6 +160,10 @@ EXPORTS = {
     "opscale_attn_prefill_mod": (c_i32, [c_vp, c_vp, c_vp, c_i64, c_i64, c_vp, c_vp, c_i32, c_i64, c_i32, c_i32, c_i32,
                                          c_i32, c_f32, c_i32, ctypes.POINTER(AttnMods), c_i32, c_vp,
                                          ctypes.POINTER(Timing)]),
+    "opscale_attn_decode_mod_workspace_size": (c_sz, [c_i32, c_i32, c_i32, c_i32]),
+    "opscale_attn_decode_mod": (c_i32, [c_vp, c_i64, c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32,
+                                        c_i32, c_i64, c_i32, c_f32, ctypes.POINTER(AttnMods), c_i32, c_vp, c_sz, c_vp,
+                                        ctypes.POINTER(Timing)]),
     "opscale_rope_frequencies": (c_i32, [ctypes.POINTER(c_f64), ctypes.POINTER(c_f32), c_i32, c_f64, c_i32, c_f64,
                                          c_f64, c_f64, c_i64]),
     "opscale_qk_norm_rope": (c_i32, [c_vp, c_vp, c_i64, c_i64, c_vp, c_vp, c_i64, c_i64, c_vp, c_vp, c_f32, c_vp,
@@ -682,6 +686,48 @@ def opscale_attn_prefill_mod(q, k, v, cu_seqlens, max_seqlen: int, scale: float,
     _check(lib.opscale_attn_prefill_mod(_ptr(q), _ptr(k), _ptr(v), qs, ks, _ptr(out), _ptr(cu_seqlens), B, T,
                                         max_seqlen, Hq, Hkv, D, scale, int(causal), ctypes.byref(mods), dt,
                                         _stream(stream), ctypes.byref(t) if t else None))
+    return (out, t) if timed else out
+
+
+def opscale_attn_decode_mod_workspace_size(B: int, Hq: int, D: int, max_context_len: int) -> int:
+    return int(load().opscale_attn_decode_mod_workspace_size(B, Hq, D, max_context_len))
+
+
+def opscale_attn_decode_mod(q, k_cache, v_cache, block_table, context_lens, max_context_len: int, scale: float,
+                            softcap: float = 0.0, slopes=None, window: int = 0, prefix_lens=None, doc_starts=None,
+                            workspace=None, out=None, stream=None, timed: bool = False):
+    """opscale_attn_decode with score modifiers and masks (see
+    opscale_attn_prefill_mod; the query of sequence b is at context_lens[b] - 1,
+    doc_starts int32 [B] its document's first key); any number of query heads a KV
+    head.  `workspace` (a uint8 GPU tensor) is allocated by torch when not given."""
+    lib = load()
+    dt, dtype = _dt(q), q.dtype
+    if q.dim() != 3 or k_cache.dim() != 4 or block_table.dim() != 2:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG,
+                           "q must be [B, Hq, D], the caches [num_blocks, block_size, Hkv, D], block_table [B, max_blocks]")
+    B, Hq, D = q.shape
+    nb, bs, Hkv, _ = k_cache.shape
+    if out is None:
+        out = q.new_empty((B, Hq, D))
+    _here(("q", q), ("k_cache", k_cache), ("v_cache", v_cache), ("out", out), ("workspace", workspace))
+    qs = _rows("q", q, B, Hq, D, dtype)
+    for n, t_ in (("k_cache", k_cache), ("v_cache", v_cache)):
+        if tuple(t_.shape) != (nb, bs, Hkv, D) or t_.dtype != dtype or not t_.is_contiguous():
+            raise OpscaleError(OPSCALE_ERR_INVALID_ARG,
+                               f"{n} must be contiguous {dtype} [num_blocks, block_size, {Hkv}, {D}]")
+    _weight("out", out, B * Hq * D, dtype)
+    cols = block_table.shape[1]
+    _ints(("block_table", block_table), size=B * cols)
+    _ints(("context_lens", context_lens), size=B)
+    mods = _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, B)
+    if workspace is None:
+        workspace = _scratch(lib.opscale_attn_decode_mod_workspace_size(B, Hq, D, max_context_len), q, stream)
+    t = Timing() if timed else None
+    _check(lib.opscale_attn_decode_mod(_ptr(q), qs, _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
+                                       _ptr(context_lens), _ptr(out), B, Hq, Hkv, D, bs, cols, nb, max_context_len,
+                                       scale, ctypes.byref(mods), dt, _ptr(workspace),
+                                       workspace.numel() * workspace.element_size(), _stream(stream),
+                                       ctypes.byref(t) if t else None))
     return (out, t) if timed else out
 
 

@@ -178,6 +178,23 @@ Work work_decode(const std::vector<int32_t>& ctx, int64_t Hq, int64_t Hkv, int64
   return {4.0 * D * Hq * N, by, 0, (int64_t)by, s * B * Hq * D};
 }
 
+Work work_decode_mod(const std::vector<int32_t>& ctx, const std::vector<int32_t>& prefix,
+                     const std::vector<int32_t>& starts, int64_t window, int64_t Hq, int64_t Hkv, int64_t D, int s,
+                     int64_t bs, int64_t max_blocks) {
+  double keys = 0, pages = 0;
+  const int64_t B = (int64_t)ctx.size();
+  for (int64_t b = 0; b < B; ++b) {
+    const int64_t n = std::min<int64_t>(std::max<int32_t>(ctx[(size_t)b], 0), max_blocks * bs);
+    if (n == 0) continue;
+    const int64_t seen = keys_seen(n - 1, n, true, window, prefix.empty() ? 0 : prefix[(size_t)b],
+                                   starts.empty() ? 0 : starts[(size_t)b]);
+    keys += (double)seen;
+    pages += (double)((seen + bs - 1) / bs);
+  }
+  const double by = s * (2.0 * Hkv * D * keys + 2.0 * B * Hq * D) + 4.0 * (pages + B);
+  return {4.0 * D * Hq * keys, by, 0, (int64_t)by, s * B * Hq * D};
+}
+
 // weight: parameters read; transient: activations / cache touched; io: the
 // payload handed to the next operator.
 Work work_rope(int64_t T, int64_t Hq, int64_t Hkv, int64_t D, int s) {
@@ -356,14 +373,14 @@ opscale_status check_prefill_mod(const void* q, const void* k, const void* v, in
 opscale_status check_decode(const void* q, int64_t qs, const void* kc, const void* vc, const int32_t* table,
                             const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
                             int32_t bs, int32_t max_blocks, int64_t num_blocks, int32_t max_ctx,
-                            float scale, opscale_dtype dt, void* ws, size_t ws_bytes) {
+                            float scale, opscale_dtype dt, void* ws, size_t ws_bytes, bool any_group = false) {
   if (!dtype_ok(dt)) return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode: unknown dtype %d", (int)dt);
   if (B < 0 || Hq <= 0 || Hkv <= 0 || B > 65535 || Hq > 65535)
     return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode: bad sizes B=%d Hq=%d Hkv=%d", B, Hq, Hkv);
   if (Hq % Hkv) return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode: Hkv=%d does not divide Hq=%d", Hkv, Hq);
   if (D != 64 && D != 128) return fail(OPSCALE_ERR_UNSUPPORTED, "attn_decode: head_dim %d (supported: 64, 128)", D);
   const int G = Hq / Hkv;
-  if (dt == OPSCALE_BF16 && G != 1 && G != 2 && G != 4 && G != 8)
+  if (dt == OPSCALE_BF16 && !any_group && G != 1 && G != 2 && G != 4 && G != 8)
     return fail(OPSCALE_ERR_UNSUPPORTED, "attn_decode: bf16 supports Hq/Hkv in {1, 2, 4, 8}, got %d", G);
   if (bs < 1 || bs > 1024 || (bs & (bs - 1)))
     return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode: block_size %d must be a power of two in [1, 1024]", bs);
@@ -384,6 +401,35 @@ opscale_status check_decode(const void* q, int64_t qs, const void* kc, const voi
   if (dt == OPSCALE_BF16 && (!ws || ws_bytes < need || !aligned16(ws)))
     return fail(OPSCALE_ERR_WORKSPACE, "attn_decode: workspace of %zu bytes (16-byte aligned) needed, got %zu",
                 need, ws ? ws_bytes : (size_t)0);
+  return OPSCALE_OK;
+}
+
+opscale_status check_decode_mod(const void* q, int64_t qs, const void* kc, const void* vc, const int32_t* table,
+                                const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t bs,
+                                int32_t max_blocks, int64_t num_blocks, int32_t max_ctx, float scale,
+                                const opscale_attn_mods* m, opscale_dtype dt, void* ws, size_t ws_bytes) {
+  opscale_status st = check_decode(q, qs, kc, vc, table, ctx, o, B, Hq, Hkv, D, bs, max_blocks, num_blocks, max_ctx,
+                                   scale, dt, ws, ws_bytes, true);
+  if (st == OPSCALE_OK) st = check_mods("attn_decode_mod", m);
+  if (st != OPSCALE_OK || B == 0) return st;
+  const int s = esize(dt);
+  if (num_blocks > ((int64_t)1 << 31) || num_blocks * bs > ((int64_t)1 << 40))
+    return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: num_blocks=%lld (page ids are int32)", (long long)num_blocks);
+  struct Range {
+    const void* p;
+    int64_t n;
+  };
+  const int64_t cache = num_blocks * bs * Hkv * D * s;
+  const Range in[] = {{q, ((B - 1) * qs + (int64_t)Hq * D) * s}, {kc, cache}, {vc, cache}, {table, 4ll * B * max_blocks},
+                      {ctx, 4ll * B}, {m ? m->slopes : nullptr, 4ll * Hq}, {m ? m->prefix_lens : nullptr, 4ll * B},
+                      {m ? m->doc_starts : nullptr, 4ll * B}};
+  const Range out{o, (int64_t)B * Hq * D * s};
+  const Range work{dt == OPSCALE_BF16 ? ws : nullptr, (int64_t)opscale::decode_workspace_bytes(B, Hq, D, max_ctx)};
+  for (const Range& r : in)
+    if (r.p && (overlap(r.p, r.n, out.p, out.n) || (work.p && overlap(r.p, r.n, work.p, work.n))))
+      return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: o and the workspace must not overlap an input");
+  if (work.p && overlap(out.p, out.n, work.p, work.n))
+    return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: o overlaps the workspace");
   return OPSCALE_OK;
 }
 
@@ -941,6 +987,40 @@ opscale_status opscale_attn_prefill_mod(const void* q, const void* k, const void
     if (mods && mods->doc_starts && (st = copy_ints(starts, mods->doc_starts, total_tokens, stream)) != OPSCALE_OK)
       return st;
     const Work wk = work_prefill_mod(cu, prefix, starts, mods ? mods->window : 0, Hq, Hkv, D, esize(dt), causal != 0);
+    timing->alg_flops = wk.flops;
+    timing->alg_bytes = wk.bytes;
+  }
+  return st;
+}
+
+size_t opscale_attn_decode_mod_workspace_size(int32_t B, int32_t Hq, int32_t D, int32_t max_context_len) {
+  return opscale_attn_decode_workspace_size(B, Hq, D, max_context_len);
+}
+
+opscale_status opscale_attn_decode_mod(const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache,
+                                       const int32_t* block_table, const int32_t* context_lens, void* o, int32_t B,
+                                       int32_t Hq, int32_t Hkv, int32_t D, int32_t block_size,
+                                       int32_t max_blocks_per_seq, int64_t num_blocks, int32_t max_context_len,
+                                       float scale, const opscale_attn_mods* mods, opscale_dtype dt, void* workspace,
+                                       size_t workspace_bytes, hipStream_t stream, opscale_timing* timing) {
+  opscale_status st = check_decode_mod(q, q_row_stride, k_cache, v_cache, block_table, context_lens, o, B, Hq, Hkv, D,
+                                       block_size, max_blocks_per_seq, num_blocks, max_context_len, scale, mods, dt,
+                                       workspace, workspace_bytes);
+  if (st != OPSCALE_OK) return st;
+  zero_timing(timing);
+  if (B == 0) return OPSCALE_OK;
+  st = run_timed(stream, timing, "attn_decode_mod launch", [&] {
+    return opscale::launch_attn_decode_mod(q, q_row_stride, k_cache, v_cache, block_table, context_lens, o, B, Hq, Hkv,
+                                           D, block_size, max_blocks_per_seq, num_blocks, max_context_len, scale, mods,
+                                           dt == OPSCALE_BF16, workspace, stream);
+  });
+  if (st == OPSCALE_OK && timing) {
+    std::vector<int32_t> ctx, prefix, starts;
+    if ((st = copy_ints(ctx, context_lens, B, stream)) != OPSCALE_OK) return st;
+    if (mods && mods->prefix_lens && (st = copy_ints(prefix, mods->prefix_lens, B, stream)) != OPSCALE_OK) return st;
+    if (mods && mods->doc_starts && (st = copy_ints(starts, mods->doc_starts, B, stream)) != OPSCALE_OK) return st;
+    const Work wk = work_decode_mod(ctx, prefix, starts, mods ? mods->window : 0, Hq, Hkv, D, esize(dt), block_size,
+                                    max_blocks_per_seq);
     timing->alg_flops = wk.flops;
     timing->alg_bytes = wk.bytes;
   }

@@ -8,7 +8,7 @@
 
 namespace opscale {
 
-// What a kernel is compiled for: 0 for plain attention, else kMod (masks, taken
+// What a prefill kernel is compiled for: 0 for plain attention, else kMod (masks, taken
 // from the arguments) with the modifiers that cost work per score.
 constexpr int kMod = 1, kCap = 2, kBias = 4;
 

@@ -115,6 +115,12 @@ hipError_t launch_attn_decode(const void* q, int64_t q_stride, const void* kc, c
                               int32_t max_context_len, float scale, bool bf16, void* ws,
                               hipStream_t s);
 
+// The same with score modifiers and masks (m may be null), any Hq / Hkv.
+hipError_t launch_attn_decode_mod(const void* q, int64_t q_stride, const void* kc, const void* vc, const int32_t* table,
+                                  const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
+                                  int32_t block_size, int32_t max_blocks, int64_t num_blocks, int32_t max_context_len,
+                                  float scale, const opscale_attn_mods* m, bool bf16, void* ws, hipStream_t s);
+
 // Rotary embedding of the q and k heads in place (rows of q_stride /
 // k_stride elements, token t at position pos[t]).
 hipError_t launch_rope(void* q, void* k, int64_t q_stride, int64_t k_stride, const int32_t* pos, int64_t T,

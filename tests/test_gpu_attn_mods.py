@@ -312,3 +312,220 @@ def test_prefill_refuses_tensors(ops):
                 dict(v=k[:4]), dict(scale=0.0)):
         with pytest.raises(ops.OpscaleError):
             ops.opscale_attn_prefill_mod(**dict(good, **bad))
+
+
+# ----------------------------------------------------------------- decode ---
+def paged(seed, ctx, Hkv, D, bs, dtype, holes=False, std=1.5):
+    ctx = np.asarray(ctx, np.int64)
+    table, nb = wl.paged_cache_layout(np.maximum(ctx, 1), bs, wl.rng_for(seed, "block_table"), extra_blocks=3)
+    kc, vc = gen(seed, "k_cache", (nb, bs, Hkv, D), dtype, std), gen(seed, "v_cache", (nb, bs, Hkv, D), dtype)
+    if holes:
+        flat = table.reshape(-1)
+        flat[::7], flat[3::11] = -1, nb
+    return table.astype(np.int32), kc, vc
+
+
+def check_decode(ops, dtype, ctx, Hq, Hkv, D, bs, kw, seed=71, holes=False, stream=None, max_ctx=None, std=1.5):
+    import torch
+    say(f"attn_decode_mod {dtype} B={len(ctx)} max={max(ctx)} Hq={Hq} Hkv={Hkv} D={D} bs={bs} {sorted(kw)} holes={holes}")
+    table, kc, vc = paged(seed, ctx, Hkv, D, bs, dtype, holes, std)
+    B = len(ctx)
+    x = gen(seed, "q", (B, (Hq + 4) * D), dtype, std)  # a stride of its own
+    dev = cuda(x)
+    q = dev[:, :Hq * D].unflatten(1, (-1, D))
+    n = max(1, max(ctx))
+    scale = 1.0 / math.sqrt(D)
+    out = torch.full((B, Hq, D), float("nan"), dtype=dev.dtype, device="cuda")
+    ops.opscale_attn_decode_mod(q, cuda(kc), cuda(vc), i32(table), i32(ctx), max_ctx or n, scale, out=out, stream=stream,
+                                **on_gpu(kw))
+    torch.cuda.synchronize()
+    qh, kh, vh = f64(x)[:, :Hq * D].reshape(B, Hq, D), f64(kc), f64(vc)
+    ref, weighted = (step.attn_decode_mod(qh, kh, v, table, ctx, scale, **kw) for v in (vh, np.abs(vh)))
+    dot = scale * np.abs(qh).sum(-1).max() * np.abs(kh).max()
+    near(f64(out.cpu()), ref, tolerance(ref, weighted, dtype, D, n, dot, kw.get("softcap"), counted(kw, n)), "decode")
+    return out
+
+
+def decode_rules(name, ctx, Hq):
+    rng = np.random.default_rng(len(ctx))
+    n = int(max(ctx))
+    starts = np.array([rng.integers(-2, max(1, c) + 2) for c in ctx])
+    prefix = np.array([rng.integers(-1, c + 3) for c in ctx])
+    return {
+        "none": dict(), "cap": dict(softcap=5.0), "bias": dict(slopes=slopes_of(Hq)), "window1": dict(window=1),
+        "window": dict(window=max(1, n // 4), softcap=5.0), "window_all": dict(window=2 ** 31 - 1),
+        "prefix_window": dict(prefix_lens=prefix, window=max(1, n // 5)),
+        "docs": dict(doc_starts=starts, slopes=slopes_of(Hq)),
+        "all": dict(doc_starts=starts, prefix_lens=prefix, window=max(1, n // 3), softcap=5.0, slopes=slopes_of(Hq)),
+        "nothing": dict(doc_starts=np.full(len(ctx), n + 5)),
+    }[name]
+
+
+DECODE_RULES = ["none", "cap", "bias", "window1", "window", "window_all", "prefix_window", "docs", "all", "nothing"]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", DECODE_RULES)
+def test_decode_rules(ops, dtype, name):
+    for ctx, Hq, Hkv, D, bs in (([700, 1, 0, 33, 64, 129], 16, 8, 128, 16), ([515, 31, 97], 6, 2, 64, 4)):
+        check_decode(ops, dtype, ctx, Hq, Hkv, D, bs, decode_rules(name, ctx, Hq))
+        check_decode(ops, dtype, ctx, Hq, Hkv, D, bs, decode_rules(name, ctx, Hq), holes=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [1, 2, 31, 32, 33, 63, 64, 65, 511, 512, 513, 1025])
+def test_decode_lengths(ops, dtype, n):
+    for name in ("cap", "all"):
+        check_decode(ops, dtype, [n], 8, 1, 128, 16, decode_rules(name, [n], 8))
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (3, 1), (7, 1), (15, 1), (16, 1), (17, 1), (32, 2), (71, 1), (28, 4), (40, 8),
+                                    (9, 3), (12, 12), (24, 12), (10, 5), (48, 16), (64, 2)])
+@pytest.mark.parametrize("D", [64, 128])
+def test_decode_head_layouts(ops, Hq, Hkv, D):
+    ctx = [300, 5, 77]
+    check_decode(ops, "bf16", ctx, Hq, Hkv, D, 16, decode_rules("all", ctx, Hq))
+    check_decode(ops, "bf16", ctx, Hq, Hkv, D, 16, decode_rules("cap", ctx, Hq))
+
+
+@pytest.mark.parametrize("bs", [1, 2, 64, 256, 1024])
+def test_decode_block_sizes(ops, bs):
+    ctx = [1100, 600, 3]
+    check_decode(ops, "bf16", ctx, 8, 2, 128, bs, decode_rules("all", ctx, 8))
+    check_decode(ops, "f32", ctx, 8, 2, 64, bs, decode_rules("prefix_window", ctx, 8))
+
+
+@pytest.mark.parametrize("B", [1, 64, 511, 512, 513, 1300])
+def test_decode_batches(ops, B):
+    rng = np.random.default_rng(B)
+    ctx = [int(x) for x in rng.integers(0, 200, B)]
+    ctx[0] = 900
+    check_decode(ops, "bf16", ctx, 4, 2, 64, 16, decode_rules("all", ctx, 4))
+    check_decode(ops, "bf16", ctx, 4, 2, 64, 16, decode_rules("prefix_window", ctx, 4), max_ctx=16)
+
+
+def test_decode_long(ops):
+    ctx = [20000, 9000]
+    check_decode(ops, "bf16", ctx, 8, 4, 128, 16, dict(window=4096, prefix_lens=np.array([100, 0]), softcap=30.0))
+    check_decode(ops, "bf16", ctx, 8, 1, 64, 64, dict(slopes=slopes_of(8)))
+    check_decode(ops, "f32", [5000], 4, 1, 128, 16, dict(softcap=30.0))
+
+
+@pytest.mark.parametrize("cap", [1e-3, 0.5, 50.0, 1e6])
+def test_decode_caps(ops, cap):
+    for std in (0.3, 4.0, 20.0):
+        check_decode(ops, "bf16", [300, 40], 8, 2, 128, 16, dict(softcap=cap), std=std)
+
+
+@pytest.mark.parametrize("Hq,Hkv", [(8, 8), (12, 3), (6, 6), (24, 12), (20, 5)])
+def test_decode_without_modifiers_is_the_plain_operator(ops, Hq, Hkv):
+    """Also for numbers of KV heads that are no power of two."""
+    import torch
+    ctx = [700, 1, 0, 90]
+    table, kc, vc = paged(72, ctx, Hkv, 128, 16, "bf16")
+    q = cuda(gen(72, "q", (4, Hq, 128), "bf16"))
+    args = (q, cuda(kc), cuda(vc), i32(table), i32(ctx), 700, 0.09)
+    a, b = ops.opscale_attn_decode(*args), ops.opscale_attn_decode_mod(*args)
+    torch.cuda.synchronize()
+    assert torch.equal(a, b)
+    ref = step.attn_decode_mod(f64(q.cpu()), f64(kc), f64(vc), table, ctx, 0.09)
+    assert np.abs(f64(a.cpu()) - ref).max() <= 2.0 ** -6 * np.abs(ref).max()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_masked_infinities_and_nan(ops, dtype):
+    """What lies in masked rows, in rows past the length and in pages that are not
+    there reaches no output; a query's NaN reaches its own head only."""
+    import torch
+    ctx, Hq, Hkv, D, bs = [300, 90, 40], 8, 2, 128, 16
+    kw = dict(window=50, prefix_lens=np.array([20, 5, 0]), softcap=9.0)
+    table, kc, vc = paged(73, ctx, Hkv, D, bs, dtype)
+    table[2, 1] = -1
+    q0 = gen(73, "q", (3, Hq, D), dtype, 1.5)
+    seen = np.zeros((kc.shape[0], bs), bool)
+    for b, n in enumerate(ctx):
+        for j in step.visible(n - 1, n, True, 50, int(kw["prefix_lens"][b]), 0):
+            if table[b, j // bs] >= 0:
+                seen[table[b, j // bs], j % bs] = True
+    kb, vb = kc.clone(), vc.clone()
+    rng = np.random.default_rng(0)
+    for p, o in np.argwhere(~seen):
+        kb[p, o] = float(rng.choice([np.inf, -np.inf, np.nan]))
+        vb[p, o] = float(rng.choice([np.inf, -np.inf, np.nan]))
+    q = q0.clone()
+    q[1, 0] = float("nan")
+    say(f"decode: masked infinities {dtype}")
+    got = ops.opscale_attn_decode_mod(cuda(q), cuda(kb), cuda(vb), i32(table), i32(ctx), 300, 0.1, **on_gpu(kw))
+    torch.cuda.synchronize()
+    got = f64(got.cpu())
+    assert np.isnan(got[1, 0]).all()
+    ref, weighted = (step.attn_decode_mod(f64(q0), f64(kc), v, table, ctx, 0.1, **kw) for v in (f64(vc), np.abs(f64(vc))))
+    got[1, 0] = ref[1, 0]
+    dot = 0.1 * np.abs(f64(q0)).sum(-1).max() * np.abs(f64(kc)).max()
+    near(got, ref, tolerance(ref, weighted, dtype, D, 300, dot, 9.0, 0.0), "the others")
+
+
+def test_decode_cache_past_32_bits(ops):
+    """A cache of more than 2^31 elements, its last pages used."""
+    import torch
+    nb, bs, Hkv, D, Hq = (1 << 31) // (16 * 8 * 128) + 64, 16, 8, 128, 16
+    say("attn_decode_mod: a cache past 2^31 elements")
+    kc = torch.zeros(nb, bs, Hkv, D, dtype=torch.bfloat16, device="cuda")
+    vc = torch.zeros_like(kc)
+    ctx = [1000, 600]
+    table = np.stack([nb - 1 - np.arange(64), np.r_[nb // 2 + np.arange(38), np.zeros(26)]]).astype(np.int32)
+    used = np.unique(table)
+    small_k, small_v = (gen(74, t, (len(used), bs, Hkv, D), "bf16", 1.5) for t in ("k_cache", "v_cache"))
+    at = torch.from_numpy(used).long().cuda()
+    kc[at], vc[at] = cuda(small_k), cuda(small_v)
+    q = gen(74, "q", (2, Hq, D), "bf16", 1.5)
+    kw = dict(softcap=20.0, window=700)
+    got = ops.opscale_attn_decode_mod(cuda(q), kc, vc, i32(table), i32(ctx), 1000, 0.08, **on_gpu(kw))
+    ref = ops.opscale_attn_decode_mod(cuda(q), cuda(small_k), cuda(small_v), i32(np.searchsorted(used, table)), i32(ctx),
+                                      1000, 0.08, **on_gpu(kw))
+    torch.cuda.synchronize()
+    assert torch.equal(got, ref) and bool(got.abs().sum() > 0)
+
+
+def test_decode_streams_workspaces_and_graph(ops):
+    import torch
+    ctx, Hq, Hkv, D = [300, 64, 5, 0], 8, 2, 128
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    check_decode(ops, "bf16", ctx, Hq, Hkv, D, 16, decode_rules("all", ctx, Hq), stream=s)
+    table, kc, vc = paged(75, ctx, Hkv, D, 16, "bf16")
+    kc, vc, table, lens = cuda(kc), cuda(vc), i32(table), i32(ctx)
+    q, out = cuda(gen(75, "q", (4, Hq, D), "bf16")), torch.empty(4, Hq, D, dtype=torch.bfloat16, device="cuda")
+    d = on_gpu(decode_rules("all", ctx, Hq))
+    ws = torch.full((ops.opscale_attn_decode_mod_workspace_size(4, Hq, D, 300),), 255, dtype=torch.uint8, device="cuda")
+    call = lambda o, w=None: ops.opscale_attn_decode_mod(q, kc, vc, table, lens, 300, 0.09, workspace=w, out=o, **d)
+    call(out, ws)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(out, ws)
+    for i in range(4):
+        q.copy_(gen(76 + i, "q", (4, Hq, D), "bf16"))
+        lens.copy_(i32([300 - 90 * i, 64 - i, 5, i]))
+        out.fill_(float("nan"))
+        ws.fill_(255)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, call(torch.empty_like(out))), i
+
+
+def test_decode_refuses_tensors(ops):
+    import torch
+    q = torch.zeros(2, 4, 64, dtype=torch.bfloat16, device="cuda")
+    kc = torch.zeros(4, 16, 2, 64, dtype=torch.bfloat16, device="cuda")
+    good = dict(q=q, k_cache=kc, v_cache=kc.clone(), block_table=i32([[0, 1], [2, 3]]), context_lens=i32([20, 3]),
+                max_context_len=20, scale=0.1)
+    ops.opscale_attn_decode_mod(**good)
+    small = torch.zeros(16, dtype=torch.uint8, device="cuda")
+    for bad in (dict(q=q.float()), dict(q=q.cpu()), dict(k_cache=kc.float()), dict(v_cache=kc[:3]),
+                dict(block_table=i32([[0, 1]])), dict(block_table=i32([0, 1, 2, 3])), dict(context_lens=i32([1])),
+                dict(context_lens=i32([1, 2]).long()), dict(workspace=small), dict(softcap=-1.0), dict(window=-3),
+                dict(slopes=f32([1, 2])), dict(prefix_lens=i32([1])), dict(doc_starts=i32([1, 2, 3])), dict(out=q),
+                dict(out=torch.zeros(2, 4, 32, dtype=q.dtype, device="cuda")), dict(max_context_len=0), dict(scale=-1.0)):
+        with pytest.raises(ops.OpscaleError):
+            ops.opscale_attn_decode_mod(**dict(good, **bad))

@@ -148,3 +148,27 @@ def test_attn_prefill_mod_refusals(lib):
         assert "attn_prefill_mod" in _err(lib)
     assert call(D=96) == 2
     assert call(T=0) == 0 and call(B=0) == 0
+
+
+DC = dict(q=G, qs=32 * 128, kc=2 * G, vc=3 * G, tab=4 * G, ctx=5 * G, o=6 * G, B=256, Hq=32, Hkv=8, D=128, bs=16, mb=512,
+          nb=69424, mc=8192, scale=0.08, mods=None, dt=1, ws=7 * G, wsb=1 << 30)
+
+
+def test_attn_decode_mod_refusals(lib):
+    def call(**kw):
+        a = dict(DC, **kw)
+        return lib.opscale_attn_decode_mod(*(a[n] for n in DC), None, None)
+
+    need = lib.opscale_attn_decode_mod_workspace_size(256, 32, 128, 8192)
+    for bad in (dict(bs=12), dict(tab=None), dict(mb=0), dict(qs=32 * 128 - 8), dict(qs=48 * 128 + 4), dict(Hkv=5),
+                dict(B=-1), dict(mc=0), dict(dt=9), dict(scale=NAN), dict(scale=-1.0), dict(nb=1 << 40), dict(q=G + 4),
+                dict(o=G), dict(o=2 * G), dict(o=3 * G + 256), dict(o=4 * G), dict(o=5 * G), dict(ws=6 * G + 16),
+                dict(ws=G), dict(ws=2 * G), dict(mods=_mods(slopes=6 * G)), dict(mods=_mods(prefix=7 * G)),
+                dict(mods=_mods(starts=6 * G + 4))):
+        assert call(**bad) == 1, bad
+    for bad in BAD_MODS:
+        assert call(mods=_mods(**bad)) == 1, bad
+        assert "attn_decode_mod" in _err(lib)
+    assert call(wsb=need - 1) == 3 and call(ws=None) == 3 and call(ws=7 * G + 8) == 3
+    assert call(D=256) == 2
+    assert call(B=0) == 0
