@@ -155,7 +155,8 @@ __global__ __launch_bounds__(512, 4) void attn_decode_split_kernel(
     const int32_t* __restrict__ table, const int32_t* __restrict__ ctx, int Hq, int Hkv,
     int log2bs, int max_blocks, int64_t num_blocks, const int64_t* __restrict__ tcs,
     const int32_t* __restrict__ first_b, int B, int nwg,
-    float scale_log2, float* __restrict__ ws_o, float* __restrict__ ws_ml, int group_heads, const AttnMods mods) {
+    float scale_log2, float* __restrict__ ws_o, float* __restrict__ ws_ml, int group_heads,
+    const MaybeMods<MOD> mods) {
   static_assert(MOD == (GQ == 0), "any number of query heads with MOD, 1 to 8 without");
   const int GH = MOD ? group_heads : GQ;               // query heads of a KV head
   const int h0 = MOD ? 16 * (int)blockIdx.z : 0;       // this workgroup's first of them
@@ -263,7 +264,8 @@ __global__ __launch_bounds__(512, 4) void attn_decode_split_kernel(
   // (MOD: zeros, whatever the query holds.)
   const __bf16* dummy = MOD ? reinterpret_cast<const __bf16*>(zero_row) : q + (int64_t)b * q_stride;
   float slope2 = 0.f;
-  if (MOD && mods.slopes && col < G) slope2 = mods.slopes[g * GH + h0 + col] * kLog2e;
+  if constexpr (MOD)
+    if (mods.slopes && col < G) slope2 = mods.slopes[g * GH + h0 + col] * kLog2e;
   auto row_ptr = [&](const __bf16* cache, int j) -> const __bf16* {
     if (!key_ok(j)) return dummy;
     const int blk = pages[(j >> log2bs) - p_first];
@@ -316,9 +318,13 @@ __global__ __launch_bounds__(512, 4) void attn_decode_split_kernel(
       for (int rr = 0; rr < 4; ++rr) {
         const int j = t0 + sub * 16 + grp * 4 + rr;
         float x = st[sub][rr];
-        if (MOD && mods.softcap > 0.f) x = fabsf(x) <= mods.cap_bound ? mods.capped_small(x) : mods.capped(x);
-        else x *= scale_log2;
-        if constexpr (MOD) x = fmaf(-slope2, (float)(span.n - 1 - j), x);
+        if constexpr (MOD) {
+          if (mods.softcap > 0.f) x = fabsf(x) <= mods.cap_bound ? mods.capped_small(x, 0.f) : mods.capped(x, 0.f);
+          else x *= scale_log2;
+          x = fmaf(-slope2, (float)(span.n - 1 - j), x);
+        } else {
+          x *= scale_log2;
+        }
         const float sv = key_ok(j) ? x : -INFINITY;
         st[sub][rr] = sv;
         tmax = fmaxf(tmax, sv);
@@ -501,7 +507,8 @@ __global__ __launch_bounds__(512, 4) void attn_decode_split_kernel(
 template <bool MOD>
 __global__ __launch_bounds__(1024) void attn_decode_plan_kernel(const int32_t* __restrict__ ctx, int B,
                                                                 int max_keys, int nwg, int64_t* __restrict__ tcs,
-                                                                int32_t* __restrict__ first_b, const AttnMods mods) {
+                                                                int32_t* __restrict__ first_b,
+                                                                const MaybeMods<MOD> mods) {
   __shared__ int64_t part[1024];
   __shared__ int64_t carry;
   if (threadIdx.x == 0) carry = 0;
@@ -555,7 +562,7 @@ template <int D, bool INL, int W, bool MOD>
 __global__ __launch_bounds__(64 * W) void attn_decode_combine_kernel(
     const float* __restrict__ ws_o, const float2* __restrict__ ws_ml, const int64_t* __restrict__ tcs,
     const int32_t* __restrict__ ctx, int max_keys, __bf16* __restrict__ o, int Hq, int B, int nwg,
-    const AttnMods mods) {
+    const MaybeMods<MOD> mods) {
   constexpr int DPL = D / 64;
   constexpr int kOwn = 64 / W;  // segments of a block of 64 that a wave sums
   __shared__ float fw_all[W][64];
@@ -583,7 +590,8 @@ __global__ __launch_bounds__(64 * W) void attn_decode_combine_kernel(
     auto sum = [](int v) { return ((int64_t)wave_sum_i(v >> 16) << 16) + wave_sum_i(v & 0xffff); };
     ft = sum(pre);
     T = sum(all);
-    lt = ft + (MOD ? decode_span(mods, ctx, max_keys, b).tiles : tiles_of(ctx[b])) - 1;
+    if constexpr (MOD) lt = ft + decode_span(mods, ctx, max_keys, b).tiles - 1;
+    else lt = ft + tiles_of(ctx[b]) - 1;
   } else {
     T = tcs[B];
     ft = tcs[b];
@@ -704,7 +712,7 @@ inline int decode_heads_per_workgroup(int Hkv) { return Hkv % 8 == 0 ? 8 : Hkv %
 // The merge of a launch's segments.
 template <bool MOD>
 hipError_t launch_decode_combine(const DecodeWs& w, const int32_t* ctx, int max_keys, __bf16* o, int32_t B, int32_t Hq,
-                                 int32_t D, int nwg, const AttnMods& mods, hipStream_t s) {
+                                 int32_t D, int nwg, const MaybeMods<MOD>& mods, hipStream_t s) {
   const dim3 cgrid((unsigned)Hq, (unsigned)B);
   // Past 16 workgroups, so about as many segments, a sequence four waves are
   // faster (us, one wave / four, 64 heads of 128: 1 x 2048 tokens 15.8 / 13.0, 4 x 1024

@@ -4,6 +4,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <cmath>
+#include <type_traits>
+
 #include "opscale.h"
 
 namespace opscale {
@@ -21,15 +24,22 @@ struct AttnMods {
   // cap_log2 * tanh, e^2y = 2^(cap_rate x), and for |x| <= cap_bound
   // x * P(x^2) with P of degree 3
   float cap_log2, cap_rate, cap_bound, cap_poly[4];
+  // A capped score t lies within +-cap_log2 (C), so with C <= 75 a row's reference
+  // r may be fixed at its first keys' largest t, or C - 60 if that is larger: the
+  // probabilities 2^(t - r) are at most 2^60, and the row's largest at least
+  // 2^(60 - 2C) >= 2^-90, with 36 powers of two of fp32 below it.  C - 60, or
+  // -infinity for larger caps, whose rows need a running maximum.
+  float cap_floor;
 
-  __device__ __forceinline__ float capped_small(float x) const {
+  // The capped score less `less`.
+  __device__ __forceinline__ float capped_small(float x, float less) const {
     const float u = x * x;
-    return x * fmaf(u, fmaf(u, fmaf(u, cap_poly[3], cap_poly[2]), cap_poly[1]), cap_poly[0]);
+    return fmaf(x, fmaf(u, fmaf(u, fmaf(u, cap_poly[3], cap_poly[2]), cap_poly[1]), cap_poly[0]), -less);
   }
   // To a few steps of fp32 at cap_log2, any x (an infinity gives +-cap_log2).
-  __device__ __forceinline__ float capped(float x) const {
+  __device__ __forceinline__ float capped(float x, float less) const {
     const float e = __builtin_amdgcn_exp2f(x * cap_rate);
-    return fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(1.f + e), cap_log2);
+    return fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(1.f + e), cap_log2 - less);
   }
 
   // A score on the fp32 path: x = scale * q . k, d = |i - j|.
@@ -38,6 +48,11 @@ struct AttnMods {
     return fmaf(-slope, d, x);
   }
 };
+
+// The argument of a kernel compiled with and without them.
+struct NoMods {};
+template <bool MOD>
+using MaybeMods = std::conditional_t<MOD, AttnMods, NoMods>;
 
 inline AttnMods make_attn_mods(const opscale_attn_mods* m, float scale) {
   AttnMods a{};
@@ -53,6 +68,7 @@ inline AttnMods make_attn_mods(const opscale_attn_mods* m, float scale) {
     a.cap_log2 = (float)(cap * log2e);
     a.cap_rate = (float)(2.0 * log2e * y);
     a.cap_bound = (float)(0.5 / y);
+    a.cap_floor = cap * log2e <= 75.0 ? (float)(cap * log2e - 60.0) : -INFINITY;
     double f = cap * log2e * y;
     for (int i = 0; i < 4; ++i, f *= y * y) a.cap_poly[i] = (float)(p[i] * f);
   }

@@ -1,6 +1,6 @@
-// Grouped-query prefill attention over a ragged batch of prompts: the kernels, for
-// plain attention (MODE 0, k_attn_prefill.hip) and for attention with score
-// modifiers and masks (k_attn_prefill_mod.hip, attn_mods.h).
+// Grouped-query prefill attention over a ragged batch of prompts: what the plain
+// operator (k_attn_prefill.hip) and the one with score modifiers and masks
+// (k_attn_prefill_mod.hip) share.
 //
 // bf16 path (D = 64 or 128): one workgroup of 4 waves per (prompt, KV head,
 // query tile).  The waves are the query heads of one GQA group (up to 4) times
@@ -107,447 +107,32 @@ __device__ __forceinline__ void lds_dma16(uint64_t base, uint32_t nrec, OPS_LDS 
 // Prompts the work-list schedule can hold in LDS (more use the grid schedule).
 constexpr int kMaxListB = 1024;
 
-// Two schedules over the same tiles (a tile: one prompt, one KV head, one
-// head block, one query-tile level), each tile computed the same way, so the
-// output does not depend on the schedule:
-//  * grid (LIST = false): blockIdx = (prompt x KV head x head block, level),
-//    highest level first; workgroups whose prompt has no tile at their level
-//    return at once.
-//  * work list (LIST = true): workgroup i takes item i of the level-major list
-//    of the tiles that exist (highest level first, then prompt, KV head and
-//    head block), so no workgroup is launched for a missing tile.
-//
-// MODE (attn_mods.h): what changes for a tile is in its do_tile only.
-//  * Key tiles: those of the prefix, then those from the first that any query of
-//    the workgroup sees on.  A tile that every query of a wave sees whole takes no
-//    mask; the others compare each key with the lane's first and last.
-//  * kCap costs VALU work beside the exponential, and VALU work as long as the
-//    MFMAs' is what bounds this kernel already.  A lane whose visible scores of
-//    the tile lie within half the cap takes a polynomial for tanh (a square, three
-//    fused steps and a product a score; it also keeps the digits of scores
-//    far below the cap), other lanes 1 - 2 / (1 + e^2x), an exponential and a
-//    reciprocal at a quarter of the rate each; a wave without such lanes skips that.
-//  * kBias adds slope * (j - i) along the keys, three steps from a group's first.
-//  * A masked key's probability is 0, but 0 times an infinity or NaN in its V row
-//    is not: a masked tile whose V holds one takes those elements out of the
-//    product and adds them for the queries that see them
-template <int D, bool LIST, int MODE>
-__global__ __launch_bounds__(256, 2) void attn_prefill_bf16_kernel(
-    const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
-    int64_t q_stride, int64_t kv_stride, __bf16* __restrict__ o, const int32_t* __restrict__ cu,
-    int B, int Hq, int Hkv, int hpb, float scale_log2, int causal, const AttnMods mods) {
-  constexpr bool MOD = MODE != 0, CAP = (MODE & kCap) != 0, BIAS = (MODE & kBias) != 0;
-  using S = PrefillSmem<D>;
-  constexpr int CPR = D / 8;          // 16-byte chunks per row
-  constexpr int DSTEPS = D / 16;      // MFMA k-steps over the head dim
-  constexpr int DT = D / 32;          // 32-wide output tiles over the head dim
-  // Lazy rescaling: the running max only moves when a tile's max exceeds it by
-  // more than this (log2 units), so probabilities stay <= 2^kLazy and the
-  // output rescale is skipped on most tiles.  Exact: numerator and
-  // denominator use the same reference.
-  constexpr float kLazy = 8.f;
-  __shared__ __attribute__((aligned(16))) char smem_raw[S::kTotal];
-  OPS_LDS char* smem = (OPS_LDS char*)smem_raw;
-
+// The launch of a bf16 prefill kernel.
+struct PrefillGrid {
+  int hpb;  // query heads of a workgroup
+  bool list;
+  unsigned x, y;
+};
+inline PrefillGrid prefill_grid(int32_t B, int64_t total_tokens, int32_t max_seqlen, int32_t Hq, int32_t Hkv) {
+  PrefillGrid p;
   const int G = Hq / Hkv;
-  const int nhb = G / hpb;
-  const int qsub = 4 / hpb;
-  const int BQ = 32 * qsub;
-  const int bq_shift = 5 + __builtin_ctz(qsub);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int qs = wave / hpb;
-  const int fr = lane & 31, fh = lane >> 5;
-  // lane roles in the transposed V reads: 16-lane group tg, member tc
-  const int tg = lane >> 4, tc = lane & 15;
-  const int tr_key = 4 * (tg >> 1) + (tc >> 2);               // + 16 s (+ 8 for the upper half)
-  const int tr_col = 16 * (tg & 1) + 4 * (tc & 3);            // + 32 dt
-
-  // One query tile: prompt b, KV head g, head block hb, level t.
-  auto do_tile = [&](const int b, const int g, const int hb, const int t, const int seq0, const int L) {
-    const int h = g * G + hb * hpb + wave % hpb;
-    const int q_lo = t * BQ + qs * 32;          // first query of this wave
-    const int q_pos = q_lo + fr;                 // this lane's query
-    const int blk_q_hi = min(L, (t + 1) * BQ);   // one past the block's last query
-    const int kv_end = causal ? blk_q_hi : L;
-    int nkv = (kv_end + kBKV - 1) / kBKV;
-    // MODE: this lane's keys (below pre, or own_lo .. own_hi), what is common to
-    // the wave's queries, and the key tiles: pre_tiles, then those from first_tile on
-    int pre = 0, own_lo = 0, own_hi = 0, wave_lo_min = 0, wave_lo_max = 0, wave_hi_min = 0, wave_hi_max = 0;
-    int pre_tiles = 0, first_tile = 0;
-    float slope2 = 0.f;
-    if constexpr (MOD) {
-      if (mods.prefix) pre = min(max(__builtin_amdgcn_readfirstlane(mods.prefix[b]), 0), L);
-      const int win = mods.window == 0 ? L : min(mods.window, L);  // (a window of L reaches every key)
-      const int q_last = min(L, q_lo + 32) - 1;                    // the wave's last query (may be before q_lo)
-      int s_min = 0, s_max = 0, start = 0, blk_s_min = 0;
-      if (mods.starts) {
-        const int32_t* st0 = mods.starts + seq0;
-        start = max(st0[min(q_pos, L - 1)], 0);
-        s_min = -wave_max_i(-start);  // (the queries past the prompt repeat its last one)
-        s_max = wave_max_i(start);
-        int m = INT32_MAX;
-        for (int r = lane; r < BQ; r += 64) m = min(m, max(st0[min(t * BQ + r, L - 1)], 0));
-        blk_s_min = -wave_max_i(-m);
-      }
-      own_lo = max(start, q_pos - win + 1);
-      own_hi = causal ? min(q_pos, L - 1) : min(L - 1, q_pos + win - 1);
-      wave_lo_min = max(s_min, q_lo - win + 1);
-      wave_lo_max = max(s_max, q_last - win + 1);
-      wave_hi_min = causal ? q_lo : min(L - 1, q_lo + win - 1);
-      wave_hi_max = causal ? q_last : min(L - 1, q_last + win - 1);
-      const int blk_lo = max(blk_s_min, max(0, t * BQ - win + 1));
-      const int own_end = causal ? blk_q_hi : min(L, blk_q_hi - 1 + win);
-      pre_tiles = (pre + kBKV - 1) / kBKV;
-      first_tile = max(blk_lo / kBKV, pre_tiles);
-      nkv = pre_tiles + max(0, (own_end + kBKV - 1) / kBKV - first_tile);
-      if constexpr (BIAS) slope2 = mods.slopes[h] * kLog2e;
-    }
-    auto tile_at = [&](int it) { return MOD && it >= pre_tiles ? it - pre_tiles + first_tile : it; };
-
-    // This wave's 32 query rows as MFMA B operand: chunk 2*s + fh of row q_pos.
-    bf16x8 qf[DSTEPS];
-    {
-      // (the record count is wave-uniform; readfirstlane keeps the
-      // descriptor in scalar registers)
-      const int rows = max(0, min(32, L - q_lo));
-      const uint32_t nrec = __builtin_amdgcn_readfirstlane(
-          rows > 0 ? (uint32_t)(((int64_t)(rows - 1) * q_stride + D) * 2) : 0u);
-      const __amdgpu_buffer_rsrc_t qr = make_rsrc(q + (int64_t)(seq0 + q_lo) * q_stride + (int64_t)h * D, nrec);
-#pragma unroll
-      for (int s = 0; s < DSTEPS; ++s) {
-        const u32x4 w = buffer_load16(qr, (uint32_t)(((int64_t)fr * q_stride + (2 * s + fh) * 8) * 2));
-        qf[s] = __builtin_bit_cast(bf16x8, w);
-      }
-    }
-
-    f32x16 acc[DT];
-#pragma unroll
-    for (int i = 0; i < DT; ++i) acc[i] = f32x16{};
-    float m_run = -INFINITY, l_part = 0.f;  // running max (log2 units) and partial sum
-
-    // K and V tiles: LDS DMA, rows past the prompt read as zeros.
-    auto load_kv = [&](int kv0, int stage) {
-      const int rows = min(kBKV, L - kv0);
-      const uint32_t nrec = __builtin_amdgcn_readfirstlane((uint32_t)(((int64_t)(rows - 1) * kv_stride + D) * 2));
-      const int64_t off = (int64_t)(seq0 + kv0) * kv_stride + (int64_t)g * D;
-      const uint64_t kb = (uint64_t)(uintptr_t)(k + off), vb = (uint64_t)(uintptr_t)(v + off);
-      OPS_LDS char* dk = smem + stage * S::kStage;
-      OPS_LDS char* dv = dk + S::kTileBytes;
-      constexpr int ROWS_PER_LOAD = 64 / CPR;  // rows covered by one 1 KB wave load
-      constexpr int LOADS = kBKV / ROWS_PER_LOAD / 4;
-#pragma unroll
-      for (int i = 0; i < LOADS; ++i) {
-        const int grp = i * 4 + wave;
-        const int r = grp * ROWS_PER_LOAD + lane / CPR;
-        const int pc = lane % CPR;
-        lds_dma16(kb, nrec, dk + grp * 1024, (uint32_t)(((int64_t)r * kv_stride + (pc ^ k_swz<D>(r)) * 8) * 2));
-        lds_dma16(vb, nrec, dv + grp * 1024, (uint32_t)(((int64_t)r * kv_stride + (pc ^ v_swz<D>(r)) * 8) * 2));
-      }
-    };
-
-    if (nkv > 0) load_kv(tile_at(0) * kBKV, 0);
-    for (int it = 0; it < nkv; ++it) {
-      const int kv0 = tile_at(it) * kBKV;
-      wait_vmem();
-      __syncthreads();
-      if (it + 1 < nkv) load_kv(tile_at(it + 1) * kBKV, (it + 1) & 1);
-      const OPS_LDS char* ks = smem + (it & 1) * S::kStage;
-      const OPS_LDS char* vs = ks + S::kTileBytes;
-      // Skip tiles that are entirely in this wave's causal future.
-      bool active = !(causal && kv0 > q_lo + 31) && q_lo < L;
-      if constexpr (MOD)  // (or in none of its queries' prefix, window and document)
-        active = q_lo < L && (kv0 < pre || (kv0 <= wave_hi_max && kv0 + kBKV - 1 >= wave_lo_min));
-      if (!active) continue;
-      f32x16 st[2];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        st[kb] = f32x16{};
-        const int r = kb * 32 + fr;
-#pragma unroll
-        for (int s = 0; s < DSTEPS; ++s) {
-          const int c = 2 * s + fh;
-          const bf16x8 kf = *reinterpret_cast<const OPS_LDS bf16x8*>(
-              ks + r * S::kRowBytes + ((c ^ k_swz<D>(r)) << 4));
-          st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], st[kb], 0, 0, 0);
-        }
-      }
-      bf16x8 pf[4];
-      bool masked = false;
-      // this lane's element (kb, e) is key kv0 + fh*4 + off, off a constant
-      const int key0 = kv0 + fh * 4;
-      auto off_of = [](int kb, int e) { return kb * 32 + (e >> 2) * 8 + (e & 3); };
-      auto sees = [&](int off) { return off < pre - key0 || (off >= own_lo - key0 && off <= own_hi - key0); };
-      // moves the reference max to a tile's max (log2 units) where that exceeds
-      // it by more than kLazy
-      auto move_reference = [&](float tmax) {
-        if (tmax > m_run + kLazy) {
-          const float alpha = fast_exp2(m_run - tmax);  // 0 on the first tile
-          l_part *= alpha;
-#pragma unroll
-          for (int i = 0; i < DT; ++i) acc[i] *= alpha;
-          m_run = tmax;
-        }
-      };
-      // max over the lane's scores and the other half's
-      auto tile_max = [&] {
-        float m = -INFINITY;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) m = fmaxf(m, st[kb][e]);
-        return fmaxf(m, other_half(m));
-      };
-      // probabilities from f(score), in log2 units less the reference
-      auto exponentials = [&](auto&& f) {
-        float psum = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float p = fast_exp2(f(st[kb][e]));
-            psum += p;
-            pf[kb * 2 + (e >> 3)][e & 7] = (__bf16)p;
-          }
-        l_part += psum;
-      };
-      auto m_use = [&] { return m_run == -INFINITY ? 0.f : m_run; };
-      if constexpr (!MOD) {
-        // mask (only tiles that reach past the diagonal or the prompt end):
-        // key kv0 + fh*4 + off is visible iff off <= lim
-        if ((causal && kv0 + kBKV - 1 > q_lo) || kv0 + kBKV > L) {
-          const int lim = (causal ? min(q_pos, L - 1) : L - 1) - kv0 - fh * 4;
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (off_of(kb, e) > lim) st[kb][e] = -INFINITY;
-        }
-        move_reference(tile_max() * scale_log2);
-        const float m = m_use();
-        exponentials([&](float x) { return fmaf(x, scale_log2, -m); });
-      } else {
-        masked = !(kv0 + kBKV <= pre || (kv0 >= wave_lo_max && kv0 + kBKV - 1 <= wave_hi_min));
-        if constexpr (CAP) {
-          if (masked) {  // (a masked score has no say in what follows)
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                if (!sees(off_of(kb, e))) st[kb][e] = 0.f;
-          }
-          float a = 0.f;
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) a = fmaxf(a, fabsf(st[kb][e]));
-          const bool small = a <= mods.cap_bound;
-          if (__builtin_amdgcn_ballot_w64(!small) == 0) {
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int e = 0; e < 16; ++e) st[kb][e] = mods.capped_small(st[kb][e]);
-          } else {
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                st[kb][e] = small ? mods.capped_small(st[kb][e]) : mods.capped(st[kb][e]);
-          }
-        }
-        if constexpr (BIAS) {
-          if constexpr (!CAP) {
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int e = 0; e < 16; ++e) st[kb][e] *= scale_log2;
-          }
-          const float d0 = (float)(key0 - q_pos);  // exact: below 2^24 keys either way
-          if (kv0 + kBKV - 1 <= q_lo || (causal && pre <= kv0)) {
-            // no visible key is ahead of its query: |i - j| = i - j
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int gq = 0; gq < 4; ++gq) {
-                float bias = slope2 * (d0 + (float)(kb * 32 + gq * 8));
-#pragma unroll
-                for (int e = 0; e < 4; ++e, bias += slope2) st[kb][gq * 4 + e] += bias;
-              }
-          } else {
-#pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-              for (int e = 0; e < 16; ++e)
-                st[kb][e] = fmaf(-slope2, fabsf(d0 + (float)off_of(kb, e)), st[kb][e]);
-          }
-        }
-        if (masked) {
-#pragma unroll
-          for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-              if (!sees(off_of(kb, e))) st[kb][e] = -INFINITY;
-        }
-        move_reference(CAP || BIAS ? tile_max() : tile_max() * scale_log2);
-        const float m = m_use();
-        exponentials([&](float x) { return CAP || BIAS ? x - m : fmaf(x, scale_log2, -m); });
-      }
-      // O^T[d][i] += sum_key V^T[d][key] P^T[key][i]; the A operand (V^T, lane:
-      // d = 32 dt + fr, keys 16 s + 8 (e/4) + 4 fh + e%4) comes from two
-      // transposed reads of the row-major V tile.
-      auto v_frag = [&](int dt, int s) {
-        const int r0 = 16 * s + tr_key, r1 = r0 + 8;
-        const int cc = 32 * dt + tr_col;  // head-dim column of this lane's 8-byte chunk
-        const int c16 = cc >> 3, half = (cc >> 2) & 1;
-        const u32x2 lo = lds_read_tr16(vs + r0 * S::kRowBytes + ((c16 ^ v_swz<D>(r0)) << 4) + half * 8);
-        const u32x2 hi = lds_read_tr16(vs + r1 * S::kRowBytes + ((c16 ^ v_swz<D>(r1)) << 4) + half * 8);
-        return u32x4{lo[0], lo[1], hi[0], hi[1]};
-      };
-      auto as_bf16 = [](const u32x4& w) { return __builtin_bit_cast(bf16x8, w); };
-      if constexpr (MOD) {
-        bool special = false;  // an infinity or NaN in a masked tile's V
-        if (masked) {
-          uint32_t top = 0;
-#pragma unroll
-          for (int i = 0; i < kBKV * CPR / 64; ++i) {
-            const u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) top = max(top, max((w[c] & 0x7fffu) << 16, w[c] & 0x7fff0000u));
-          }
-          special = __builtin_amdgcn_ballot_w64(top >= 0x7f800000u) != 0;
-        }
-        if (special) {
-          // key by key, for the queries that see it: the score again, from the
-          // query's two halves (fh), then V's row
-          const float m = m_use();
-#pragma unroll 1
-          for (int key = 0; key < kBKV; ++key) {
-            float x = 0.f;
-#pragma unroll
-            for (int s = 0; s < DSTEPS; ++s) {
-              const bf16x8 kf = *reinterpret_cast<const OPS_LDS bf16x8*>(
-                  ks + key * S::kRowBytes + (((2 * s + fh) ^ k_swz<D>(key)) << 4));
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x = fmaf((float)kf[e], (float)qf[s][e], x);
-            }
-            x += other_half(x);
-            const int j = kv0 + key;
-            if constexpr (CAP) x = fabsf(x) <= mods.cap_bound ? mods.capped_small(x) : mods.capped(x);
-            else x *= scale_log2;
-            if constexpr (BIAS) x = fmaf(-slope2, fabsf((float)(j - q_pos)), x);
-            if (!(j < pre || (j >= own_lo && j <= own_hi))) continue;
-            const float p = (float)(__bf16)fast_exp2(x - m);
-#pragma unroll
-            for (int i = 0; i < DT * 4; ++i) {  // columns 8 i + 4 fh .. + 3
-              const bf16x4 w = *reinterpret_cast<const OPS_LDS bf16x4*>(vs + key * S::kRowBytes +
-                                                                        ((i ^ v_swz<D>(key)) << 4) + fh * 8);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) acc[i >> 2][(i & 3) * 4 + e] = fmaf(p, (float)w[e], acc[i >> 2][(i & 3) * 4 + e]);
-            }
-          }
-          continue;
-        }
-      }
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(v_frag(dt, s)), pf[s], acc[dt], 0, 0, 0);
-      }
-    }
-
-    // normalize and store: lane owns query q_pos; acc[dt][e] is
-    // d = dt*32 + (e/4)*8 + fh*4 + e%4.
-    const float l_tot = l_part + other_half(l_part);
-    if (q_pos < L && q_lo < L) {
-      const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-      __bf16* orow = o + ((int64_t)(seq0 + q_pos) * Hq + h) * D;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int gq = 0; gq < 4; ++gq) {
-          u32x2 out;
-          out[0] = pack_bf2(acc[dt][gq * 4 + 0] * inv, acc[dt][gq * 4 + 1] * inv);
-          out[1] = pack_bf2(acc[dt][gq * 4 + 2] * inv, acc[dt][gq * 4 + 3] * inv);
-          *reinterpret_cast<u32x2*>(orow + dt * 32 + gq * 8 + fh * 4) = out;
-        }
-    }
-    wait_vmem();      // (a stage load of a wave with no active step may still be in flight)
-    __syncthreads();  // the next tile reuses the LDS stages
-  };
-
-  if constexpr (!LIST) {
-    const int bx = blockIdx.x;
-    const int b = bx / (Hkv * nhb);
-    const int g = (bx / nhb) % Hkv;
-    const int hb = bx % nhb;
-    const int seq0 = cu[b];
-    const int L = cu[b + 1] - seq0;
-    const int ntiles = (L + BQ - 1) / BQ;
-    for (int t = gridDim.y - 1 - blockIdx.y; t < ntiles; t += gridDim.y) do_tile(b, g, hb, t, seq0, L);
-  } else {
-    // n_s[b]: query tiles of prompt b.  The list holds, for every level t from
-    // the highest down, the prompts with a tile at level t (batch order), each
-    // with its HG (KV head, head block) pairs.  The tile groups at levels >= t
-    // number F(t) = sum_b max(0, n_b - t), so item group q sits at the level
-    // t with F(t + 1) <= q < F(t), found by bisection.
-    // The table (cu_s, n_s) sits in the K/V stage buffers, so it is rebuilt
-    // for every item: the tile's loads overwrite it.
-    static_assert((2 * kMaxListB + 1) * 4 <= S::kTotal, "work table does not fit the stage buffers");
-    OPS_LDS int32_t* cu_s = (OPS_LDS int32_t*)smem;
-    OPS_LDS int32_t* n_s = cu_s + kMaxListB + 1;
-    const int HG = Hkv * nhb;
-    for (int64_t i = blockIdx.x;; i += gridDim.x) {
-      for (int x = threadIdx.x; x <= B; x += 256) {
-        const int c = cu[x];
-        cu_s[x] = c;
-        if (x < B) n_s[x] = (cu[x + 1] - c + BQ - 1) >> bq_shift;
-      }
-      __syncthreads();
-      // (values below are equal in every lane and every wave; the first 64
-      // tile counts stay in a register)
-      const int n0 = lane < B ? n_s[lane] : 0;
-      auto F = [&](int t) {
-        int acc_n = max(0, n0 - t);
-        for (int b0 = 64; b0 < B; b0 += 64)
-          if (b0 + lane < B) acc_n += max(0, n_s[b0 + lane] - t);
-        return wave_sum_i(acc_n);
-      };
-      int top = n0;
-      for (int b0 = 64; b0 < B; b0 += 64)
-        if (b0 + lane < B) top = max(top, n_s[b0 + lane]);
-      top = wave_max_i(top);
-      if (i >= (int64_t)F(0) * HG) break;
-      const int qg = (int)(i / HG), r = (int)(i % HG);
-      int lo = 0, hi = top;  // F(lo) > qg >= F(hi)
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (F(mid) > qg) lo = mid;
-        else hi = mid;
-      }
-      const int t = lo;
-      // the j-th prompt (batch order) with a tile at level t
-      int j = qg - F(t + 1);
-      int b = 0;
-      for (int b0 = 0; b0 < B; b0 += 64) {
-        const bool has = b0 == 0 ? n0 > t : (b0 + lane < B && n_s[b0 + lane] > t);
-        const uint64_t m = __builtin_amdgcn_ballot_w64(has);
-        const int pc = __builtin_popcountll(m);
-        if (j < pc) {
-          const int before = __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0));
-          b = b0 + __builtin_ctzll(__builtin_amdgcn_ballot_w64(has && before == j));
-          break;
-        }
-        j -= pc;
-      }
-      // the values are uniform; saying so keeps the tile's buffer descriptors
-      // in scalar registers
-      const int ub = __builtin_amdgcn_readfirstlane(b);
-      const int s0 = __builtin_amdgcn_readfirstlane(cu_s[ub]);
-      const int s1 = __builtin_amdgcn_readfirstlane(cu_s[ub + 1]);
-      __syncthreads();  // every wave has read the table
-      do_tile(ub, r / nhb, r % nhb, t, s0, s1 - s0);
-    }
-  }
+  p.hpb = (G % 4 == 0) ? 4 : (G % 2 == 0) ? 2 : 1;
+  const int BQ = 32 * (4 / p.hpb);
+  // The grid launches B x ceil(max_seqlen / BQ) x HG workgroups, of which
+  // only sum_b ceil(L_b / BQ) x HG have a tile; the work list launches about
+  // that many (an upper bound: total_tokens / BQ + B tiles per HG) but pays a
+  // small fixed cost per workgroup to find its item.  Prompts that fill less
+  // than three quarters of B x max_seqlen favour the work list.
+  const int64_t max_items = (total_tokens / BQ + B) * (int64_t)Hkv * (G / p.hpb);
+  p.list = B <= kMaxListB && (double)total_tokens < 0.75 * (double)B * (double)max_seqlen;
+  // OPSCALE_TUNE_PREFILL_SCHEDULE overrides the choice (0 grid, 1 list);
+  // batches of more than kMaxListB prompts always use the grid.
+  const int32_t force = tuning(OPSCALE_TUNE_PREFILL_SCHEDULE);
+  if (force == 0) p.list = false;
+  else if (force == 1) p.list = B <= kMaxListB;
+  p.x = p.list ? (unsigned)std::min<int64_t>(0x7fffffff, max_items) : (unsigned)(B * Hkv * (G / p.hpb));
+  p.y = p.list ? 1u : (unsigned)std::min<int64_t>(65535, (max_seqlen + BQ - 1) / BQ);
+  return p;
 }
 
 // ------------------------------------------------------------ fp32 path ----
@@ -580,7 +165,8 @@ template <int D, bool LIST, bool MOD>
 __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_prefill_f32_kernel(
     const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v,
     int64_t q_stride, int64_t kv_stride, float* __restrict__ o, const int32_t* __restrict__ cu,
-    int B, int Hq, int Hkv, int64_t items, int levels, int min_len, float scale, int causal, const AttnMods mods) {
+    int B, int Hq, int Hkv, int64_t items, int levels, int min_len, float scale, int causal,
+    const MaybeMods<MOD> mods) {
   constexpr int DC = D / 8, DT = D / 32;  // chunk pairs of a row, 32-wide output tiles
   constexpr int kCols = 64, kPad = kCols + 4;  // the merge takes 64 columns at a time
   __shared__ __attribute__((aligned(16))) float os[4][32][kPad];
@@ -796,7 +382,7 @@ template <int D, bool MOD>
 __global__ __launch_bounds__(64) void attn_prefill_f32_row_kernel(
     const float* __restrict__ q, const float* __restrict__ k, const float* __restrict__ v,
     int64_t q_stride, int64_t kv_stride, float* __restrict__ o, const int32_t* __restrict__ cu,
-    int B, int Hq, int Hkv, int max_len, float scale, int causal, const AttnMods mods) {
+    int B, int Hq, int Hkv, int max_len, float scale, int causal, const MaybeMods<MOD> mods) {
   constexpr int DPL = D / 64;
   __shared__ float qs[D];
   __shared__ float ps[64];
@@ -866,7 +452,7 @@ hipError_t launch_attn_prefill_f32(const void* q, const void* k, const void* v,
                                           int64_t q_stride, int64_t kv_stride, void* o,
                                           const int32_t* cu, int32_t B, int64_t total_tokens, int32_t max_seqlen,
                                           int32_t Hq, int32_t Hkv, int32_t D, float scale, bool causal,
-                                          const AttnMods& mods, hipStream_t s) {
+                                          const MaybeMods<MOD>& mods, hipStream_t s) {
   const AttnF32Plan p = attn_f32_plan(B, total_tokens, max_seqlen, Hq, D);
   const float *qf = static_cast<const float*>(q), *kf = static_cast<const float*>(k);
   const float* vf = static_cast<const float*>(v);
@@ -883,45 +469,6 @@ hipError_t launch_attn_prefill_f32(const void* q, const void* k, const void* v,
                              : (p.levels ? &attn_prefill_f32_kernel<64, false, MOD> : &attn_prefill_f32_kernel<64, true, MOD>);
   hipLaunchKernelGGL(kern, dim3(p.grid), dim3(256), 0, s, qf, kf, vf, q_stride, kv_stride, of, cu, B, Hq, Hkv, p.items,
                      p.levels, p.row_len, scale, (int)causal, mods);
-  return hipGetLastError();
-}
-
-template <int MODE>
-hipError_t launch_attn_prefill_bf16(const void* q, const void* k, const void* v, int64_t q_stride, int64_t kv_stride,
-                                    void* o, const int32_t* cu, int32_t B, int64_t total_tokens, int32_t max_seqlen,
-                                    int32_t Hq, int32_t Hkv, int32_t D, float scale, bool causal, const AttnMods& mods,
-                                    hipStream_t s) {
-  const int G = Hq / Hkv;
-  const int hpb = (G % 4 == 0) ? 4 : (G % 2 == 0) ? 2 : 1;
-  const int BQ = 32 * (4 / hpb);
-  const float sl2 = scale * kLog2e;
-  // The grid launches B x ceil(max_seqlen / BQ) x HG workgroups, of which
-  // only sum_b ceil(L_b / BQ) x HG have a tile; the work list launches about
-  // that many (an upper bound: total_tokens / BQ + B tiles per HG) but pays a
-  // small fixed cost per workgroup to find its item.  Prompts that fill less
-  // than three quarters of B x max_seqlen favour the work list.
-  const int64_t max_items = (total_tokens / BQ + B) * (int64_t)Hkv * (G / hpb);
-  bool list = B <= kMaxListB && (double)total_tokens < 0.75 * (double)B * (double)max_seqlen;
-  // OPSCALE_TUNE_PREFILL_SCHEDULE overrides the choice (0 grid, 1 list);
-  // batches of more than kMaxListB prompts always use the grid.
-  const int32_t force = tuning(OPSCALE_TUNE_PREFILL_SCHEDULE);
-  if (force == 0) list = false;
-  else if (force == 1) list = B <= kMaxListB;
-  const unsigned gx = list ? (unsigned)std::min<int64_t>(0x7fffffff, max_items) : (unsigned)(B * Hkv * (G / hpb));
-  const unsigned gy = list ? 1u : (unsigned)std::min<int64_t>(65535, (max_seqlen + BQ - 1) / BQ);
-#define OPS_PF(DD, P)                                                                                   \
-  hipLaunchKernelGGL((attn_prefill_bf16_kernel<DD, P, MODE>), dim3(gx, gy), dim3(256), 0, s,            \
-                     static_cast<const __bf16*>(q), static_cast<const __bf16*>(k),                      \
-                     static_cast<const __bf16*>(v), q_stride, kv_stride, static_cast<__bf16*>(o), cu, B, \
-                     Hq, Hkv, hpb, sl2, (int)causal, mods)
-  if (D == 128) {
-    if (list) OPS_PF(128, true);
-    else OPS_PF(128, false);
-  } else {
-    if (list) OPS_PF(64, true);
-    else OPS_PF(64, false);
-  }
-#undef OPS_PF
   return hipGetLastError();
 }
 

@@ -100,7 +100,7 @@ hipError_t launch_attn_decode(const void* q, int64_t q_stride, const void* kcach
   const DecodeWs w = decode_ws(ws, B, Hq, D, nwg);
   if (B > kInlineB) {
     hipLaunchKernelGGL(attn_decode_plan_kernel<false>, dim3(1), dim3(1024), 0, s, ctx, B, max_blocks << log2bs, nwg,
-                       w.tcs, w.first, AttnMods{});
+                       w.tcs, w.first, NoMods{});
     const hipError_t e0 = hipGetLastError();
     if (e0 != hipSuccess) return e0;
   }
@@ -116,7 +116,7 @@ hipError_t launch_attn_decode(const void* q, int64_t q_stride, const void* kcach
   hipLaunchKernelGGL((attn_decode_split_kernel<DD, GG, HH, II, false>), grid, dim3(kWaves * 64), 0, s,  \
                      static_cast<const __bf16*>(q), q_stride, static_cast<const __bf16*>(kcache), \
                      static_cast<const __bf16*>(vcache), table, ctx, Hq, Hkv, log2bs, max_blocks, \
-                     num_blocks, w.tcs, w.first, B, nwg, sl2, w.o, w.ml, GG, AttnMods{})
+                     num_blocks, w.tcs, w.first, B, nwg, sl2, w.o, w.ml, GG, NoMods{})
 #define OPS_DEC_H(DD, GG)                    \
   switch (HB) {                              \
     case 1: OPS_DEC(DD, GG, 1); break;       \
@@ -142,7 +142,7 @@ hipError_t launch_attn_decode(const void* q, int64_t q_stride, const void* kcach
 #undef OPS_DEC_L
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return launch_decode_combine<false>(w, ctx, max_blocks << log2bs, static_cast<__bf16*>(o), B, Hq, D, nwg, AttnMods{},
+  return launch_decode_combine<false>(w, ctx, max_blocks << log2bs, static_cast<__bf16*>(o), B, Hq, D, nwg, NoMods{},
                                       s);
 }
 
