@@ -537,44 +537,46 @@ def opscale_rope_frequencies(rot: int, theta: float, scaling: str = "none", fact
     return torch.tensor(list(f), dtype=torch.float64, device=device), m.value
 
 
-_i32, _f32, _f64 = None, None, None  # torch's dtypes, filled on first use
+_i32 = _f32 = _f64 = None  # torch's dtypes, filled on first use
 
 
-def _here(*named) -> None:
-    """Each (name, tensor) on the current device, where the call's kernels run."""
-    if _raw_stream is None:
-        _stream(None)
-    dev = _device()
-    for name, t_ in named:
-        if t_ is not None and t_.get_device() != dev:
-            raise OpscaleError(OPSCALE_ERR_INVALID_ARG,
-                               f"{name} is on {t_.device}: tensors must be on the GPU that is current (cuda:{dev})")
-
-
-def _ints(*named, size=None):
-    """Each (name, tensor) contiguous int32 on the current GPU, of `size` elements if given."""
-    global _i32
+def _current() -> int:
+    """The current GPU, where a call's kernels run."""
+    global _i32, _f32, _f64
     if _i32 is None:
         import torch
-        _i32 = torch.int32
-    _here(*named)
-    for name, t_ in named:
-        if t_.dtype != _i32 or not t_.is_contiguous() or (size is not None and t_.numel() != size):
-            raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"{name} must be a contiguous int32 tensor"
-                               + ("" if size is None else f" of {size} elements"))
+        _stream(None)
+        _i32, _f32, _f64 = torch.int32, torch.float32, torch.float64
+    return _device()
 
 
-def _rows(name, t_, T, H, D, dtype) -> int:
+def _refuse(name, t_, what, dev):
+    at = t_.get_device()
+    where = "" if at == dev else f"; it is on {t_.device}, the current GPU is cuda:{dev}"
+    raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"{name} must be {what}, is {t_.dtype} {tuple(t_.shape)} with strides "
+                       f"{t_.stride()}{where}")
+
+
+def _rows(name, t_, shape, dtype, dev) -> int:
     """The row stride of t_ [T, H, D] (heads contiguous; any of a single row's)."""
-    if t_.dtype != dtype or t_.dim() != 3 or t_.shape[0] != T:
-        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"{name} must be {dtype} with {T} rows of heads")
-    _heads_view(name, t_, H, D)
-    return t_.stride(0) if T > 1 else H * D
+    T, H, D = shape
+    st = t_.stride()
+    if t_.dtype != dtype or t_.shape != shape or st[2] != 1 or (st[1] != D and H > 1) or t_.get_device() != dev:
+        _refuse(name, t_, f"{dtype} [{T}, {H}, {D}] with contiguous heads", dev)
+    return st[0] if T > 1 else H * D
 
 
-def _weight(name, t_, n, dtype):
-    if t_.dtype != dtype or t_.numel() != n or not t_.is_contiguous():
-        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"{name} must be contiguous {dtype} of {n} elements")
+def _flat(name, t_, n, dtype, dev):
+    """t_ contiguous, of n elements; its address."""
+    if t_.dtype != dtype or t_.numel() != n or t_.get_device() != dev or not t_.is_contiguous():
+        _refuse(name, t_, f"contiguous {dtype} of {n} elements", dev)
+    return t_.data_ptr()
+
+
+def _cache(name, t_, shape, dtype, dev):
+    if t_.dtype != dtype or t_.shape != shape or t_.get_device() != dev or not t_.is_contiguous():
+        _refuse(name, t_, f"contiguous {dtype} {tuple(shape)}", dev)
+    return t_.data_ptr()
 
 
 def opscale_qk_norm_rope(q, k, positions=None, inv_freq=None, q_weight=None, k_weight=None, eps: float = 1e-6,
@@ -587,75 +589,61 @@ def opscale_qk_norm_rope(q, k, positions=None, inv_freq=None, q_weight=None, k_w
     q_out and k_out; the token dimension of each may be strided.
     opscale_rope_frequencies makes inv_freq and magnitude.  Returns (q, k), the
     results."""
-    global _f64
     lib = load()
-    dt, dtype = _dt(q), q.dtype
+    dev, dt, dtype = _current(), _dt(q), q.dtype
     if q.dim() != 3 or k.dim() != 3:
         raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "q and k must be [T, heads, D]")
-    T, Hq, D = q.shape
+    q_shape = T, Hq, D = q.shape
     Hkv = k.shape[1]
-    q_out = q if q_out is None else q_out
-    k_out = k if k_out is None else k_out
-    _here(("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out), ("inv_freq", inv_freq), ("q_weight", q_weight),
-          ("k_weight", k_weight))
-    qs, ks = _rows("q", q, T, Hq, D, dtype), _rows("k", k, T, Hkv, D, dtype)
-    qos = qs if q_out is q else _rows("q_out", q_out, T, Hq, D, dtype)
-    kos = ks if k_out is k else _rows("k_out", k_out, T, Hkv, D, dtype)
-    rot = 0
+    k_shape = T, Hkv, D
+    qs, ks = _rows("q", q, q_shape, dtype, dev), _rows("k", k, k_shape, dtype, dev)
+    if q_out is None:
+        q_out, qos = q, qs
+    else:
+        qos = _rows("q_out", q_out, q_shape, dtype, dev)
+    if k_out is None:
+        k_out, kos = k, ks
+    else:
+        kos = _rows("k_out", k_out, k_shape, dtype, dev)
+    rot, pos, freq, wq, wk = 0, None, None, None, None
     if inv_freq is not None:
-        if _f64 is None:
-            import torch
-            _f64 = torch.float64
-        _weight("inv_freq", inv_freq, inv_freq.numel(), _f64)
         if positions is None:
             raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "a rotation takes positions")
-        _ints(("positions", positions), size=T)
         rot = 2 * inv_freq.numel()
-    else:
-        positions = None
-    if (q_weight is None) != (k_weight is None):
-        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "q_weight and k_weight are given both or neither")
-    if q_weight is not None:
-        _weight("q_weight", q_weight, D, dtype)
-        _weight("k_weight", k_weight, D, dtype)
+        freq = _flat("inv_freq", inv_freq, rot // 2, _f64, dev)
+        pos = _flat("positions", positions, T, _i32, dev)
+    if q_weight is not None or k_weight is not None:
+        if q_weight is None or k_weight is None:
+            raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "q_weight and k_weight are given both or neither")
+        wq, wk = _flat("q_weight", q_weight, D, dtype, dev), _flat("k_weight", k_weight, D, dtype, dev)
     bs = nb = vs = 0
-    if k_cache is None and v_cache is None:
-        v = slot_mapping = None
-    else:
+    vp = kc = vc = slots = None
+    if k_cache is not None or v_cache is not None:
         if k_cache is None or v_cache is None or v is None or slot_mapping is None:
             raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "a cache write takes k_cache, v_cache, v and slot_mapping")
-        _here(("v", v), ("k_cache", k_cache), ("v_cache", v_cache))
-        vs = _rows("v", v, T, Hkv, D, dtype)
-        _ints(("slot_mapping", slot_mapping), size=T)
-        nb, bs = k_cache.shape[0], k_cache.shape[1]
-        for n, t_ in (("k_cache", k_cache), ("v_cache", v_cache)):
-            if tuple(t_.shape) != (nb, bs, Hkv, D) or t_.dtype != dtype or not t_.is_contiguous():
-                raise OpscaleError(OPSCALE_ERR_INVALID_ARG,
-                                   f"{n} must be contiguous {dtype} [num_blocks, block_size, {Hkv}, {D}]")
+        vs, vp = _rows("v", v, k_shape, dtype, dev), v.data_ptr()
+        slots = _flat("slot_mapping", slot_mapping, T, _i32, dev)
+        nb, bs = k_cache.shape[:2]
+        shape = nb, bs, Hkv, D
+        kc, vc = _cache("k_cache", k_cache, shape, dtype, dev), _cache("v_cache", v_cache, shape, dtype, dev)
     t = Timing() if timed else None
-    _check(lib.opscale_qk_norm_rope(_ptr(q), _ptr(k), qs, ks, _ptr(q_out), _ptr(k_out), qos, kos, _ptr(q_weight),
-                                    _ptr(k_weight), eps, _ptr(positions), _ptr(inv_freq), rot, int(interleaved),
-                                    magnitude, _ptr(v), vs, _ptr(k_cache), _ptr(v_cache), _ptr(slot_mapping), bs, nb,
-                                    T, Hq, Hkv, D, dt, _stream(stream), ctypes.byref(t) if t else None))
+    _check(lib.opscale_qk_norm_rope(q.data_ptr(), k.data_ptr(), qs, ks, q_out.data_ptr(), k_out.data_ptr(), qos, kos, wq,
+                                    wk, eps, pos, freq, rot, interleaved, magnitude, vp, vs, kc, vc, slots, bs, nb, T,
+                                    Hq, Hkv, D, dt, _stream(stream), ctypes.byref(t) if t else None))
     return ((q_out, k_out), t) if timed else (q_out, k_out)
 
 
-def _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, rows):
+def _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, rows, dev):
     """The score modifiers and masks of an attention call over B prompts or sequences."""
-    global _f32
     if slopes is not None:
-        if _f32 is None:
-            import torch
-            _f32 = torch.float32
-        _here(("slopes", slopes))
-        _weight("slopes", slopes, Hq, _f32)
+        slopes = _flat("slopes", slopes, Hq, _f32, dev)
     if prefix_lens is not None:
-        _ints(("prefix_lens", prefix_lens), size=B)
+        prefix_lens = _flat("prefix_lens", prefix_lens, B, _i32, dev)
     if doc_starts is not None:
-        _ints(("doc_starts", doc_starts), size=rows)
+        doc_starts = _flat("doc_starts", doc_starts, rows, _i32, dev)
     if not 0 <= window < 1 << 31:
         raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"window {window} must be in [0, 2^31)")
-    return AttnMods(softcap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(doc_starts))
+    return ctypes.byref(AttnMods(softcap, window, slopes, prefix_lens, doc_starts))
 
 
 def opscale_attn_prefill_mod(q, k, v, cu_seqlens, max_seqlen: int, scale: float, causal: bool = True,
@@ -667,25 +655,24 @@ def opscale_attn_prefill_mod(q, k, v, cu_seqlens, max_seqlen: int, scale: float,
     (doc_starts int32 [T], its first key, local to the prompt), fewer than `window`
     keys away and, causal, not ahead.  A query that sees no key gets zeros."""
     lib = load()
-    dt, dtype = _dt(q), q.dtype
+    dev, dt, dtype = _current(), _dt(q), q.dtype
     if q.dim() != 3 or k.dim() != 3:
         raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "q and k must be [T, heads, D]")
-    T, Hq, D = q.shape
+    shape = T, Hq, D = q.shape
     Hkv = k.shape[1]
-    if out is None:
-        out = q.new_empty((T, Hq, D))
-    _here(("q", q), ("k", k), ("v", v), ("out", out))
-    qs, ks, vs = _rows("q", q, T, Hq, D, dtype), _rows("k", k, T, Hkv, D, dtype), _rows("v", v, T, Hkv, D, dtype)
+    kv = T, Hkv, D
+    qs, ks, vs = _rows("q", q, shape, dtype, dev), _rows("k", k, kv, dtype, dev), _rows("v", v, kv, dtype, dev)
     if ks != vs:
         raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "k and v must share a row stride")
-    _weight("out", out, T * Hq * D, dtype)
+    if out is None:
+        out = q.new_empty(shape)
     B = cu_seqlens.numel() - 1
-    _ints(("cu_seqlens", cu_seqlens))
-    mods = _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, T)
+    cu = _flat("cu_seqlens", cu_seqlens, B + 1, _i32, dev)
+    mods = _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, T, dev)
     t = Timing() if timed else None
-    _check(lib.opscale_attn_prefill_mod(_ptr(q), _ptr(k), _ptr(v), qs, ks, _ptr(out), _ptr(cu_seqlens), B, T,
-                                        max_seqlen, Hq, Hkv, D, scale, int(causal), ctypes.byref(mods), dt,
-                                        _stream(stream), ctypes.byref(t) if t else None))
+    _check(lib.opscale_attn_prefill_mod(q.data_ptr(), k.data_ptr(), v.data_ptr(), qs, ks,
+                                        _flat("out", out, T * Hq * D, dtype, dev), cu, B, T, max_seqlen, Hq, Hkv, D,
+                                        scale, causal, mods, dt, _stream(stream), ctypes.byref(t) if t else None))
     return (out, t) if timed else out
 
 
@@ -705,29 +692,27 @@ def opscale_attn_decode_mod(q, k_cache, v_cache, block_table, context_lens, max_
     if q.dim() != 3 or k_cache.dim() != 4 or block_table.dim() != 2:
         raise OpscaleError(OPSCALE_ERR_INVALID_ARG,
                            "q must be [B, Hq, D], the caches [num_blocks, block_size, Hkv, D], block_table [B, max_blocks]")
-    B, Hq, D = q.shape
-    nb, bs, Hkv, _ = k_cache.shape
-    if out is None:
-        out = q.new_empty((B, Hq, D))
-    _here(("q", q), ("k_cache", k_cache), ("v_cache", v_cache), ("out", out), ("workspace", workspace))
-    qs = _rows("q", q, B, Hq, D, dtype)
-    for n, t_ in (("k_cache", k_cache), ("v_cache", v_cache)):
-        if tuple(t_.shape) != (nb, bs, Hkv, D) or t_.dtype != dtype or not t_.is_contiguous():
-            raise OpscaleError(OPSCALE_ERR_INVALID_ARG,
-                               f"{n} must be contiguous {dtype} [num_blocks, block_size, {Hkv}, {D}]")
-    _weight("out", out, B * Hq * D, dtype)
+    dev = _current()
+    shape = B, Hq, D = q.shape
+    qs = _rows("q", q, shape, dtype, dev)
+    cache = nb, bs, Hkv, _ = k_cache.shape
+    if cache[3] != D:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"the caches have heads of {cache[3]}, q of {D}")
+    kc, vc = _cache("k_cache", k_cache, cache, dtype, dev), _cache("v_cache", v_cache, cache, dtype, dev)
     cols = block_table.shape[1]
-    _ints(("block_table", block_table), size=B * cols)
-    _ints(("context_lens", context_lens), size=B)
-    mods = _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, B)
+    table = _flat("block_table", block_table, B * cols, _i32, dev)
+    ctx = _flat("context_lens", context_lens, B, _i32, dev)
+    mods = _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, B, dev)
+    if out is None:
+        out = q.new_empty(shape)
     if workspace is None:
         workspace = _scratch(lib.opscale_attn_decode_mod_workspace_size(B, Hq, D, max_context_len), q, stream)
+    nbytes = workspace.numel() * workspace.element_size()
     t = Timing() if timed else None
-    _check(lib.opscale_attn_decode_mod(_ptr(q), qs, _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
-                                       _ptr(context_lens), _ptr(out), B, Hq, Hkv, D, bs, cols, nb, max_context_len,
-                                       scale, ctypes.byref(mods), dt, _ptr(workspace),
-                                       workspace.numel() * workspace.element_size(), _stream(stream),
-                                       ctypes.byref(t) if t else None))
+    _check(lib.opscale_attn_decode_mod(q.data_ptr(), qs, kc, vc, table, ctx, _flat("out", out, B * Hq * D, dtype, dev),
+                                       B, Hq, Hkv, D, bs, cols, nb, max_context_len, scale, mods, dt,
+                                       _flat("workspace", workspace, workspace.numel(), workspace.dtype, dev), nbytes,
+                                       _stream(stream), ctypes.byref(t) if t else None))
     return (out, t) if timed else out
 
 
@@ -740,23 +725,26 @@ def opscale_block_tables(context_lens, new_lens, block_table, free_blocks, free_
     slot_mapping [max_tokens], kv_lens [B], free_next [1]); `out`: the same five,
     to be filled.  Tokens past the last are padding (position 0, slot -1)."""
     lib = load()
+    dev = _current()
+    if block_table.dim() != 2:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "block_table must be [B, max_blocks_per_seq]")
     B, cols = block_table.shape
-    _ints(("context_lens", context_lens), ("new_lens", new_lens), size=B)
-    _ints(("block_table", block_table), ("free_blocks", free_blocks))
-    _ints(("free_begin", free_begin), size=1)
+    ctx, fresh = _flat("context_lens", context_lens, B, _i32, dev), _flat("new_lens", new_lens, B, _i32, dev)
+    table = _flat("block_table", block_table, B * cols, _i32, dev)
+    num_free = free_blocks.numel()
+    free, begin = _flat("free_blocks", free_blocks, num_free, _i32, dev), _flat("free_begin", free_begin, 1, _i32, dev)
+    sizes = B + 1, max_tokens, max_tokens, B, 1
     if out is None:
-        new = context_lens.new_empty
-        out = new(B + 1), new(max_tokens), new(max_tokens), new(B), new(1)
+        if not 0 <= max_tokens < 1 << 31:
+            raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"max_tokens {max_tokens} must be in [0, 2^31)")
+        out = context_lens.new_empty(sum(sizes)).split(sizes)  # (one allocation)
+        ptrs = [t_.data_ptr() for t_ in out]
     else:
-        for n, t_, size in zip(("cu_seqlens", "positions", "slot_mapping", "kv_lens", "free_next"), out,
-                               (B + 1, max_tokens, max_tokens, B, 1)):
-            _ints((n, t_), size=size)
-    cu, positions, slots, kv_lens, free_next = out
+        names = "cu_seqlens", "positions", "slot_mapping", "kv_lens", "free_next"
+        ptrs = [_flat(n, t_, size, _i32, dev) for n, t_, size in zip(names, out, sizes)]
     t = Timing() if timed else None
-    _check(lib.opscale_block_tables(_ptr(context_lens), _ptr(new_lens), B, _ptr(block_table), cols, block_size,
-                                    _ptr(free_blocks), free_blocks.numel(), _ptr(free_begin), max_tokens, _ptr(cu),
-                                    _ptr(positions), _ptr(slots), _ptr(kv_lens), _ptr(free_next), _stream(stream),
-                                    ctypes.byref(t) if t else None))
+    _check(lib.opscale_block_tables(ctx, fresh, B, table, cols, block_size, free, num_free, begin, max_tokens, *ptrs,
+                                    _stream(stream), ctypes.byref(t) if t else None))
     return (out, t) if timed else out
 
 
