@@ -373,14 +373,14 @@ opscale_status check_prefill_mod(const void* q, const void* k, const void* v, in
 opscale_status check_decode(const void* q, int64_t qs, const void* kc, const void* vc, const int32_t* table,
                             const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
                             int32_t bs, int32_t max_blocks, int64_t num_blocks, int32_t max_ctx,
-                            float scale, opscale_dtype dt, void* ws, size_t ws_bytes, bool any_group = false) {
+                            float scale, opscale_dtype dt, void* ws, size_t ws_bytes, bool mod = false) {
   if (!dtype_ok(dt)) return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode: unknown dtype %d", (int)dt);
   if (B < 0 || Hq <= 0 || Hkv <= 0 || B > 65535 || Hq > 65535)
     return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode: bad sizes B=%d Hq=%d Hkv=%d", B, Hq, Hkv);
   if (Hq % Hkv) return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode: Hkv=%d does not divide Hq=%d", Hkv, Hq);
   if (D != 64 && D != 128) return fail(OPSCALE_ERR_UNSUPPORTED, "attn_decode: head_dim %d (supported: 64, 128)", D);
   const int G = Hq / Hkv;
-  if (dt == OPSCALE_BF16 && !any_group && G != 1 && G != 2 && G != 4 && G != 8)
+  if (dt == OPSCALE_BF16 && !mod && G != 1 && G != 2 && G != 4 && G != 8)
     return fail(OPSCALE_ERR_UNSUPPORTED, "attn_decode: bf16 supports Hq/Hkv in {1, 2, 4, 8}, got %d", G);
   if (bs < 1 || bs > 1024 || (bs & (bs - 1)))
     return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode: block_size %d must be a power of two in [1, 1024]", bs);
@@ -397,7 +397,8 @@ opscale_status check_decode(const void* q, int64_t qs, const void* kc, const voi
   if (!aligned16(q) || !aligned16(kc) || !aligned16(vc) || !aligned16(o) ||
       (reinterpret_cast<uintptr_t>(table) & 3) || (reinterpret_cast<uintptr_t>(ctx) & 3))
     return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode: tensors must be 16-byte aligned, indices 4-byte");
-  const size_t need = opscale::decode_workspace_bytes(B, Hq, D, max_ctx);
+  const size_t need = mod ? opscale::decode_mod_workspace_bytes(B, Hq, D, max_ctx)
+                          : opscale::decode_workspace_bytes(B, Hq, D, max_ctx);
   if (dt == OPSCALE_BF16 && (!ws || ws_bytes < need || !aligned16(ws)))
     return fail(OPSCALE_ERR_WORKSPACE, "attn_decode: workspace of %zu bytes (16-byte aligned) needed, got %zu",
                 need, ws ? ws_bytes : (size_t)0);
@@ -424,7 +425,7 @@ opscale_status check_decode_mod(const void* q, int64_t qs, const void* kc, const
                       {ctx, 4ll * B}, {m ? m->slopes : nullptr, 4ll * Hq}, {m ? m->prefix_lens : nullptr, 4ll * B},
                       {m ? m->doc_starts : nullptr, 4ll * B}};
   const Range out{o, (int64_t)B * Hq * D * s};
-  const Range work{dt == OPSCALE_BF16 ? ws : nullptr, (int64_t)opscale::decode_workspace_bytes(B, Hq, D, max_ctx)};
+  const Range work{dt == OPSCALE_BF16 ? ws : nullptr, (int64_t)opscale::decode_mod_workspace_bytes(B, Hq, D, max_ctx)};
   for (const Range& r : in)
     if (r.p && (overlap(r.p, r.n, out.p, out.n) || (work.p && overlap(r.p, r.n, work.p, work.n))))
       return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: o and the workspace must not overlap an input");
@@ -994,7 +995,8 @@ opscale_status opscale_attn_prefill_mod(const void* q, const void* k, const void
 }
 
 size_t opscale_attn_decode_mod_workspace_size(int32_t B, int32_t Hq, int32_t D, int32_t max_context_len) {
-  return opscale_attn_decode_workspace_size(B, Hq, D, max_context_len);
+  if (B <= 0 || Hq <= 0 || D <= 0) return 16;
+  return opscale::decode_mod_workspace_bytes(B, Hq, D, std::max<int32_t>(1, max_context_len));
 }
 
 opscale_status opscale_attn_decode_mod(const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache,

@@ -115,7 +115,9 @@ hipError_t launch_attn_decode(const void* q, int64_t q_stride, const void* kc, c
                               int32_t max_context_len, float scale, bool bf16, void* ws,
                               hipStream_t s);
 
-// The same with score modifiers and masks (m may be null), any Hq / Hkv.
+// The same with score modifiers and masks (m may be null), any Hq / Hkv; its workspace
+// is laid out alike, for up to twice the workgroups.
+size_t decode_mod_workspace_bytes(int32_t B, int32_t Hq, int32_t D, int32_t max_context_len);
 hipError_t launch_attn_decode_mod(const void* q, int64_t q_stride, const void* kc, const void* vc, const int32_t* table,
                                   const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
                                   int32_t block_size, int32_t max_blocks, int64_t num_blocks, int32_t max_context_len,

@@ -427,9 +427,12 @@ def test_decode_without_modifiers_is_the_plain_operator(ops, Hq, Hkv):
     args = (q, cuda(kc), cuda(vc), i32(table), i32(ctx), 700, 0.09)
     a, b = ops.opscale_attn_decode(*args), ops.opscale_attn_decode_mod(*args)
     torch.cuda.synchronize()
-    assert torch.equal(a, b)
-    ref = step.attn_decode_mod(f64(q.cpu()), f64(kc), f64(vc), table, ctx, 0.09)
-    assert np.abs(f64(a.cpu()) - ref).max() <= 2.0 ** -6 * np.abs(ref).max()
+    # (the two split the keys differently: each is held to the definition)
+    qh, kh = f64(q.cpu()), f64(kc)
+    ref, weighted = (step.attn_decode_mod(qh, kh, v, table, ctx, 0.09) for v in (f64(vc), np.abs(f64(vc))))
+    tol = tolerance(ref, weighted, "bf16", 128, 700, 0.09 * np.abs(qh).sum(-1).max() * np.abs(kh).max(), None, 0.0)
+    near(f64(a.cpu()), ref, tol, "plain")
+    near(f64(b.cpu()), ref, tol, "without modifiers")
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
