@@ -425,7 +425,8 @@ size_t opscale_attn_decode_mod_workspace_size(int32_t B, int32_t Hq, int32_t D, 
 
 /*
  * opscale_attn_decode with score modifiers and masks (its arguments, layouts and
- * conditions; mods NULL: none; o and the workspace overlap nothing else), the query
+ * conditions, but both paths need the workspace; mods NULL: none; o and the workspace
+ * overlap nothing else), the query
  * of sequence b at position context_lens[b] - 1.  Only 32-key tiles that hold a
  * visible key are read.  Any Hq / Hkv on both paths.
  */

@@ -399,7 +399,7 @@ opscale_status check_decode(const void* q, int64_t qs, const void* kc, const voi
     return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode: tensors must be 16-byte aligned, indices 4-byte");
   const size_t need = mod ? opscale::decode_mod_workspace_bytes(B, Hq, D, max_ctx)
                           : opscale::decode_workspace_bytes(B, Hq, D, max_ctx);
-  if (dt == OPSCALE_BF16 && (!ws || ws_bytes < need || !aligned16(ws)))
+  if ((dt == OPSCALE_BF16 || mod) && (!ws || ws_bytes < need || !aligned16(ws)))
     return fail(OPSCALE_ERR_WORKSPACE, "attn_decode: workspace of %zu bytes (16-byte aligned) needed, got %zu",
                 need, ws ? ws_bytes : (size_t)0);
   return OPSCALE_OK;
@@ -425,11 +425,11 @@ opscale_status check_decode_mod(const void* q, int64_t qs, const void* kc, const
                       {ctx, 4ll * B}, {m ? m->slopes : nullptr, 4ll * Hq}, {m ? m->prefix_lens : nullptr, 4ll * B},
                       {m ? m->doc_starts : nullptr, 4ll * B}};
   const Range out{o, (int64_t)B * Hq * D * s};
-  const Range work{dt == OPSCALE_BF16 ? ws : nullptr, (int64_t)opscale::decode_mod_workspace_bytes(B, Hq, D, max_ctx)};
+  const Range work{ws, (int64_t)opscale::decode_mod_workspace_bytes(B, Hq, D, max_ctx)};
   for (const Range& r : in)
-    if (r.p && (overlap(r.p, r.n, out.p, out.n) || (work.p && overlap(r.p, r.n, work.p, work.n))))
+    if (r.p && (overlap(r.p, r.n, out.p, out.n) || overlap(r.p, r.n, work.p, work.n)))
       return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: o and the workspace must not overlap an input");
-  if (work.p && overlap(out.p, out.n, work.p, work.n))
+  if (overlap(out.p, out.n, work.p, work.n))
     return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: o overlaps the workspace");
   return OPSCALE_OK;
 }

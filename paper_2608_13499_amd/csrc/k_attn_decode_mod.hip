@@ -22,6 +22,11 @@
 // past that a one-workgroup kernel writes it to the workspace first.
 // A second kernel merges a (sequence, head)'s segments in order: deterministic.
 //
+// fp32 takes the same plan on v_mfma_f32_16x16x4_f32: K, Q and V in 16-byte loads
+// straight to the operand registers (step e of chunk s is column 16 s + 4 (lane / 16) + e for
+// scores, output column 4 (lane % 16) + e of 64 for P V: both relabel a summed or
+// an output index), exact tanhf, everything in fp32.
+//
 // A tile whose 32 keys are all visible, in valid pages of 16 slots or more, is
 // addressed from two scalar page bases with per-lane offsets that never change
 // (bf16, 256 sequences of 128 to 8192 tokens, 8 KV heads: per-key addresses from
@@ -72,7 +77,19 @@ __device__ __forceinline__ int64_t share(int64_t T, int g, int nwg) {
 }
 
 // What a key that is not there is read as.
-__device__ __align__(16) const uint32_t zero_row[128 / 2] = {};
+__device__ __align__(16) const uint32_t zero_row[128] = {};
+
+// Inclusive scan over the wave (DPP: shifts within a 16-lane row, then the last
+// lane of a row to the rows after it).
+__device__ __forceinline__ int wave_scan_i(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);
+  return v;
+}
 
 // max / sum of a value over the four 16-lane rows of a wave, on every lane.
 __device__ __forceinline__ float rows_max(float x) {
@@ -89,7 +106,7 @@ __device__ __forceinline__ float rows_sum(float x) {
 }
 
 struct DecodeArgs {
-  const __bf16 *q, *kc, *vc;
+  const void *q, *kc, *vc;
   int64_t q_stride;
   const int32_t *table, *ctx;
   int Hkv, GH;  // KV heads; query heads of each
@@ -99,27 +116,28 @@ struct DecodeArgs {
   const int32_t* first_b;
   int B, nwg;
   bool aligned;
-  float scale_log2;
+  float scale, scale_log2;
   float *ws_o, *ws_ml;
   AttnMods mods;
 };
 
 }  // namespace
 
-template <int D, int HB, bool INL>
-__global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArgs a) {
-  constexpr int CPR = D / 8;             // 16-byte chunks per cache row
-  constexpr int KSTEPS = D / 32;         // MFMA k-steps over the head dim (QK)
+template <bool BF16, int D, int HB, bool INL>
+__global__ __launch_bounds__(512, BF16 ? 4 : 2) void attn_decode_mod_kernel(const DecodeArgs a) {
+  constexpr int ES = BF16 ? 2 : 4;
+  constexpr int CPR = D / 8;             // bf16: 16-byte chunks per cache row
+  constexpr int KCH = D * ES / 64;       // 64-byte pieces of a row (16 bytes a lane of a 4-lane column)
   constexpr int DT = D / 16;             // 16-wide output tiles over the head dim (PV)
   constexpr int WPH = kWaves / HB;       // waves sharing one head
-  constexpr int VROWS = 64 / CPR;        // V rows per 1 KB wave load
-  constexpr int VLOADS = kTile / VROWS;  // wave loads per V tile
-  constexpr int VBYTES = kTile * D * 2;  // one V tile
+  constexpr int VROWS = 64 / CPR;        // bf16: V rows per 1 KB wave load
+  constexpr int VLOADS = kTile / VROWS;  // bf16: wave loads per V tile
+  constexpr int VBYTES = kTile * D * 2;  // bf16: one V tile; the merge's buffer
   constexpr int kNontemporal = 2;        // cache-policy bit NT: the cache is streamed once
   constexpr float kLazy = 8.f;
   __shared__ __attribute__((aligned(16))) char vbuf[kWaves][VBYTES];
   __shared__ int32_t pages[kMaxPages];
-  __shared__ int64_t tcs_s[INL ? kInlineB + 1 : 1];  // tiles before each sequence; aligned: pieces
+  __shared__ int64_t tcs_s[INL ? kInlineB + 1 : 1];  // tiles before each sequence
   __shared__ int32_t n_s[INL ? kInlineB : 1], pre_s[INL ? kInlineB : 1], lo_s[INL ? kInlineB : 1];
   __shared__ uint32_t wsum[kWaves];
   __shared__ float ml_s[kWaves][16][2];  // the waves' max and sum of each head
@@ -131,8 +149,35 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int col = lane & 15, grp = lane >> 4;
 
-  // Inclusive scan of x over the workgroup.
-  auto scan = [&](uint32_t x) -> int64_t {
+  int64_t t_lo, t_hi;  // this workgroup's tiles: of the list (straddling), or of sequence b_first
+  int b_first;
+  int own_n = 0, own_pre = 0, own_lo = 0;  // aligned: of b_first
+  if (INL && a.aligned) {
+    // up to 64 sequences, a lane each, every wave by itself
+    DecodeSpan sp{};
+    if (lane < a.B) sp = decode_span(a.mods, a.ctx, max_keys, lane);
+    int64_t T = (int64_t)wave_sum_i(sp.tiles >> 16) << 16;  // (of up to 2^32 in two halves)
+    T += wave_sum_i(sp.tiles & 0xffff);
+    if (T == 0) return;
+    const int64_t c = piece_tiles(T, a.nwg, a.B, WPH);
+    const int mine = c < (1 << 30) ? (sp.tiles + (int)c - 1) / (int)c : (sp.tiles > 0);
+    const int incl = wave_scan_i(mine);
+    const uint64_t here = __builtin_amdgcn_ballot_w64(incl - mine <= wgi && wgi < incl);
+    if (here == 0) return;  // fewer pieces than workgroups
+    b_first = __builtin_ctzll(here);
+    t_lo = (wgi - __builtin_amdgcn_readlane(incl - mine, b_first)) * c;
+    t_hi = min(t_lo + c, (int64_t)__builtin_amdgcn_readlane(sp.tiles, b_first));
+    own_n = __builtin_amdgcn_readlane(sp.n, b_first);
+    own_pre = __builtin_amdgcn_readlane(sp.pre, b_first);
+    own_lo = __builtin_amdgcn_readlane(sp.lo, b_first);
+  } else if constexpr (INL) {
+    const int t = threadIdx.x;
+    DecodeSpan sp{};
+    if (t < a.B) {
+      sp = decode_span(a.mods, a.ctx, max_keys, t);
+      n_s[t] = sp.n, pre_s[t] = sp.pre, lo_s[t] = sp.lo;
+    }
+    uint32_t x = (uint32_t)sp.tiles;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
       const uint32_t y = __shfl_up(x, d, 64);  // (at most 64 x 2^26 tiles: fits 32 bits)
@@ -142,54 +187,21 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
     __syncthreads();
     int64_t incl = x;
     for (int w = 0; w < wave; ++w) incl += wsum[w];
-    return incl;
-  };
-  int64_t T, t_lo, t_hi;  // straddling: this workgroup's tiles [t_lo, t_hi) of the list
-  int b_first;
-  if constexpr (INL) {
-    const int t = threadIdx.x;
-    DecodeSpan sp{};
-    if (t < a.B) {
-      sp = decode_span(a.mods, a.ctx, max_keys, t);
-      n_s[t] = sp.n, pre_s[t] = sp.pre, lo_s[t] = sp.lo;
-    }
-    int64_t incl = scan((uint32_t)sp.tiles);
+    if (t < a.B) tcs_s[t] = incl - sp.tiles;
     if (t == kWaves * 64 - 1) tcs_s[a.B] = incl;
-    if (!a.aligned && t < a.B) tcs_s[t] = incl - sp.tiles;
     __syncthreads();
-    T = uniform64(tcs_s[a.B]);
-    if (T == 0) return;
-    if (a.aligned) {
-      const int64_t c = piece_tiles(T, a.nwg, a.B, WPH);
-      const uint32_t mine = c < (1 << 30) ? (uint32_t)(sp.tiles + (int)c - 1) / (uint32_t)c : (sp.tiles > 0);
-      incl = scan(mine);
-      // the one sequence whose pieces include this workgroup's
-      __syncthreads();  // (every wave has read T and the scan's sums)
-      if (t == 0) tcs_s[0] = -1;
-      __syncthreads();
-      if (incl - mine <= wgi && wgi < incl) {
-        tcs_s[0] = t;
-        tcs_s[1] = (wgi - (incl - mine)) * c;
-        tcs_s[2] = min((wgi - (incl - mine) + 1) * c, (int64_t)sp.tiles);
-      }
-      __syncthreads();
-      b_first = (int)uniform64(tcs_s[0]);
-      if (b_first < 0) return;  // fewer pieces than workgroups
-      t_lo = uniform64(tcs_s[1]);
-      t_hi = uniform64(tcs_s[2]);
-    } else {
-      t_lo = share(T, wgi, a.nwg), t_hi = share(T, wgi + 1, a.nwg);
-      if (t_lo >= t_hi) return;
-      int lo = 0, hi = a.B;  // largest b with tcs[b] <= t_lo
-      while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (tcs_s[mid] <= t_lo) lo = mid;
-        else hi = mid;
-      }
-      b_first = __builtin_amdgcn_readfirstlane(lo);
+    const int64_t T = uniform64(tcs_s[a.B]);
+    t_lo = share(T, wgi, a.nwg), t_hi = share(T, wgi + 1, a.nwg);
+    if (t_lo >= t_hi) return;
+    int lo = 0, hi = a.B;  // largest b with tcs[b] <= t_lo
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (tcs_s[mid] <= t_lo) lo = mid;
+      else hi = mid;
     }
+    b_first = __builtin_amdgcn_readfirstlane(lo);
   } else {
-    T = uniform64(a.tcs[a.B]);
+    const int64_t T = uniform64(a.tcs[a.B]);
     t_lo = share(T, wgi, a.nwg), t_hi = share(T, wgi + 1, a.nwg);
     if (t_lo >= t_hi) return;
     b_first = __builtin_amdgcn_readfirstlane(a.first_b[wgi]);
@@ -202,17 +214,19 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
   const int g = hg * HB + wave % HB;     // this wave's KV head
   const int wt = wave / HB;              // its share of the head's key tiles
   const int64_t row_elems = (int64_t)a.Hkv * D;
-  const int64_t row_bytes = row_elems * 2;
+  const int64_t row_bytes = row_elems * ES;
   OPS_LDS char* vb = (OPS_LDS char*)vbuf[wave];
-  // this lane's bytes within a tile's first K rows, and within a V load's rows (the
-  // swizzle alternates between two patterns for 256-byte rows)
-  // (below 2^31: 16 rows of at most 65535 heads)
-  const uint32_t k_lane = (uint32_t)(col * row_bytes + ((int64_t)g * D + grp * 8) * 2);
+  // This lane's bytes within 16 K rows, and within the rows of a V load: bf16, by
+  // DMA, rows lane / CPR (the swizzle alternates between two patterns for 256-byte
+  // rows); fp32, rows 4 * grp (+ rr).  Below 2^31: 16 rows of at most 65535 heads.
+  const uint32_t head_at = (uint32_t)(g * D * ES);
+  const uint32_t k_lane = (uint32_t)(col * row_bytes) + head_at + grp * 16;
   uint32_t v_lane[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const int r = lane / CPR;
-    v_lane[i] = (uint32_t)(r * row_bytes + ((int64_t)g * D + ((lane % CPR) ^ v_swz<D>(i * VROWS + r)) * 8) * 2);
+    v_lane[i] = BF16 ? (uint32_t)(r * row_bytes) + head_at + ((lane % CPR) ^ v_swz<D>(i * VROWS + r)) * 16
+                     : (uint32_t)(4 * grp * row_bytes) + head_at + col * 16;
   }
   float slope2 = 0.f;  // of head `col`
   if (a.mods.slopes && col < G) slope2 = a.mods.slopes[g * GH + h0 + col] * kLog2e;
@@ -222,15 +236,14 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
   auto segment = [&](const int b, int k_begin, int k_end, const int k2_begin, const int k2_end, const int n,
                      const int pre, const int lo, const int64_t pslot) {
     // Query heads of this group as the MFMA B operand (column = head).
-    bf16x8 qf[KSTEPS];
+    u32x4 qf[KCH];
     {
-      const bool has = col < G;
-      const __bf16* qrow = a.q + (int64_t)b * a.q_stride + ((int64_t)g * GH + h0 + (has ? col : 0)) * D;
+      const char* qrow = static_cast<const char*>(a.q) +
+                         ((int64_t)b * a.q_stride + ((int64_t)g * GH + h0 + (col < G ? col : 0)) * D) * ES;
 #pragma unroll
-      for (int s = 0; s < KSTEPS; ++s) {
-        u32x4 w = {0u, 0u, 0u, 0u};
-        if (has) w = *reinterpret_cast<const u32x4*>(qrow + s * 32 + grp * 8);
-        qf[s] = __builtin_bit_cast(bf16x8, w);
+      for (int s = 0; s < KCH; ++s) {
+        qf[s] = u32x4{0u, 0u, 0u, 0u};
+        if (col < G) qf[s] = *reinterpret_cast<const u32x4*>(qrow + s * 64 + grp * 16);
       }
     }
     const int32_t* trow = a.table + (int64_t)b * a.max_blocks;
@@ -246,11 +259,13 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
       }
     };
     float m_run = -INFINITY, l_part = 0.f;  // reference of head `col`, this lane's keys' sum
-    f32x4 acc[DT];                          // O[head 4*grp + r][d = 16*dt + col]
+    f32x4 acc[DT];                          // O[head 4*grp + r][column column_of(dt)]
+    auto column_of = [&](int dt) { return BF16 ? 16 * dt + col : 64 * (dt >> 2) + 4 * col + (dt & 3); };
 #pragma unroll
     for (int i = 0; i < DT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-    u32x4 kf[2][KSTEPS];
+    u32x4 kf[2][KCH];
+    f32x4 vf32[BF16 ? 1 : 2][4][BF16 ? 1 : D / 64];  // fp32: V of key 16*sub + 4*grp + rr, columns 64 q + 4 col ..
     // Scores, softmax and P V of the tile at t0; `seen`: bit j for key t0 + j.
     auto compute_tile = [&](const int t0, const uint32_t seen) {
       // scores S^T[key][head]: lane holds head `col`, keys t0 + 16*sub + 4*grp + rr
@@ -259,8 +274,17 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
       for (int sub = 0; sub < 2; ++sub) {
         st[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int s = 0; s < KSTEPS; ++s)
-          st[sub] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[sub][s]), qf[s], st[sub], 0, 0, 0);
+        for (int s = 0; s < KCH; ++s) {
+          if constexpr (BF16) {
+            st[sub] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[sub][s]),
+                                                              __builtin_bit_cast(bf16x8, qf[s]), st[sub], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              st[sub] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[sub][s][e]), __uint_as_float(qf[s][e]),
+                                                             st[sub], 0, 0, 0);
+          }
+        }
       }
       auto each = [&](auto&& f) {
 #pragma unroll
@@ -269,7 +293,12 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
           for (int rr = 0; rr < 4; ++rr) st[sub][rr] = f(st[sub][rr], sub * 16 + rr);
       };
       const uint32_t bits = seen >> (4 * grp);  // bit 16*sub + rr: this lane's keys
-      if (a.mods.softcap > 0.f) {
+      if constexpr (!BF16) {
+        each([&](float x, int) {
+          x *= a.scale;
+          return (a.mods.softcap > 0.f ? a.mods.softcap * tanhf(x / a.mods.softcap) : x) * kLog2e;
+        });
+      } else if (a.mods.softcap > 0.f) {
         float big = 0.f;  // (a key that is not there or masked has no say: its K is zeros, or it counts as 0)
         if (seen != 0xffffffffu) each([&](float x, int j) { return (bits >> j) & 1 ? x : 0.f; });
 #pragma unroll
@@ -301,6 +330,7 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
       }
       const float m_use = m_run == -INFINITY ? 0.f : m_run;
       // P as the MFMA A operand: slot e of lane (col, grp) is key 4*grp + e%4 + 16*(e/4)
+      // (fp32: step rr takes key 4*grp + rr, the value as it lies)
       bf16x8 pa;
       float psum = 0.f;
 #pragma unroll
@@ -309,7 +339,8 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
         for (int rr = 0; rr < 4; ++rr) {
           const float p = fast_exp2(st[sub][rr] - m_use);
           psum += p;
-          pa[sub * 4 + rr] = (__bf16)p;
+          st[sub][rr] = p;
+          if constexpr (BF16) pa[sub * 4 + rr] = (__bf16)p;
         }
       l_part = l_part * alpha + psum;
       // rescale O rows (heads 4*grp + r) when any head's reference moved
@@ -321,18 +352,28 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
           for (int i = 0; i < DT; ++i) acc[i][rr] *= f;
         }
       }
-      // V as the B operand: lane (d = 16*dt + col, group grp) needs keys
-      // 4*grp + e (e < 4) and 16 + 4*grp + (e - 4); one transposed read each.
-      const int trow0 = 4 * grp + (col >> 2);
+      if constexpr (BF16) {
+        // V as the B operand: lane (d = 16*dt + col, group grp) needs keys
+        // 4*grp + e (e < 4) and 16 + 4*grp + (e - 4); one transposed read each.
+        const int trow0 = 4 * grp + (col >> 2);
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        const int cc = dt * 16 + 4 * (col & 3);  // head-dim column of this lane's 8-byte chunk
-        const int c16 = cc >> 3, half = (cc >> 2) & 1;
-        const int r0 = trow0, r1 = trow0 + 16;
-        const u32x2 w0 = lds_read_tr16(vb + r0 * (D * 2) + ((c16 ^ v_swz<D>(r0)) << 4) + half * 8);
-        const u32x2 w1 = lds_read_tr16(vb + r1 * (D * 2) + ((c16 ^ v_swz<D>(r1)) << 4) + half * 8);
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{w0[0], w0[1], w1[0], w1[1]});
-        acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, vf, acc[dt], 0, 0, 0);
+        for (int dt = 0; dt < DT; ++dt) {
+          const int cc = dt * 16 + 4 * (col & 3);  // head-dim column of this lane's 8-byte chunk
+          const int c16 = cc >> 3, half = (cc >> 2) & 1;
+          const int r0 = trow0, r1 = trow0 + 16;
+          const u32x2 w0 = lds_read_tr16(vb + r0 * (D * 2) + ((c16 ^ v_swz<D>(r0)) << 4) + half * 8);
+          const u32x2 w1 = lds_read_tr16(vb + r1 * (D * 2) + ((c16 ^ v_swz<D>(r1)) << 4) + half * 8);
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, u32x4{w0[0], w0[1], w1[0], w1[1]});
+          acc[dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa, vf, acc[dt], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr)
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt)
+              acc[dt] = __builtin_amdgcn_mfma_f32_16x16x4f32(st[sub][rr], vf32[sub][rr][dt >> 2][dt & 3], acc[dt], 0, 0, 0);
       }
     };
     // Each wave loads a tile, waits for it and uses it; latency is hidden by the
@@ -354,12 +395,21 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
           const __amdgpu_buffer_rsrc_t kr = make_rsrc(kc + base, 16 * (uint32_t)row_bytes);
           const __amdgpu_buffer_rsrc_t vr = make_rsrc(vc + base, 16 * (uint32_t)row_bytes);
 #pragma unroll
-          for (int s = 0; s < KSTEPS; ++s)
+          for (int s = 0; s < KCH; ++s)
             kf[sub][s] = __builtin_amdgcn_raw_buffer_load_b128(kr, k_lane + s * 64, 0, 0);
+          if constexpr (BF16) {
 #pragma unroll
-          for (int i = sub * VLOADS / 2; i < (sub + 1) * VLOADS / 2; ++i)
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (OPS_LDS void*)(vb + i * 1024), 16, v_lane[i & 1],
-                                                     (i * VROWS % 16) * (int)row_bytes, 0, kNontemporal);
+            for (int i = sub * VLOADS / 2; i < (sub + 1) * VLOADS / 2; ++i)
+              __builtin_amdgcn_raw_ptr_buffer_load_lds(vr, (OPS_LDS void*)(vb + i * 1024), 16, v_lane[i & 1],
+                                                       (i * VROWS % 16) * (int)row_bytes, 0, kNontemporal);
+          } else {
+#pragma unroll
+            for (int rr = 0; rr < 4; ++rr)
+#pragma unroll
+              for (int q = 0; q < D / 64; ++q)
+                vf32[sub][rr][q] = __builtin_bit_cast(
+                    f32x4, __builtin_amdgcn_raw_buffer_load_b128(vr, v_lane[0] + q * 256, rr * (int)row_bytes, 0));
+          }
         }
       } else {
         auto key_ok = [&](int j) {
@@ -369,7 +419,7 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
           const char* zeros = reinterpret_cast<const char*>(zero_row);
           if (!ok) return zeros;
           const int blk = pages[(j >> a.log2bs) - p_first];
-          return cache + (((int64_t)blk << a.log2bs) + (j & (bs - 1))) * row_bytes + (int64_t)g * D * 2;
+          return cache + (((int64_t)blk << a.log2bs) + (j & (bs - 1))) * row_bytes + head_at;
         };
         seen = 0;
 #pragma unroll
@@ -379,13 +429,25 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
           seen |= (uint32_t)(__builtin_amdgcn_ballot_w64(ok) & 0xffff) << (16 * sub);
           const char* kr = row(kc, j, ok);
 #pragma unroll
-          for (int s = 0; s < KSTEPS; ++s) kf[sub][s] = *reinterpret_cast<const u32x4*>(kr + s * 64 + grp * 16);
+          for (int s = 0; s < KCH; ++s) kf[sub][s] = *reinterpret_cast<const u32x4*>(kr + s * 64 + grp * 16);
         }
+        if constexpr (BF16) {
 #pragma unroll 1
-        for (int i = 0; i < VLOADS; ++i) {
-          const int r = i * VROWS + lane / CPR;
-          const int c = (lane % CPR) ^ v_swz<D>(r);  // logical chunk landing at this lane's slot
-          global_load16_lds_nt(row(vc, t0 + r, (seen >> r) & 1) + c * 16, vb + i * 1024);
+          for (int i = 0; i < VLOADS; ++i) {
+            const int r = i * VROWS + lane / CPR;
+            const int c = (lane % CPR) ^ v_swz<D>(r);  // logical chunk landing at this lane's slot
+            global_load16_lds_nt(row(vc, t0 + r, (seen >> r) & 1) + c * 16, vb + i * 1024);
+          }
+        } else {
+#pragma unroll
+          for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+            for (int rr = 0; rr < 4; ++rr) {
+              const int r = 16 * sub + 4 * grp + rr;
+              const char* vr = row(vc, t0 + r, (seen >> r) & 1) + col * 16;
+#pragma unroll
+              for (int q = 0; q < D / 64; ++q) vf32[sub][rr][q] = *reinterpret_cast<const f32x4*>(vr + q * 256);
+            }
         }
       }
       wait_vmem();
@@ -418,7 +480,7 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
         if (hh < G) {
           const int64_t slot = (int64_t)(g * GH + h0 + hh) * nslots + pslot;
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) a.ws_o[slot * D + dt * 16 + col] = acc[dt][rr];
+          for (int dt = 0; dt < DT; ++dt) a.ws_o[slot * D + column_of(dt)] = acc[dt][rr];
         }
       }
       if (col < G && grp == 0) {
@@ -435,35 +497,36 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
         const int hh = 4 * grp + rr;
         if (hh < G)
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) mine[hh * D + dt * 16 + col] = acc[dt][rr];
+          for (int dt = 0; dt < DT; ++dt) mine[hh * D + column_of(dt)] = acc[dt][rr];
       }
       if (grp == 0) {
         ml_s[wave][col][0] = m_run;
         ml_s[wave][col][1] = l_run;
       }
       __syncthreads();
-      // a thread keeps its column and walks the HB * G heads
+      // a thread keeps its column and takes every STEP-th query head of each KV head
       constexpr int STEP = kWaves * 64 / D;
       const int d = threadIdx.x % D;
-      for (int r = threadIdx.x / D; r < HB * 16; r += STEP) {
-        const int hl = r >> 4, hh = r & 15;  // head slot, query head
-        if (hh >= G) continue;
-        float M = -INFINITY;
+      for (int hh = threadIdx.x / D; hh < G; hh += STEP) {
 #pragma unroll
-        for (int w = 0; w < WPH; ++w) M = fmaxf(M, ml_s[w * HB + hl][hh][0]);
-        float o = 0.f, l = 0.f;
+        for (int hl = 0; hl < HB; ++hl) {
+          float M = -INFINITY;
 #pragma unroll
-        for (int w = 0; w < WPH; ++w) {
-          const float* e = ml_s[w * HB + hl][hh];
-          const float f = e[0] == -INFINITY ? 0.f : fast_exp2(e[0] - M);
-          o += f * reinterpret_cast<const float*>(vbuf[w * HB + hl])[hh * D + d];
-          l += f * e[1];
-        }
-        const int64_t slot = (int64_t)((hg * HB + hl) * GH + h0 + hh) * nslots + pslot;
-        a.ws_o[slot * D + d] = o;
-        if (d == 0) {
-          a.ws_ml[slot * 2 + 0] = M;
-          a.ws_ml[slot * 2 + 1] = l;
+          for (int w = 0; w < WPH; ++w) M = fmaxf(M, ml_s[w * HB + hl][hh][0]);
+          float o = 0.f, l = 0.f;
+#pragma unroll
+          for (int w = 0; w < WPH; ++w) {
+            const float* e = ml_s[w * HB + hl][hh];
+            const float f = e[0] == -INFINITY ? 0.f : fast_exp2(e[0] - M);
+            o += f * reinterpret_cast<const float*>(vbuf[w * HB + hl])[hh * D + d];
+            l += f * e[1];
+          }
+          const int64_t slot = (int64_t)((hg * HB + hl) * GH + h0 + hh) * nslots + pslot;
+          a.ws_o[slot * D + d] = o;
+          if (d == 0) {
+            a.ws_ml[slot * 2 + 0] = M;
+            a.ws_ml[slot * 2 + 1] = l;
+          }
         }
       }
     }
@@ -471,11 +534,14 @@ __global__ __launch_bounds__(512, 4) void attn_decode_mod_kernel(const DecodeArg
 
   auto run = [&](int b, int64_t v0, int64_t v1, int64_t pslot) {  // tiles [v0, v1) of sequence b
     DecodeSpan s;
-    if constexpr (INL)
-      s = make_span(__builtin_amdgcn_readfirstlane(n_s[b]), __builtin_amdgcn_readfirstlane(pre_s[b]),
-                    __builtin_amdgcn_readfirstlane(lo_s[b]));
-    else
+    if constexpr (INL) {
+      const bool own = a.aligned;
+      s = make_span(own ? own_n : __builtin_amdgcn_readfirstlane(n_s[b]),
+                    own ? own_pre : __builtin_amdgcn_readfirstlane(pre_s[b]),
+                    own ? own_lo : __builtin_amdgcn_readfirstlane(lo_s[b]));
+    } else {
       s = decode_span(a.mods, a.ctx, max_keys, __builtin_amdgcn_readfirstlane(b));
+    }
     const int shift = s.first_tile - s.pre_tiles, x0 = (int)v0, x1 = (int)v1;
     segment(b, min(x0, s.pre_tiles) * kTile, min(min(x1, s.pre_tiles) * kTile, s.n),
             (max(x0, s.pre_tiles) + shift) * kTile, min((max(x1, s.pre_tiles) + shift) * kTile, s.n), s.n, s.pre, s.lo,
@@ -540,15 +606,15 @@ __global__ __launch_bounds__(1024) void attn_decode_mod_plan_kernel(const Decode
 // weights 64 at a time across the lanes.  The plan is built again from the lengths
 // (INL): they are cached, what the first kernel's workgroups would have written
 // lies in other XCDs' caches.
-template <int D, bool INL, int W>
-__global__ __launch_bounds__(64 * W) void attn_decode_mod_combine_kernel(const DecodeArgs a, __bf16* __restrict__ o,
-                                                                         int Hq, int waves) {
-  constexpr int DPL = D / 64, kOwn = 64 / W;
+template <class OUT, int D, bool INL, int W>
+__global__ __launch_bounds__(64 * W) void attn_decode_mod_combine_kernel(const DecodeArgs a, OUT* __restrict__ o, int Hq,
+                                                                         int waves) {
+  constexpr int DPL = D / 64, kOwn = 64 / W, kRows = W > 1 ? kOwn : 8;  // rows requested at once
   __shared__ float fw_all[W][64];
   const int h = blockIdx.x, b = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int max_keys = a.max_blocks << a.log2bs;
   float* fw = fw_all[wave];  // (every wave computes all the weights, for the sum and its own rows)
-  __bf16* orow = o + ((int64_t)b * Hq + h) * D;
+  OUT* orow = o + ((int64_t)b * Hq + h) * D;
   int64_t T, ft, lt;  // tiles in all; this sequence's first and last
   int64_t s0;         // first slot
   int S;              // slots
@@ -586,7 +652,7 @@ __global__ __launch_bounds__(64 * W) void attn_decode_mod_combine_kernel(const D
   if (lt < ft) {  // no key seen: a zero row
     if (wave == 0)
 #pragma unroll
-      for (int c = 0; c < DPL; ++c) orow[lane + c * 64] = (__bf16)0.f;
+      for (int c = 0; c < DPL; ++c) orow[lane + c * 64] = (OUT)0.f;
     return;
   }
   int g0 = 0;
@@ -628,17 +694,17 @@ __global__ __launch_bounds__(64 * W) void attn_decode_mod_combine_kernel(const D
     }
     fw[lane] = f;
     __builtin_amdgcn_wave_barrier();
-    // this wave's rows, eight requested at a time without waiting for the weights; rows of
+    // this wave's rows, kRows requested at a time without waiting for the weights; rows of
     // dead slots are dropped by the select
     const int end = min(kOwn * (wave + 1), S - i0);
-    for (int j = kOwn * wave; j < end; j += 8) {
-      float v[8][DPL];
+    for (int j = kOwn * wave; j < end; j += kRows) {
+      float v[kRows][DPL];
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+      for (int u = 0; u < kRows; ++u)
 #pragma unroll
         for (int c = 0; c < DPL; ++c) v[u][c] = a.ws_o[(base + i0 + min(j + u, end - 1)) * D + lane + c * 64];
 #pragma unroll
-      for (int u = 0; u < 8; ++u) {
+      for (int u = 0; u < kRows; ++u) {
         const float fj = j + u < end ? fw[j + u] : 0.f;
 #pragma unroll
         for (int c = 0; c < DPL; ++c) acc[c] += fj == 0.f ? 0.f : fj * v[u][c];
@@ -661,87 +727,7 @@ __global__ __launch_bounds__(64 * W) void attn_decode_mod_combine_kernel(const D
       for (int c = 0; c < DPL; ++c) acc[c] += part[w][lane + c * 64];
   }
 #pragma unroll
-  for (int c = 0; c < DPL; ++c) orow[lane + c * 64] = (__bf16)(acc[c] * inv);
-}
-
-// fp32: a workgroup of sixteen waves per (query head, sequence).  A 16-lane row takes a key:
-// each lane D / 16 of its elements, so K and V rows arrive as whole lines, the
-// score is four DPP steps, and the row keeps a running softmax of its own with its
-// D / 16 output columns a lane.  64 keys are under way at once, kAhead of a row
-// requested together; the 64 partial results are merged through LDS in row order.
-// What bounds a small call is the chain of those loads (one sequence of 700 keys, 8
-// heads of 128, one KV head: 22 dependent steps of 32 keys took 17.7 us, three
-// of 256 __F32__).  It uses no workspace.
-template <int D>
-__global__ __launch_bounds__(1024) void attn_decode_mod_f32_kernel(
-    const float* __restrict__ q, int64_t q_stride, const float* __restrict__ kc, const float* __restrict__ vc,
-    const int32_t* __restrict__ table, const int32_t* __restrict__ ctx, float* __restrict__ o, int Hq, int Hkv,
-    int log2bs, int max_blocks, int64_t num_blocks, float scale, const AttnMods mods) {
-  constexpr int EPL = D / 16, kRows = 64, kAhead = D == 128 ? 4 : 8;
-  using V = float __attribute__((ext_vector_type(EPL)));
-  __shared__ __attribute__((aligned(16))) float part[kRows][D];
-  __shared__ float ms[kRows], ls[kRows];
-  const int h = blockIdx.x, b = blockIdx.y, col = threadIdx.x & 15, row = threadIdx.x >> 4;
-  const int g = h / (Hq / Hkv), bs = 1 << log2bs;
-  const DecodeSpan span = decode_span(mods, ctx, max_blocks << log2bs, b);
-  const int32_t* trow = table + (int64_t)b * max_blocks;
-  const float slope = mods.slopes ? mods.slopes[h] : 0.f;
-  const V qv = *reinterpret_cast<const V*>(q + (int64_t)b * q_stride + (int64_t)h * D + col * EPL);
-  float m_run = -INFINITY, l_run = 0.f;
-  V acc = {};
-  // keys [0, pre), then [max(lo, pre), n), numbered through
-  const int first = max(span.lo, span.pre), count = span.pre + max(0, span.n - first);
-  for (int i0 = row; i0 < count; i0 += kRows * kAhead) {
-    V kv[kAhead], vv[kAhead];
-    int key[kAhead];  // -1: none
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      const int i = i0 + a * kRows, j = i < span.pre ? i : i - span.pre + first;
-      const int blk = i < count ? trow[j >> log2bs] : -1;
-      key[a] = (uint32_t)blk < (uint64_t)num_blocks ? j : -1;
-      kv[a] = V{}, vv[a] = V{};
-      if (key[a] >= 0) {
-        const int64_t at = (((int64_t)blk * bs + (j & (bs - 1))) * Hkv + g) * D + col * EPL;
-        kv[a] = *reinterpret_cast<const V*>(kc + at);
-        vv[a] = *reinterpret_cast<const V*>(vc + at);
-      }
-    }
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a) {
-      float x = 0.f;
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) x = fmaf(qv[e], kv[a][e], x);
-      x += dpp_f<0xB1>(x);
-      x += dpp_f<0x4E>(x);
-      x += dpp_f<0x141>(x);
-      x += dpp_f<0x140>(x);
-      if (key[a] < 0) continue;  // (all lanes of the row)
-      x = mods.score(x * scale, slope, (float)(span.n - 1 - key[a]));
-      const float m_new = fmaxf(m_run, x), m_use = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = expf(m_run - m_use), p = expf(x - m_use);
-      l_run = fmaf(l_run, alpha, p);
-      m_run = m_new;
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) acc[e] = fmaf(p, vv[a][e], acc[e] * alpha);
-    }
-  }
-  *reinterpret_cast<V*>(&part[row][col * EPL]) = acc;
-  if (col == 0) {
-    ms[row] = m_run;
-    ls[row] = l_run;
-  }
-  __syncthreads();
-  if (threadIdx.x < D) {
-    float m = -INFINITY, l = 0.f, sum = 0.f;
-    for (int r = 0; r < kRows; ++r) m = fmaxf(m, ms[r]);
-    for (int r = 0; r < kRows; ++r) {
-      if (ms[r] == -INFINITY && ls[r] == 0.f) continue;  // (a row without keys)
-      const float f = expf(ms[r] - (m == -INFINITY ? 0.f : m));
-      l = fmaf(f, ls[r], l);
-      sum = fmaf(f, part[r][threadIdx.x], sum);
-    }
-    o[((int64_t)b * Hq + h) * D + threadIdx.x] = l == 0.f ? 0.f : sum / l;
-  }
+  for (int c = 0; c < DPL; ++c) orow[lane + c * 64] = (OUT)(acc[c] * inv);
 }
 
 // Workgroups per head group: as the plain operator's (at most one a CU, 64 a
@@ -754,13 +740,13 @@ static int32_t mod_workgroups(int32_t B, int32_t max_context_len, int32_t window
   const int64_t most = std::max(1, kMaxWorkgroups / std::max(1, groups));
   const int64_t tiles = b * per_seq;
   const int64_t cap = tiles <= 2 * waves * most ? 2 * most : most;
-  return (int32_t)std::min<int64_t>(cap, std::min<int64_t>(tiles, b * kSeqWorkgroups) + b);
+  return (int32_t)std::min<int64_t>(cap, std::min<int64_t>(tiles, b * (cap / most) * kSeqWorkgroups) + b);
 }
 
 size_t decode_mod_workspace_bytes(int32_t B, int32_t Hq, int32_t D, int32_t max_context_len) {
   // (whatever the window and the groups: at most twice kMaxWorkgroups)
   const int64_t b = std::max(1, B), tiles = b * ((std::max(1, max_context_len) + (int64_t)kTile - 1) / kTile);
-  const int64_t nwg = std::min<int64_t>(2 * kMaxWorkgroups, std::min<int64_t>(tiles, b * kSeqWorkgroups) + b);
+  const int64_t nwg = std::min<int64_t>(2 * kMaxWorkgroups, std::min<int64_t>(tiles, 2 * b * kSeqWorkgroups) + b);
   return decode_ws(nullptr, B, Hq, D, (int32_t)nwg).bytes;
 }
 
@@ -772,65 +758,65 @@ hipError_t launch_attn_decode_mod(const void* q, int64_t q_stride, const void* k
   int log2bs = 0;
   while ((1 << log2bs) < block_size) ++log2bs;
   const AttnMods mods = make_attn_mods(m, scale);
-  if (!bf16) {
-    const auto kern = D == 128 ? &attn_decode_mod_f32_kernel<128> : &attn_decode_mod_f32_kernel<64>;
-    hipLaunchKernelGGL(kern, dim3((unsigned)Hq, (unsigned)B), dim3(1024), 0, s, static_cast<const float*>(q), q_stride,
-                       static_cast<const float*>(kcache), static_cast<const float*>(vcache), table, ctx,
-                       static_cast<float*>(o), Hq, Hkv, log2bs, max_blocks, num_blocks, scale, mods);
-    return hipGetLastError();
-  }
   const int HB = decode_heads_per_workgroup(Hkv), G = Hq / Hkv, blocks = (G + 15) / 16;
   const int nwg = mod_workgroups(B, max_context_len, mods.window, Hkv / HB * blocks, kWaves / HB);
   const DecodeWs w = decode_ws(ws, B, Hq, D, nwg);
   DecodeArgs a{};
-  a.q = static_cast<const __bf16*>(q), a.kc = static_cast<const __bf16*>(kcache);
-  a.vc = static_cast<const __bf16*>(vcache);
-  a.q_stride = q_stride, a.table = table, a.ctx = ctx, a.Hkv = Hkv, a.GH = G;
+  a.q = q, a.kc = kcache, a.vc = vcache, a.q_stride = q_stride, a.table = table, a.ctx = ctx, a.Hkv = Hkv, a.GH = G;
   a.log2bs = log2bs, a.max_blocks = max_blocks, a.num_blocks = num_blocks;
-  a.tcs = w.tcs, a.first_b = w.first, a.B = B, a.nwg = nwg, a.aligned = B <= kInlineB && nwg >= 2 * B;
-  a.scale_log2 = scale * kLog2e, a.ws_o = w.o, a.ws_ml = w.ml, a.mods = mods;
+  a.tcs = w.tcs, a.first_b = w.first, a.B = B, a.nwg = nwg, a.aligned = B <= 64 && nwg >= 2 * B;
+  a.scale = scale, a.scale_log2 = scale * kLog2e, a.ws_o = w.o, a.ws_ml = w.ml, a.mods = mods;
   if (B > kInlineB) {
     hipLaunchKernelGGL(attn_decode_mod_plan_kernel, dim3(1), dim3(1024), 0, s, a, w.tcs, w.first);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   const dim3 grid((unsigned)nwg, (unsigned)(Hkv / HB), (unsigned)blocks);
-#define OPS_DEC(DD, HH)                                                                                       \
-  if (B <= kInlineB)                                                                                          \
-    hipLaunchKernelGGL((attn_decode_mod_kernel<DD, HH, true>), grid, dim3(kWaves * 64), 0, s, a);             \
-  else                                                                                                        \
-    hipLaunchKernelGGL((attn_decode_mod_kernel<DD, HH, false>), grid, dim3(kWaves * 64), 0, s, a);            \
+#define OPS_DEC_I(TT, DD, HH, II) \
+  hipLaunchKernelGGL((attn_decode_mod_kernel<TT, DD, HH, II>), grid, dim3(kWaves * 64), 0, s, a)
+#define OPS_DEC(TT, DD, HH)                           \
+  if (B <= kInlineB) OPS_DEC_I(TT, DD, HH, true);     \
+  else OPS_DEC_I(TT, DD, HH, false);                  \
   break
-#define OPS_DEC_H(DD)             \
-  switch (HB) {                   \
-    case 1: OPS_DEC(DD, 1);       \
-    case 2: OPS_DEC(DD, 2);       \
-    case 4: OPS_DEC(DD, 4);       \
-    default: OPS_DEC(DD, 8);      \
+#define OPS_DEC_H(TT, DD)             \
+  switch (HB) {                       \
+    case 1: OPS_DEC(TT, DD, 1);       \
+    case 2: OPS_DEC(TT, DD, 2);       \
+    case 4: OPS_DEC(TT, DD, 4);       \
+    default: OPS_DEC(TT, DD, 8);      \
   }
-  if (D == 128) {
-    OPS_DEC_H(128)
+  if (bf16 && D == 128) {
+    OPS_DEC_H(true, 128)
+  } else if (bf16) {
+    OPS_DEC_H(true, 64)
+  } else if (D == 128) {
+    OPS_DEC_H(false, 128)
   } else {
-    OPS_DEC_H(64)
+    OPS_DEC_H(false, 64)
   }
 #undef OPS_DEC_H
 #undef OPS_DEC
+#undef OPS_DEC_I
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   // (four waves past 16 segments a sequence, as the plain operator's merge)
   const bool many = nwg > 16 * B;
   const dim3 cgrid((unsigned)Hq, (unsigned)B);
-  __bf16* ob = static_cast<__bf16*>(o);
-#define OPS_COMB_W(DD, II, WW) \
-  hipLaunchKernelGGL((attn_decode_mod_combine_kernel<DD, II, WW>), cgrid, dim3(64 * WW), 0, s, a, ob, Hq, kWaves / HB)
-#define OPS_COMB(DD)                                  \
-  if (B > kInlineB) OPS_COMB_W(DD, false, 1);         \
-  else if (many) OPS_COMB_W(DD, true, 4);             \
-  else OPS_COMB_W(DD, true, 1)
-  if (D == 128) {
-    OPS_COMB(128);
+#define OPS_COMB_W(TT, DD, II, WW)                                                                               \
+  hipLaunchKernelGGL((attn_decode_mod_combine_kernel<TT, DD, II, WW>), cgrid, dim3(64 * WW), 0, s, a,            \
+                     static_cast<TT*>(o), Hq, kWaves / HB)
+#define OPS_COMB(TT, DD)                                  \
+  if (B > kInlineB) OPS_COMB_W(TT, DD, false, 1);         \
+  else if (many) OPS_COMB_W(TT, DD, true, 4);             \
+  else OPS_COMB_W(TT, DD, true, 1)
+  if (bf16 && D == 128) {
+    OPS_COMB(__bf16, 128);
+  } else if (bf16) {
+    OPS_COMB(__bf16, 64);
+  } else if (D == 128) {
+    OPS_COMB(float, 128);
   } else {
-    OPS_COMB(64);
+    OPS_COMB(float, 64);
   }
 #undef OPS_COMB_W
 #undef OPS_COMB
