@@ -28,7 +28,7 @@ namespace opscale {
 //    subtraction is the polynomial's last step.
 //  * The bias adds slope * (j - i) along the keys, three steps from a group's first.
 //  * A masked key's probability is 0, but 0 times an infinity or NaN in its V row
-//    is not: a masked tile whose V holds one is summed key by key.
+//    is not: see special.
 template <int D, bool LIST, int MODE>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
     const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
@@ -71,15 +71,19 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
     const int pre = mods.prefix ? min(max(__builtin_amdgcn_readfirstlane(mods.prefix[b]), 0), L) : 0;
     const int win = mods.window == 0 ? L : min(mods.window, L);  // (a window of L reaches every key)
     const int q_last = min(L, q_lo + 32) - 1;                    // the wave's last query (may be before q_lo)
-    int s_min = 0, s_max = 0, start = 0, blk_s_min = 0;
+    int s_min = 0, s_max = 0, start = 0, blk_s_min = 0, blk_s_max = 0;
     if (mods.starts) {
       const int32_t* st0 = mods.starts + seq0;
       start = max(st0[min(q_pos, L - 1)], 0);
       s_min = -wave_max_i(-start);  // (the queries past the prompt repeat its last one)
       s_max = wave_max_i(start);
-      int m = INT32_MAX;
-      for (int r = lane; r < BQ; r += 64) m = min(m, max(st0[min(t * BQ + r, L - 1)], 0));
-      blk_s_min = -wave_max_i(-m);
+      int lo = INT32_MAX, hi = 0;
+      for (int r = lane; r < BQ; r += 64) {
+        const int v = max(st0[min(t * BQ + r, L - 1)], 0);
+        lo = min(lo, v), hi = max(hi, v);
+      }
+      blk_s_min = -wave_max_i(-lo);
+      blk_s_max = wave_max_i(hi);
     }
     const int own_lo = max(start, q_pos - win + 1);
     const int own_hi = causal ? min(q_pos, L - 1) : min(L - 1, q_pos + win - 1);
@@ -87,7 +91,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
     const int wave_lo_max = max(s_max, q_last - win + 1);
     const int wave_hi_min = causal ? q_lo : min(L - 1, q_lo + win - 1);
     const int wave_hi_max = causal ? q_last : min(L - 1, q_last + win - 1);
-    const int blk_lo = max(blk_s_min, max(0, t * BQ - win + 1));
+    const int blk_lo = max(blk_s_min, max(0, t * BQ - win + 1)), blk_lo_max = max(blk_s_max, blk_q_hi - win);
+    const int blk_hi_min = causal ? t * BQ : min(L - 1, t * BQ + win - 1);
     const int own_end = causal ? blk_q_hi : min(L, blk_q_hi - 1 + win);
     const int pre_tiles = (pre + kBKV - 1) / kBKV;
     const int first_tile = max(blk_lo / kBKV, pre_tiles);
@@ -143,11 +148,45 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
       wait_vmem();
       __syncthreads();
       if (it + 1 < nkv) load_kv(tile_at(it + 1) * kBKV, (it + 1) & 1);
-      const OPS_LDS char* ks = smem + (it & 1) * S::kStage;
-      const OPS_LDS char* vs = ks + S::kTileBytes;
       // Skip tiles that none of this wave's queries sees into.
       const bool active = q_lo < L && (kv0 < pre || (kv0 <= wave_hi_max && kv0 + kBKV - 1 >= wave_lo_min));
-      if (!active) continue;
+      const OPS_LDS char* ks = smem + (it & 1) * S::kStage;
+      OPS_LDS char* vs = smem + (it & 1) * S::kStage + S::kTileBytes;
+      // A masked key's probability is 0, but its product with an infinity or NaN in V is
+      // not.  So where a tile that some query of the workgroup does not see whole
+      // holds such elements, the waves first add them for the queries that see them,
+      // then put zeros in their place.  (Every way round the loop ends in P V: a
+      // way past it for such tiles, to sum them otherwise, kept two copies of the
+      // accumulators, 64 register moves a tile.)  The same on every wave:
+      auto special = [&] {
+        if (kv0 + kBKV <= pre || (kv0 >= blk_lo_max && kv0 + kBKV - 1 <= blk_hi_min)) return false;
+        uint32_t top = 0;
+#pragma unroll 4
+        for (int i = 0; i < kBKV * CPR / 64; ++i) {
+          const u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) top = max(top, max((w[c] & 0x7fffu) << 16, w[c] & 0x7fff0000u));
+        }
+        return __builtin_amdgcn_ballot_w64(top >= 0x7f800000u) != 0;
+      };
+      auto clear_special = [&] {  // (a quarter of the tile a wave)
+        __syncthreads();
+#pragma unroll 1
+        for (int i = wave; i < kBKV * CPR / 64; i += 4) {
+          u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            if ((w[c] & 0x7f80u) == 0x7f80u) w[c] &= 0xffff0000u;
+            if ((w[c] & 0x7f800000u) == 0x7f800000u) w[c] &= 0xffffu;
+          }
+          *reinterpret_cast<OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16) = w;
+        }
+        __syncthreads();
+      };
+      if (!active) {
+        if (special()) clear_special();
+        continue;
+      }
       f32x16 st[2];
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb) {
@@ -254,48 +293,27 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
         return u32x4{lo[0], lo[1], hi[0], hi[1]};
       };
       auto as_bf16 = [](const u32x4& w) { return __builtin_bit_cast(bf16x8, w); };
-      bool special = false;  // an infinity or NaN in a masked tile's V
-      if (masked) {
-        uint32_t top = 0;
-#pragma unroll 4
-        for (int i = 0; i < kBKV * CPR / 64; ++i) {
-          const u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) top = max(top, max((w[c] & 0x7fffu) << 16, w[c] & 0x7fff0000u));
-        }
-        special = __builtin_amdgcn_ballot_w64(top >= 0x7f800000u) != 0;
-      }
-      if (special) {
-        // key by key, for the queries that see it: the score again, from the
-        // query's two halves (fh), then V's row
+      if (special()) {
+        // the special elements, for the queries that see them
 #pragma unroll 1
         for (int key = 0; key < kBKV; ++key) {
-          float x = 0.f;
+          const OPS_LDS char* row = vs + key * S::kRowBytes;
+          const u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(row + (lane % CPR) * 16);
+          uint32_t top = 0;
 #pragma unroll
-          for (int s = 0; s < DSTEPS; ++s) {
-            const bf16x8 kf = *reinterpret_cast<const OPS_LDS bf16x8*>(
-                ks + key * S::kRowBytes + (((2 * s + fh) ^ k_swz<D>(key)) << 4));
-            u32x4 qw = __builtin_bit_cast(u32x4, qf[s]);
-            asm("" : "+v"(qw));  // (converted here: as floats before the loop they would take 8 DSTEPS registers)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x = fmaf((float)kf[e], (float)__builtin_bit_cast(bf16x8, qw)[e], x);
-          }
-          x += other_half(x);
+          for (int c = 0; c < 4; ++c) top = max(top, max((w[c] & 0x7fffu) << 16, w[c] & 0x7fff0000u));
+          if (__builtin_amdgcn_ballot_w64(top >= 0x7f800000u) == 0) continue;
           const int j = kv0 + key;
-          if constexpr (CAP) x = fabsf(x) <= mods.cap_bound ? mods.capped_small(x, 0.f) : mods.capped(x, 0.f);
-          else x *= scale_log2;
-          if constexpr (BIAS) x = fmaf(-slope2, fabsf((float)(j - q_pos)), x);
-          if (!(j < pre || (j >= own_lo && j <= own_hi))) continue;
-          const float p = (float)(__bf16)fast_exp2(x - (m_run == -INFINITY ? 0.f : m_run));
+          const bool see = j < pre || (j >= own_lo && j <= own_hi);
 #pragma unroll
           for (int i = 0; i < DT * 4; ++i) {  // columns 8 i + 4 fh .. + 3
-            const bf16x4 w = *reinterpret_cast<const OPS_LDS bf16x4*>(vs + key * S::kRowBytes +
-                                                                      ((i ^ v_swz<D>(key)) << 4) + fh * 8);
+            const bf16x4 x = *reinterpret_cast<const OPS_LDS bf16x4*>(row + ((i ^ v_swz<D>(key)) << 4) + fh * 8);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i >> 2][(i & 3) * 4 + e] = fmaf(p, (float)w[e], acc[i >> 2][(i & 3) * 4 + e]);
+            for (int e = 0; e < 4; ++e)
+              acc[i >> 2][(i & 3) * 4 + e] += see && !(fabsf((float)x[e]) < INFINITY) ? (float)x[e] : 0.f;
           }
         }
-        continue;
+        clear_special();
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
