@@ -4,8 +4,9 @@
 //
 // Two prefix sums over the requests (new tokens, then pages taken) and two
 // expansions (a position and a slot a token, a table entry a page).  The bytes
-// are few; what bounds it is the chain of launch, lengths, scan and stores, so
-// it is one launch without a workspace: workgroup (x, y) owns requests 256 x
+// are few; what bounds it is the chain of launch, lengths, scan and stores (256
+// requests of one token 3.5 us, of which an empty launch is 3.2), so it is one
+// launch without a workspace: workgroup (x, y) owns requests 256 x
 // .. 256 x + 255, sums the lengths before them itself (256 a step, from L2) and
 // scans its own in LDS; the tokens and pages of a group are dealt over its y
 // workgroups, each element finding its request by bisection in LDS (8 steps).
@@ -157,8 +158,9 @@ hipError_t launch_block_tables(const int32_t* ctx, const int32_t* fresh, int32_t
   int log2bs = 0;
   while ((1 << log2bs) < block_size) ++log2bs;
   const int64_t gx = std::max<int64_t>(1, (B + kGroup - 1) / kGroup);
-  // about four tokens a thread, up to four workgroups a CU
-  const int64_t gy = std::max<int64_t>(1, std::min<int64_t>(max_tokens / (4 * kGroup * gx), 1024 / gx));
+  // about two tokens a thread, up to four workgroups a CU (1024 prompts, 199k
+  // tokens: 6.8 us; one token a thread 7.0, four 7.8, eight 9.9)
+  const int64_t gy = std::max<int64_t>(1, std::min<int64_t>(max_tokens / (2 * kGroup * gx), 1024 / gx));
   hipLaunchKernelGGL(block_tables_kernel, dim3((unsigned)gx, (unsigned)gy), dim3(kGroup), 0, s, ctx, fresh, B, table,
                      max_blocks, log2bs, free_blocks, num_free, free_begin, max_tokens, cu, positions, slots, kv_lens,
                      free_next);

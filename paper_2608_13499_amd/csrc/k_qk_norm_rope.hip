@@ -14,6 +14,7 @@
 // product and reduction, fp32 sine and cosine) into LDS, where every head reads
 // it.  The norm's gains sit in registers: a thread's place in its head is the same
 // in every pass.
+#include <algorithm>
 #include <type_traits>
 
 #include "common.h"
@@ -25,7 +26,7 @@ namespace opscale {
 namespace {
 
 constexpr double kTwoPi = 6.283185307179586476925286766559;
-constexpr int kMaxTpw = 4;   // tokens of a workgroup
+constexpr int kMaxTpw = 8;   // tokens of a workgroup
 constexpr int kMaxRot = 256;
 
 // Sum over aligned groups of L lanes (L a power of two up to 16).
@@ -231,8 +232,14 @@ hipError_t launch_qk_norm_rope(const QkNormRope& p, bool bf16, hipStream_t s) {
   a.Hq = p.Hq, a.Hkv = p.Hkv, a.D = p.D, a.rot = p.rot;
   a.heads = p.Hq + p.Hkv + (p.k_cache ? p.Hkv : 0);
   a.eps = p.eps, a.magnitude = p.magnitude;
-  a.tpw = p.T >= 4 * 256 ? kMaxTpw : 1;
   const int lanes = p.D <= 32 ? 2 : p.D <= 64 ? 4 : p.D <= 128 ? 8 : 16;
+  // As many tokens as a workgroup holds in one pass of its threads, as long as
+  // every CU keeps four workgroups.  Bf16, in place, rule / one token each:
+  //   65536 tokens of 2 + 1 heads of 64: 19 / 79 us; 8192: 4.1 / 12 us
+  //   16384 tokens of 4 + 2 heads of 64:  8 / 23 us
+  // More tokens than one pass only cost: 8871 of 64 + 8 heads of 128 with their
+  // cache take 69 us with one each, 74 with two and 79 with four.
+  a.tpw = (int)std::max<int64_t>(1, std::min<int64_t>({kMaxTpw, 256 / (lanes * a.heads), p.T / 1024}));
 #define OPS_QK_L(B, L, N, H) hipLaunchKernelGGL((qk_norm_rope_kernel<B, L, N, H>), dim3(grid), dim3(256), 0, s, a)
 #define OPS_QK_N(B, N, H)                  \
   switch (lanes) {                         \

@@ -109,7 +109,8 @@ def test_qk_norm_rope_layouts(ops, dtype, inter, D, rot):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("T,Hq,Hkv", [(1, 1, 1), (1, 32, 8), (2, 71, 1), (7, 28, 4), (33, 64, 64), (1021, 3, 1),
-                                      (1024, 5, 5), (1027, 8, 2), (2051, 12, 4)])
+                                      (1024, 5, 5), (1027, 8, 2), (2051, 12, 4),
+                                      (4099, 2, 2), (8201, 2, 1)])
 def test_qk_norm_rope_sizes(ops, dtype, T, Hq, Hkv):
     _run_heads(ops, dtype, T, Hq, Hkv, 64, 64, T % 2 == 1, False, "ramp", in_place=T % 3 == 0, cache=16)
 
