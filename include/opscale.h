@@ -425,10 +425,10 @@ size_t opscale_attn_decode_mod_workspace_size(int32_t B, int32_t Hq, int32_t D, 
 
 /*
  * opscale_attn_decode with score modifiers and masks (its arguments, layouts and
- * conditions, but both paths need the workspace; mods NULL: none; o and the workspace
- * overlap nothing else), the query
- * of sequence b at position context_lens[b] - 1.  Only 32-key tiles that hold a
- * visible key are read.  Any Hq / Hkv on both paths.
+ * conditions, but both paths need the workspace, max_blocks_per_seq * block_size is
+ * at most 2^31 - 1024, and o and the workspace overlap nothing else; mods NULL:
+ * none), the query of sequence b at position context_lens[b] - 1.  Only 32-key tiles
+ * that hold a visible key are read.  Any Hq / Hkv on both paths.
  */
 opscale_status opscale_attn_decode_mod(const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache,
                                        const int32_t* block_table, const int32_t* context_lens, void* o, int32_t B,

@@ -414,8 +414,9 @@ opscale_status check_decode_mod(const void* q, int64_t qs, const void* kc, const
   if (st == OPSCALE_OK) st = check_mods("attn_decode_mod", m);
   if (st != OPSCALE_OK || B == 0) return st;
   const int s = esize(dt);
-  if (num_blocks > ((int64_t)1 << 31) || num_blocks * bs > ((int64_t)1 << 40))
-    return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: num_blocks=%lld (page ids are int32)", (long long)num_blocks);
+  if ((int64_t)max_blocks * bs > kMaxDim - 1024 || num_blocks > kMaxDim || num_blocks * bs > ((int64_t)1 << 36))
+    return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: max_blocks_per_seq=%d num_blocks=%lld of %d (at most 2^31 - 1024 "
+                "keys a sequence, 2^31 blocks and 2^36 slots)", max_blocks, (long long)num_blocks, bs);
   struct Range {
     const void* p;
     int64_t n;

@@ -278,6 +278,31 @@ def test_prefill_offsets_past_32_bits(ops):
         assert np.abs(got[t, h] - r).max() <= 2.0 ** -6 * np.abs(r).max()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_prefill_prompts_past_one_grid(ops, dtype):
+    """More prompts than a launch has workgroups, nearly all of them empty."""
+    import torch
+    B, D = (1 << 24) + 300, 64
+    say(f"attn_prefill_mod {dtype}: {B} prompts")
+    lens = np.zeros(B, np.int64)
+    at = [0, 1, 5000, (1 << 24) - 2, (1 << 24) - 1, 1 << 24, B - 1]
+    lens[at] = [3, 40, 1, 33, 65, 70, 7]
+    cu, T = wl.cu_seqlens(lens), int(lens.sum())
+    x = gen(63, "q", (T, 3 * D), dtype, 1.5)
+    q, k, v = (cuda(x)[:, i * D:(i + 1) * D].unflatten(1, (1, D)) for i in range(3))
+    prefix = np.zeros(B, np.int64)
+    prefix[at] = [2, 0, 1, 20, 64, 1, 7]
+    kw = dict(softcap=5.0, window=9)
+    out = ops.opscale_attn_prefill_mod(q, k, v, i32(cu), 70, 0.125, True, prefix_lens=i32(prefix), **kw)
+    torch.cuda.synchronize()
+    few = wl.cu_seqlens(lens[at])
+    qh, kh, vh = (f64(x)[:, i * D:(i + 1) * D].reshape(T, 1, D) for i in range(3))
+    kw["prefix_lens"] = prefix[at]
+    ref, weighted = (step.attn_prefill_mod(qh, kh, t, few, 0.125, True, **kw) for t in (vh, np.abs(vh)))
+    dot = 0.125 * np.abs(qh).sum(-1).max() * np.abs(kh).max()
+    near(f64(out.cpu()), ref, tolerance(ref, weighted, dtype, D, 70, dot, 5.0, 0.0), "prompts past one grid")
+
+
 def test_prefill_streams_and_graph(ops):
     import torch
     lens, Hq, Hkv, D = [200, 33, 64], 8, 2, 128

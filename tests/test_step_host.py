@@ -169,6 +169,11 @@ def test_attn_decode_mod_refusals(lib):
     for bad in BAD_MODS:
         assert call(mods=_mods(**bad)) == 1, bad
         assert "attn_decode_mod" in _err(lib)
+    # keys of one sequence and slots of the cache
+    free = dict(tab=1 << 60, o=1 << 61, ws=3 << 60)
+    assert call(bs=1024, mb=(1 << 21) - 1, B=0) == 0 and call(bs=1, mb=(1 << 31) - 1023, **free) == 1
+    assert "2^31 - 1024" in _err(lib)
+    assert call(bs=1024, nb=(1 << 26) + 1, **free) == 1 and "2^36" in _err(lib)
     assert call(wsb=need - 1) == 3 and call(ws=None) == 3 and call(ws=7 * G + 8) == 3
     assert call(D=256) == 2
     assert call(B=0) == 0
