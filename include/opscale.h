@@ -451,7 +451,11 @@ typedef enum {
   OPSCALE_OP_ROPE = 5,
   OPSCALE_OP_RESHAPE_AND_CACHE = 6,
   OPSCALE_OP_ADD_RMSNORM = 7,
-  OPSCALE_OP_FUSED_MOE = 8
+  OPSCALE_OP_FUSED_MOE = 8,
+  OPSCALE_OP_QK_NORM_ROPE = 9,
+  OPSCALE_OP_BLOCK_TABLES = 10,
+  OPSCALE_OP_ATTN_PREFILL_MOD = 11,
+  OPSCALE_OP_ATTN_DECODE_MOD = 12
 } opscale_op;
 
 /* One operator call: the argument list of the matching entry point. */
@@ -489,6 +493,30 @@ typedef struct {
       const void *x, *w1, *w2; const int32_t* topk_ids; const float* topk_weights; void* out;
       int64_t T; int32_t H, F, E, topk; void* workspace; size_t workspace_bytes;
     } fused_moe;
+    struct {
+      const void *q, *k; int64_t q_row_stride, k_row_stride; void *q_out, *k_out;
+      int64_t q_out_row_stride, k_out_row_stride; const void *q_weight, *k_weight; float eps;
+      const int32_t* positions; const double* inv_freq; int32_t rot, interleaved; float magnitude;
+      const void* v; int64_t v_row_stride; void *k_cache, *v_cache; const int32_t* slot_mapping;
+      int32_t block_size; int64_t num_blocks, T; int32_t Hq, Hkv, D;
+    } qk_norm_rope;
+    struct {
+      const int32_t *context_lens, *new_lens; int32_t B; int32_t* block_table;
+      int32_t max_blocks_per_seq, block_size; const int32_t* free_blocks; int64_t num_free;
+      const int32_t* free_begin; int64_t max_tokens;
+      int32_t *cu_seqlens, *positions, *slot_mapping, *kv_lens, *free_next;
+    } block_tables;
+    struct { /* attn_prefill's arguments; mods as if given by address */
+      const void *q, *k, *v; int64_t q_row_stride, kv_row_stride; void* o;
+      const int32_t* cu_seqlens; int32_t B; int64_t total_tokens; int32_t max_seqlen;
+      int32_t Hq, Hkv, D; float scale; int32_t causal; opscale_attn_mods mods;
+    } attn_prefill_mod;
+    struct {
+      const void* q; int64_t q_row_stride; const void *k_cache, *v_cache;
+      const int32_t *block_table, *context_lens; void* o;
+      int32_t B, Hq, Hkv, D, block_size, max_blocks_per_seq; int64_t num_blocks;
+      int32_t max_context_len; float scale; opscale_attn_mods mods; void* workspace; size_t workspace_bytes;
+    } attn_decode_mod;
   } u;
 } opscale_op_desc;
 

@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libopscale.so")
 OPSCALE_OK, OPSCALE_ERR_INVALID_ARG, OPSCALE_ERR_UNSUPPORTED, OPSCALE_ERR_WORKSPACE, OPSCALE_ERR_HIP = range(5)
 OPSCALE_F32, OPSCALE_BF16 = 0, 1
 (OP_RMSNORM, OP_LINEAR, OP_SWIGLU, OP_ATTN_PREFILL, OP_ATTN_DECODE, OP_ROPE, OP_RESHAPE_AND_CACHE,
- OP_ADD_RMSNORM, OP_FUSED_MOE) = range(9)
+ OP_ADD_RMSNORM, OP_FUSED_MOE, OP_QK_NORM_ROPE, OP_BLOCK_TABLES, OP_ATTN_PREFILL_MOD, OP_ATTN_DECODE_MOD) = range(13)
 (TUNE_GEMM_TILE, TUNE_GEMM_SKINNY, TUNE_GEMM_SPLITK, TUNE_GEMM_TAIL, TUNE_SKINNY_NG, TUNE_PREFILL_SCHEDULE,
  TUNE_MOE_FUSE, TUNE_GEMM_DECODE) = range(8)
 TUNE_AUTO = -1
@@ -90,11 +90,36 @@ class AttnMods(ctypes.Structure):
     _fields_ = [("softcap", c_f32), ("window", c_i32), ("slopes", c_vp), ("prefix_lens", c_vp), ("doc_starts", c_vp)]
 
 
+class _QkNormRopeArgs(ctypes.Structure):
+    _fields_ = [("q", c_vp), ("k", c_vp), ("q_row_stride", c_i64), ("k_row_stride", c_i64), ("q_out", c_vp),
+                ("k_out", c_vp), ("q_out_row_stride", c_i64), ("k_out_row_stride", c_i64), ("q_weight", c_vp),
+                ("k_weight", c_vp), ("eps", c_f32), ("positions", c_vp), ("inv_freq", c_vp), ("rot", c_i32),
+                ("interleaved", c_i32), ("magnitude", c_f32), ("v", c_vp), ("v_row_stride", c_i64), ("k_cache", c_vp),
+                ("v_cache", c_vp), ("slot_mapping", c_vp), ("block_size", c_i32), ("num_blocks", c_i64), ("T", c_i64),
+                ("Hq", c_i32), ("Hkv", c_i32), ("D", c_i32)]
+
+
+class _BlockTablesArgs(ctypes.Structure):
+    _fields_ = [("context_lens", c_vp), ("new_lens", c_vp), ("B", c_i32), ("block_table", c_vp),
+                ("max_blocks_per_seq", c_i32), ("block_size", c_i32), ("free_blocks", c_vp), ("num_free", c_i64),
+                ("free_begin", c_vp), ("max_tokens", c_i64), ("cu_seqlens", c_vp), ("positions", c_vp),
+                ("slot_mapping", c_vp), ("kv_lens", c_vp), ("free_next", c_vp)]
+
+
+class _PrefillModArgs(ctypes.Structure):
+    _fields_ = [*_PrefillArgs._fields_, ("mods", AttnMods)]
+
+
+class _DecodeModArgs(ctypes.Structure):
+    _fields_ = [*_DecodeArgs._fields_[:-2], ("mods", AttnMods), *_DecodeArgs._fields_[-2:]]
+
+
 class _OpUnion(ctypes.Union):
     _fields_ = [("rmsnorm", _RmsnormArgs), ("linear", _LinearArgs), ("swiglu", _SwigluArgs),
                 ("attn_prefill", _PrefillArgs), ("attn_decode", _DecodeArgs), ("rope", _RopeArgs),
                 ("reshape_and_cache", _CacheWriteArgs), ("add_rmsnorm", _AddRmsnormArgs),
-                ("fused_moe", _FusedMoeArgs)]
+                ("fused_moe", _FusedMoeArgs), ("qk_norm_rope", _QkNormRopeArgs), ("block_tables", _BlockTablesArgs),
+                ("attn_prefill_mod", _PrefillModArgs), ("attn_decode_mod", _DecodeModArgs)]
 
 
 class OpDesc(ctypes.Structure):
@@ -973,4 +998,60 @@ def desc_add_rmsnorm(x, residual, w, y, eps=1e-5) -> OpDesc:
     d = OpDesc(op=OP_ADD_RMSNORM, dt=_dt(x))
     H = x.shape[-1]
     d.u.add_rmsnorm = _AddRmsnormArgs(_ptr(x), _ptr(residual), _ptr(w), _ptr(y), x.numel() // H, H, eps)
+    return d
+
+
+def desc_qk_norm_rope(q, k, positions=None, inv_freq=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False,
+                      magnitude=1.0, v=None, k_cache=None, v_cache=None, slot_mapping=None, q_out=None,
+                      k_out=None) -> OpDesc:
+    """In place, each run norms and turns the heads again: give q_out and k_out."""
+    d = OpDesc(op=OP_QK_NORM_ROPE, dt=_dt(q))
+    T, Hq, D = q.shape
+    q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+    for name, t in (("q", q), ("k", k), ("q_out", q_out), ("k_out", k_out), ("v", v)):
+        if t is not None:
+            _heads_view(name, t, t.shape[1], D)
+    nb, bs = (0, 0) if k_cache is None else k_cache.shape[:2]
+    rot = 0 if inv_freq is None else 2 * inv_freq.numel()
+    d.u.qk_norm_rope = _QkNormRopeArgs(_ptr(q), _ptr(k), q.stride(0), k.stride(0), _ptr(q_out), _ptr(k_out),
+                                       q_out.stride(0), k_out.stride(0), _ptr(q_weight), _ptr(k_weight), eps,
+                                       _ptr(positions), _ptr(inv_freq), rot, int(interleaved), magnitude, _ptr(v),
+                                       0 if v is None else v.stride(0), _ptr(k_cache), _ptr(v_cache),
+                                       _ptr(slot_mapping), bs, nb, T, Hq, k.shape[1], D)
+    return d
+
+
+def desc_block_tables(context_lens, new_lens, block_table, free_blocks, free_begin, block_size, max_tokens,
+                      out) -> OpDesc:
+    """`out`: the five tensors of opscale_block_tables."""
+    d = OpDesc(op=OP_BLOCK_TABLES, dt=OPSCALE_F32)
+    B, cols = block_table.shape
+    d.u.block_tables = _BlockTablesArgs(_ptr(context_lens), _ptr(new_lens), B, _ptr(block_table), cols, block_size,
+                                        _ptr(free_blocks), free_blocks.numel(), _ptr(free_begin), max_tokens,
+                                        *(_ptr(t) for t in out))
+    return d
+
+
+def desc_attn_prefill_mod(q, k, v, out, cu_seqlens, max_seqlen, scale, causal=True, softcap=0.0, slopes=None, window=0,
+                          prefix_lens=None, doc_starts=None) -> OpDesc:
+    d = OpDesc(op=OP_ATTN_PREFILL_MOD, dt=_dt(q))
+    T, Hq, D = q.shape
+    d.u.attn_prefill_mod = _PrefillModArgs(_ptr(q), _ptr(k), _ptr(v), q.stride(0), k.stride(0), _ptr(out),
+                                           _ptr(cu_seqlens), cu_seqlens.numel() - 1, T, max_seqlen, Hq, k.shape[1], D,
+                                           scale, int(causal),
+                                           AttnMods(softcap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(doc_starts)))
+    return d
+
+
+def desc_attn_decode_mod(q, k_cache, v_cache, block_table, context_lens, out, max_context_len, scale, workspace,
+                         softcap=0.0, slopes=None, window=0, prefix_lens=None, doc_starts=None) -> OpDesc:
+    d = OpDesc(op=OP_ATTN_DECODE_MOD, dt=_dt(q))
+    B, Hq, D = q.shape
+    nb, bs, Hkv, _ = k_cache.shape
+    _heads_view("q", q, Hq, D)
+    d.u.attn_decode_mod = _DecodeModArgs(_ptr(q), q.stride(0), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
+                                         _ptr(context_lens), _ptr(out), B, Hq, Hkv, D, bs, block_table.shape[1], nb,
+                                         max_context_len, scale,
+                                         AttnMods(softcap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(doc_starts)),
+                                         _ptr(workspace), workspace.numel() * workspace.element_size())
     return d

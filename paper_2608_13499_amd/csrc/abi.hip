@@ -217,6 +217,20 @@ Work work_qk_norm_rope(const opscale::QkNormRope& p, int s) {
           s * (qk + 2 * v), s * (qk + v)};
 }
 
+// Integers only: the lengths, two entries a token, and the pages taken, read and written.
+Work work_block_tables(const std::vector<int32_t>& ctx, const std::vector<int32_t>& fresh, int64_t max_blocks, int64_t bs,
+                       int64_t max_tokens) {
+  const int64_t B = (int64_t)ctx.size(), most = max_blocks * bs;
+  int64_t tokens = 0, pages = 0;
+  for (size_t b = 0; b < ctx.size(); ++b) {
+    const int64_t c = std::max(ctx[b], 0), n = std::min<int64_t>(std::max(fresh[b], 0), max_tokens - tokens);
+    tokens += n;
+    pages += (std::min(c + n, most) + bs - 1) / bs - (std::min(c, most) + bs - 1) / bs;
+  }
+  const int64_t by = 4 * (4 * B + 3 + 2 * max_tokens + 2 * pages);
+  return {0.0, (double)by, 0, by, 4 * (2 * B + 2 + 2 * max_tokens + pages)};
+}
+
 // MoE: each valid (token, slot) pair does the two expert GEMMs (2 H 2F + 2 F H
 // flops, 6 H F) and the SwiGLU (6 F); x and out are read / written once and
 // the weights of every expert that receives a token are read once.
@@ -655,6 +669,28 @@ opscale_status check_fused_moe(const void* x, const void* w1, const void* w2, co
   return OPSCALE_OK;
 }
 
+// The work of an attention call with modifiers, from its lengths on the device.
+opscale_status work_of_prefill_mod(const int32_t* cu_seqlens, int32_t B, int64_t T, int32_t Hq, int32_t Hkv, int32_t D,
+                                   bool causal, const opscale_attn_mods* m, opscale_dtype dt, hipStream_t stream, Work* wk) {
+  std::vector<int32_t> cu, prefix, starts;
+  opscale_status st = copy_ints(cu, cu_seqlens, (int64_t)B + 1, stream);
+  if (st == OPSCALE_OK && m && m->prefix_lens) st = copy_ints(prefix, m->prefix_lens, B, stream);
+  if (st == OPSCALE_OK && m && m->doc_starts) st = copy_ints(starts, m->doc_starts, T, stream);
+  if (st == OPSCALE_OK) *wk = work_prefill_mod(cu, prefix, starts, m ? m->window : 0, Hq, Hkv, D, esize(dt), causal);
+  return st;
+}
+opscale_status work_of_decode_mod(const int32_t* context_lens, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t bs,
+                                  int32_t max_blocks, const opscale_attn_mods* m, opscale_dtype dt, hipStream_t stream,
+                                  Work* wk) {
+  std::vector<int32_t> ctx, prefix, starts;
+  opscale_status st = copy_ints(ctx, context_lens, B, stream);
+  if (st == OPSCALE_OK && m && m->prefix_lens) st = copy_ints(prefix, m->prefix_lens, B, stream);
+  if (st == OPSCALE_OK && m && m->doc_starts) st = copy_ints(starts, m->doc_starts, B, stream);
+  if (st == OPSCALE_OK)
+    *wk = work_decode_mod(ctx, prefix, starts, m ? m->window : 0, Hq, Hkv, D, esize(dt), bs, max_blocks);
+  return st;
+}
+
 opscale::QkNormRope qk_norm_rope_args(const void* q, const void* k, int64_t qs, int64_t ks, void* qo, void* ko,
                                       int64_t qos, int64_t kos, const void* wq, const void* wk, float eps,
                                       const int32_t* pos, const double* freq, int32_t rot, int32_t interleaved,
@@ -983,12 +1019,9 @@ opscale_status opscale_attn_prefill_mod(const void* q, const void* k, const void
                                             stream);
   });
   if (st == OPSCALE_OK && timing) {
-    std::vector<int32_t> cu, prefix, starts;
-    if ((st = copy_ints(cu, cu_seqlens, (int64_t)B + 1, stream)) != OPSCALE_OK) return st;
-    if (mods && mods->prefix_lens && (st = copy_ints(prefix, mods->prefix_lens, B, stream)) != OPSCALE_OK) return st;
-    if (mods && mods->doc_starts && (st = copy_ints(starts, mods->doc_starts, total_tokens, stream)) != OPSCALE_OK)
-      return st;
-    const Work wk = work_prefill_mod(cu, prefix, starts, mods ? mods->window : 0, Hq, Hkv, D, esize(dt), causal != 0);
+    Work wk{};
+    st = work_of_prefill_mod(cu_seqlens, B, total_tokens, Hq, Hkv, D, causal != 0, mods, dt, stream, &wk);
+    if (st != OPSCALE_OK) return st;
     timing->alg_flops = wk.flops;
     timing->alg_bytes = wk.bytes;
   }
@@ -1018,12 +1051,9 @@ opscale_status opscale_attn_decode_mod(const void* q, int64_t q_row_stride, cons
                                            dt == OPSCALE_BF16, workspace, stream);
   });
   if (st == OPSCALE_OK && timing) {
-    std::vector<int32_t> ctx, prefix, starts;
-    if ((st = copy_ints(ctx, context_lens, B, stream)) != OPSCALE_OK) return st;
-    if (mods && mods->prefix_lens && (st = copy_ints(prefix, mods->prefix_lens, B, stream)) != OPSCALE_OK) return st;
-    if (mods && mods->doc_starts && (st = copy_ints(starts, mods->doc_starts, B, stream)) != OPSCALE_OK) return st;
-    const Work wk = work_decode_mod(ctx, prefix, starts, mods ? mods->window : 0, Hq, Hkv, D, esize(dt), block_size,
-                                    max_blocks_per_seq);
+    Work wk{};
+    st = work_of_decode_mod(context_lens, B, Hq, Hkv, D, block_size, max_blocks_per_seq, mods, dt, stream, &wk);
+    if (st != OPSCALE_OK) return st;
     timing->alg_flops = wk.flops;
     timing->alg_bytes = wk.bytes;
   }
@@ -1106,11 +1136,12 @@ opscale_status opscale_block_tables(const int32_t* context_lens, const int32_t* 
                                         slot_mapping, kv_lens, free_next, stream);
   });
   if (st == OPSCALE_OK && timing) {
-    std::vector<int32_t> begin, next;
-    if ((st = copy_ints(begin, free_begin, 1, stream)) != OPSCALE_OK) return st;
-    if ((st = copy_ints(next, free_next, 1, stream)) != OPSCALE_OK) return st;
-    timing->alg_flops = 0.0;  // (integers)
-    timing->alg_bytes = 4.0 * (4.0 * B + 3.0 + 2.0 * (double)max_tokens + 2.0 * ((double)next[0] - (double)begin[0]));
+    std::vector<int32_t> ctx, fresh;
+    if (B > 0 && (st = copy_ints(ctx, context_lens, B, stream)) != OPSCALE_OK) return st;
+    if (B > 0 && (st = copy_ints(fresh, new_lens, B, stream)) != OPSCALE_OK) return st;
+    const Work wk = work_block_tables(ctx, fresh, max_blocks_per_seq, block_size, max_tokens);
+    timing->alg_flops = wk.flops;
+    timing->alg_bytes = wk.bytes;
   }
   return st;
 }
@@ -1284,6 +1315,70 @@ opscale_status prepare_op(const opscale_op_desc* d, hipStream_t stream, const ch
       st = copy_ints(ids, a.topk_ids, a.T * a.topk, stream);
       if (st != OPSCALE_OK) return st;
       wk = work_fused_moe(ids, a.T, a.H, a.F, a.E, 2);
+      break;
+    }
+    case OPSCALE_OP_QK_NORM_ROPE: {
+      const auto& a = d->u.qk_norm_rope;
+      const opscale::QkNormRope p = qk_norm_rope_args(
+          a.q, a.k, a.q_row_stride, a.k_row_stride, a.q_out, a.k_out, a.q_out_row_stride, a.k_out_row_stride, a.q_weight,
+          a.k_weight, a.eps, a.positions, a.inv_freq, a.rot, a.interleaved, a.magnitude, a.v, a.v_row_stride, a.k_cache,
+          a.v_cache, a.slot_mapping, a.block_size, a.num_blocks, a.T, a.Hq, a.Hkv, a.D);
+      st = check_qk_norm_rope(p, a.block_size, a.num_blocks, dt);
+      if (st != OPSCALE_OK) return st;
+      if (a.T == 0) return fail(OPSCALE_ERR_INVALID_ARG, "%s: empty problem", who);
+      launch = [=] { return opscale::launch_qk_norm_rope(p, bf16, stream); };
+      wk = work_qk_norm_rope(p, esize(dt));
+      break;
+    }
+    case OPSCALE_OP_BLOCK_TABLES: {
+      const auto& a = d->u.block_tables;
+      st = check_block_tables(a.context_lens, a.new_lens, a.B, a.block_table, a.max_blocks_per_seq, a.block_size,
+                              a.free_blocks, a.num_free, a.free_begin, a.max_tokens, a.cu_seqlens, a.positions,
+                              a.slot_mapping, a.kv_lens, a.free_next);
+      if (st != OPSCALE_OK) return st;
+      if (a.B == 0) return fail(OPSCALE_ERR_INVALID_ARG, "%s: empty problem", who);
+      launch = [=] {
+        return opscale::launch_block_tables(a.context_lens, a.new_lens, a.B, a.block_table, a.max_blocks_per_seq,
+                                            a.block_size, a.free_blocks, a.num_free, a.free_begin, a.max_tokens,
+                                            a.cu_seqlens, a.positions, a.slot_mapping, a.kv_lens, a.free_next, stream);
+      };
+      std::vector<int32_t> ctx, fresh;
+      if ((st = copy_ints(ctx, a.context_lens, a.B, stream)) != OPSCALE_OK) return st;
+      if ((st = copy_ints(fresh, a.new_lens, a.B, stream)) != OPSCALE_OK) return st;
+      wk = work_block_tables(ctx, fresh, a.max_blocks_per_seq, a.block_size, a.max_tokens);
+      break;
+    }
+    case OPSCALE_OP_ATTN_PREFILL_MOD: {
+      const auto a = d->u.attn_prefill_mod;  // (mods by value: the launch outlives *d)
+      st = check_prefill_mod(a.q, a.k, a.v, a.q_row_stride, a.kv_row_stride, a.o, a.cu_seqlens, a.B, a.total_tokens,
+                             a.max_seqlen, a.Hq, a.Hkv, a.D, a.scale, &a.mods, dt);
+      if (st != OPSCALE_OK) return st;
+      if (a.B == 0 || a.total_tokens == 0) return fail(OPSCALE_ERR_INVALID_ARG, "%s: empty problem", who);
+      launch = [=] {
+        return opscale::launch_attn_prefill_mod(a.q, a.k, a.v, a.q_row_stride, a.kv_row_stride, a.o, a.cu_seqlens, a.B,
+                                                a.total_tokens, a.max_seqlen, a.Hq, a.Hkv, a.D, a.scale, a.causal != 0,
+                                                &a.mods, bf16, stream);
+      };
+      st = work_of_prefill_mod(a.cu_seqlens, a.B, a.total_tokens, a.Hq, a.Hkv, a.D, a.causal != 0, &a.mods, dt, stream, &wk);
+      if (st != OPSCALE_OK) return st;
+      break;
+    }
+    case OPSCALE_OP_ATTN_DECODE_MOD: {
+      const auto a = d->u.attn_decode_mod;
+      st = check_decode_mod(a.q, a.q_row_stride, a.k_cache, a.v_cache, a.block_table, a.context_lens, a.o, a.B, a.Hq,
+                            a.Hkv, a.D, a.block_size, a.max_blocks_per_seq, a.num_blocks, a.max_context_len, a.scale,
+                            &a.mods, dt, a.workspace, a.workspace_bytes);
+      if (st != OPSCALE_OK) return st;
+      if (a.B == 0) return fail(OPSCALE_ERR_INVALID_ARG, "%s: empty problem", who);
+      launch = [=] {
+        return opscale::launch_attn_decode_mod(a.q, a.q_row_stride, a.k_cache, a.v_cache, a.block_table, a.context_lens,
+                                               a.o, a.B, a.Hq, a.Hkv, a.D, a.block_size, a.max_blocks_per_seq,
+                                               a.num_blocks, a.max_context_len, a.scale, &a.mods, bf16, a.workspace,
+                                               stream);
+      };
+      st = work_of_decode_mod(a.context_lens, a.B, a.Hq, a.Hkv, a.D, a.block_size, a.max_blocks_per_seq, &a.mods, dt,
+                              stream, &wk);
+      if (st != OPSCALE_OK) return st;
       break;
     }
     default:

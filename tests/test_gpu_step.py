@@ -331,3 +331,58 @@ def test_block_tables_refuses_tensors(ops):
                 dict(out=(e["new_lens"],) * 5), dict(max_tokens=-1, out=None)):
         with pytest.raises((ops.OpscaleError, RuntimeError)):
             ops.opscale_block_tables(**dict(e, **bad))
+
+
+# --------------------------------------------- timing and profiles of a step ---
+def test_work_and_profiles(ops):
+    """Timed calls and profiles count the work of the definition, in closed form."""
+    import torch
+    flush = torch.zeros(1 << 20, dtype=torch.float32, device="cuda")
+    B, Hq, Hkv, D, bs, new, kept = 6, 8, 2, 64, 16, 40, 50
+    ctx, fresh = i32([kept] * B), i32([new] * B)
+    table, free, begin = i32(np.full((B, 8), -1)), i32(range(64)), i32([0])
+    out, t = ops.opscale_block_tables(ctx, fresh, table, free, begin, bs, B * new, timed=True)
+    pages = B * (-(-(kept + new) // bs) - -(-kept // bs))
+    assert t.alg_flops == 0 and t.alg_bytes == 4 * (4 * B + 3 + 2 * B * new + 2 * pages)
+    p = ops.opscale_op_profile(ops.desc_block_tables(ctx, fresh, table, free, begin, bs, B * new, out), 1, 3, flush)
+    assert (p.alg_flops, p.alg_bytes) == (0, t.alg_bytes) and p.us_median > 0
+    assert int(out[4]) == pages
+
+    # a prompt of its own for each: the tokens, norms, a rotation of half the head, the cache
+    T = B * new
+    pos, slots, cu = i32(list(range(new)) * B), i32(np.random.default_rng(0).permutation(T)), i32(np.arange(B + 1) * new)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    q, k, v = (torch.randn(T, h, D, device="cuda", generator=g).bfloat16() for h in (Hq, Hkv, Hkv))
+    kc, vc = (torch.zeros(T // bs, bs, Hkv, D, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    w, (f, m) = torch.ones(D, dtype=torch.bfloat16, device="cuda"), ops.opscale_rope_frequencies(D // 2, 1e4)
+    kw = dict(positions=pos, inv_freq=f, q_weight=w, k_weight=w, magnitude=m, v=v, k_cache=kc, v_cache=vc,
+              slot_mapping=slots, q_out=torch.empty_like(q), k_out=torch.empty_like(k))
+    (q1, k1), t = ops.opscale_qk_norm_rope(q, k, timed=True, **kw)
+    heads = T * (Hq + Hkv)
+    weights = 2 * 2 * D + 4 * (D // 2)  # two gains, and D / 4 frequencies of 8 bytes
+    assert t.alg_flops == 4 * heads * D + 3 * heads * (D // 2)
+    assert t.alg_bytes == 2 * (2 * heads * D + 3 * T * Hkv * D) + weights + 8 * T
+    p = ops.opscale_op_profile(ops.desc_qk_norm_rope(q, k, **kw), 1, 3, flush)
+    assert (p.alg_flops, p.alg_bytes) == (t.alg_flops, t.alg_bytes)
+    assert (p.weight_bytes, p.io_bytes) == (weights, 2 * (heads + T * Hkv) * D)
+
+    # prefill: a window of 10, the first 4 keys seen by all
+    seen = sum(len(step.visible(i, new, True, 10, 4, 0)) for i in range(new))
+    rules = dict(softcap=5.0, window=10, prefix_lens=i32([4] * B), doc_starts=i32([0] * T),
+                 slopes=torch.ones(Hq, device="cuda"))
+    o, t = ops.opscale_attn_prefill_mod(q1, k1, v, cu, new, 0.1, True, timed=True, **rules)
+    assert t.alg_flops == 4 * D * Hq * B * seen
+    p = ops.opscale_op_profile(ops.desc_attn_prefill_mod(q1, k1, v, torch.empty_like(o), cu, new, 0.1, True, **rules), 1,
+                               3, flush)
+    assert (p.alg_flops, p.alg_bytes) == (t.alg_flops, t.alg_bytes) and p.us_median > 0
+
+    # decode: the same window and prefix over 40 keys
+    tab, lens = i32(np.arange(18).reshape(B, 3) % (T // bs)), i32([new] * B)
+    q1, rules["doc_starts"] = q1[:B].contiguous(), i32([0] * B)
+    o, t = ops.opscale_attn_decode_mod(q1, kc, vc, tab, lens, new, 0.1, timed=True, **rules)
+    assert t.alg_flops == 4 * D * Hq * B * 14
+    o2 = torch.zeros_like(o)
+    ws = torch.empty(ops.opscale_attn_decode_mod_workspace_size(B, Hq, D, new), dtype=torch.uint8, device="cuda")
+    p = ops.opscale_op_profile(ops.desc_attn_decode_mod(q1, kc, vc, tab, lens, o2, new, 0.1, ws, **rules), 1, 3, flush)
+    assert (p.alg_flops, p.alg_bytes) == (t.alg_flops, t.alg_bytes)
+    assert torch.equal(o, o2)

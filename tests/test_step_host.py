@@ -2,6 +2,7 @@
 the rotation's frequencies, and every refusal before anything is enqueued."""
 import ctypes
 import math
+import os
 
 import numpy as np
 import pytest
@@ -177,3 +178,41 @@ def test_attn_decode_mod_refusals(lib):
     assert call(wsb=need - 1) == 3 and call(ws=None) == 3 and call(ws=7 * G + 8) == 3
     assert call(D=256) == 2
     assert call(B=0) == 0
+
+
+# ------------------------------------------------------------- profiling ---
+def test_descriptor_layouts(tmp_path):
+    """The descriptors' fields lie where the header puts them."""
+    import shutil
+    import subprocess
+    if shutil.which("gcc") is None:
+        pytest.skip("gcc not available")
+    import paper_2608_13499_amd as ops
+    L = ops._lib
+    members = {"qk_norm_rope": L._QkNormRopeArgs, "block_tables": L._BlockTablesArgs,
+               "attn_prefill_mod": L._PrefillModArgs, "attn_decode_mod": L._DecodeModArgs}
+    lines = ["#include <stdio.h>", "#include <stddef.h>", '#include "opscale.h"', "int main(void) {",
+             'printf("desc %zu\\n", sizeof(opscale_op_desc));', 'printf("mods %zu\\n", sizeof(opscale_attn_mods));',
+             'printf("last %d\\n", (int)OPSCALE_OP_ATTN_DECODE_MOD);']
+    for m, cls in members.items():
+        lines += [f'printf("{m}.{f} %zu\\n", offsetof(opscale_op_desc, u.{m}.{f}) - offsetof(opscale_op_desc, u));'
+                  for f, _ in cls._fields_]
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    src.write_text("\n".join(lines + ["return 0; }"]))
+    include = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    r = subprocess.run(["gcc", "-I", include, "-I", "/opt/rocm/include", "-D__HIP_PLATFORM_AMD__", str(src), "-o", str(exe)],
+                       capture_output=True, text=True)
+    if r.returncode != 0:
+        pytest.skip("cannot compile against the HIP headers here: " + r.stderr[-200:])
+    out = dict(line.split() for line in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.splitlines())
+    assert int(out.pop("desc")) == ctypes.sizeof(L.OpDesc) and int(out.pop("mods")) == ctypes.sizeof(L.AttnMods)
+    assert int(out.pop("last")) == L.OP_ATTN_DECODE_MOD
+    assert {n: int(at) for n, at in out.items()} == {f"{m}.{f}": getattr(cls, f).offset for m, cls in members.items()
+                                                     for f, _ in cls._fields_}
+
+
+def test_profile_refusals(lib):
+    import paper_2608_13499_amd as ops
+    L, out = ops._lib, ops.Profile()
+    for op in (L.OP_QK_NORM_ROPE, L.OP_BLOCK_TABLES, L.OP_ATTN_PREFILL_MOD, L.OP_ATTN_DECODE_MOD, 13):
+        assert lib.opscale_op_profile(ctypes.byref(ops.OpDesc(op=op, dt=1)), 1, 1, None, 0, None, ctypes.byref(out)) == 1, op
