@@ -401,7 +401,7 @@ opscale_status opscale_block_tables(const int32_t* context_lens, const int32_t* 
 typedef struct {
   float softcap;              /* 0: none; finite and >= 0 */
   int32_t window;             /* 0: none; >= 0 */
-  const float* slopes;        /* DEVICE fp32 [Hq], finite, or NULL */
+  const float* slopes;        /* DEVICE fp32 [Hq], magnitudes below 2^32, or NULL */
   const int32_t* prefix_lens; /* DEVICE int32 [B] or NULL (0); values outside [0, length] count as the nearer end */
   const int32_t* doc_starts;  /* DEVICE int32, or NULL (0): the first key of the query's document, one for each
                                  token in prefill ([total_tokens], local to its prompt), one for each
@@ -411,8 +411,9 @@ typedef struct {
 
 /*
  * opscale_attn_prefill with score modifiers and masks (its arguments, layouts
- * and conditions; mods NULL: none; o overlaps no input).  A masked key has no part
- * in a row, whatever its K and V rows hold (infinities and NaN among it).
+ * and conditions; mods NULL: none; o overlaps no input; with slopes, scale is at
+ * least 2^-64).  A masked key has no part in a row, whatever its K and V rows hold
+ * (infinities and NaN among it).
  */
 opscale_status opscale_attn_prefill_mod(const void* q, const void* k, const void* v, int64_t q_row_stride,
                                         int64_t kv_row_stride, void* o, const int32_t* cu_seqlens, int32_t B,

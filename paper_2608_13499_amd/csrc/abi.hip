@@ -375,6 +375,8 @@ opscale_status check_prefill_mod(const void* q, const void* k, const void* v, in
   opscale_status st = check_prefill(q, k, v, qs, kvs, o, cu, B, T, max_seqlen, Hq, Hkv, D, scale, dt);
   if (st == OPSCALE_OK) st = check_mods("attn_prefill_mod", m);
   if (st != OPSCALE_OK || B == 0 || T == 0) return st;
+  if (m && m->slopes && scale < 0x1p-64f)  // (slopes / scale is formed)
+    return fail(OPSCALE_ERR_INVALID_ARG, "attn_prefill_mod: with slopes, scale must be at least 2^-64");
   const int s = esize(dt);
   const int64_t no = T * Hq * D * s, nq = ((T - 1) * qs + (int64_t)Hq * D) * s, nkv = ((T - 1) * kvs + (int64_t)Hkv * D) * s;
   if (overlap(o, no, q, nq) || overlap(o, no, k, nkv) || overlap(o, no, v, nkv) || overlap(o, no, cu, 4ll * (B + 1)) ||

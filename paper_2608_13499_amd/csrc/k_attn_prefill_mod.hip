@@ -26,9 +26,12 @@ namespace opscale {
 //  * A cap of up to 52 bounds the scores so that the reference of the first visible
 //    keys serves to the end (cap_floor): no maximum, no rescale, and the
 //    subtraction is the polynomial's last step.
-//  * The bias adds slope * (j - i) along the keys, three steps from a group's first.
+//  * A bias without a cap costs no VALU work but where keys are ahead of queries: what
+//    it adds along a tile's keys comes out of the MFMAs with the scores, the rest
+//    goes into the subtraction of the reference.  Behind a cap it adds slope * (j - i),
+//    three steps from a group's first.
 //  * A masked key's probability is 0, but 0 times an infinity or NaN in its V row
-//    is not: see special.
+//    is not: see careful.
 template <int D, bool LIST, int MODE>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
     const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,
@@ -45,6 +48,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
   // denominator use the same reference.
   constexpr float kLazy = 8.f;
   __shared__ __attribute__((aligned(16))) char smem_raw[S::kTotal];
+  __shared__ int spoiled[4];  // per wave
   OPS_LDS char* smem = (OPS_LDS char*)smem_raw;
 
   const int G = Hq / Hkv;
@@ -99,6 +103,15 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
     const int nkv = pre_tiles + max(0, (own_end + kBKV - 1) / kBKV - first_tile);
     float slope2 = 0.f;
     if constexpr (BIAS) slope2 = mods.slopes[h] * kLog2e;
+    // Bias alone: the part along a tile's keys comes with the scores, from one more
+    // MFMA step of key offsets (0 .. 63, exact) times the slope in three bf16 pieces
+    // (24 bits), in units of q . k.
+    const float slope_raw = BIAS && !CAP ? slope2 / scale_log2 : 0.f;
+    uint32_t slope_hm = 0, slope_lo = 0;  // (slope's first two and last pieces)
+    if constexpr (BIAS && !CAP) {
+      const float hi = (float)(__bf16)slope_raw, mid = (float)(__bf16)(slope_raw - hi);
+      if (fh == 0) slope_hm = pack_bf2(hi, mid), slope_lo = pack_bf2(slope_raw - hi - mid, 0.f);
+    }
     auto tile_at = [&](int it) { return it >= pre_tiles ? it - pre_tiles + first_tile : it; };
 
     // This wave's 32 query rows as MFMA B operand: chunk 2*s + fh of row q_pos.
@@ -118,9 +131,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
     }
 
     f32x16 acc[DT];
-#pragma unroll
-    for (int i = 0; i < DT; ++i) acc[i] = f32x16{};
-    float m_run = -INFINITY, l_part = 0.f;  // running max (log2 units) and partial sum
+    float m_run, l_part;  // running max (log2 units) and partial sum
 
     // K and V tiles: LDS DMA, rows past the prompt read as zeros.
     auto load_kv = [&](int kv0, int stage) {
@@ -142,185 +153,220 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
       }
     };
 
-    if (nkv > 0) load_kv(tile_at(0) * kBKV, 0);
-    for (int it = 0; it < nkv; ++it) {
-      const int kv0 = tile_at(it) * kBKV;
-      wait_vmem();
-      __syncthreads();
-      if (it + 1 < nkv) load_kv(tile_at(it + 1) * kBKV, (it + 1) & 1);
-      // Skip tiles that none of this wave's queries sees into.
-      const bool active = q_lo < L && (kv0 < pre || (kv0 <= wave_hi_max && kv0 + kBKV - 1 >= wave_lo_min));
-      const OPS_LDS char* ks = smem + (it & 1) * S::kStage;
-      OPS_LDS char* vs = smem + (it & 1) * S::kStage + S::kTileBytes;
-      // A masked key's probability is 0, but its product with an infinity or NaN in V is
-      // not.  So where a tile that some query of the workgroup does not see whole
-      // holds such elements, the waves first add them for the queries that see them,
-      // then put zeros in their place.  (Every way round the loop ends in P V: a
-      // way past it for such tiles, to sum them otherwise, kept two copies of the
-      // accumulators, 64 register moves a tile.)  The same on every wave:
-      auto special = [&] {
-        if (kv0 + kBKV <= pre || (kv0 >= blk_lo_max && kv0 + kBKV - 1 <= blk_hi_min)) return false;
-        uint32_t top = 0;
+    // A masked key's probability is 0, but 0 times an infinity or NaN in its V row is a
+    // NaN.  So a query tile whose result holds a NaN is computed again, carefully.
+    // (Packed documents, 10189 tokens of 16 heads of 64: 56 us; with care taken on the
+    // first pass, every partly masked V tile searched, 67.)
+    for (bool careful = false;; careful = true) {
+#pragma unroll
+      for (int i = 0; i < DT; ++i) acc[i] = f32x16{};
+      m_run = -INFINITY, l_part = 0.f;
+      if (nkv > 0) load_kv(tile_at(0) * kBKV, 0);
+      for (int it = 0; it < nkv; ++it) {
+        const int kv0 = tile_at(it) * kBKV;
+        wait_vmem();
+        __syncthreads();
+        if (it + 1 < nkv) load_kv(tile_at(it + 1) * kBKV, (it + 1) & 1);
+        // Skip tiles that none of this wave's queries sees into.
+        const bool active = q_lo < L && (kv0 < pre || (kv0 <= wave_hi_max && kv0 + kBKV - 1 >= wave_lo_min));
+        const OPS_LDS char* ks = smem + (it & 1) * S::kStage;
+        OPS_LDS char* vs = smem + (it & 1) * S::kStage + S::kTileBytes;
+        // Carefully: where a tile that some query of the workgroup does not see whole
+        // holds such elements, the waves first add them for the queries that see them,
+        // then put zeros in their place.  (Every way round the loop ends in P V: a
+        // way past it for such tiles, to sum them otherwise, kept two copies of the
+        // accumulators, 64 register moves a tile.)  The same on every wave:
+        auto special = [&] {
+          if (!careful || kv0 + kBKV <= pre || (kv0 >= blk_lo_max && kv0 + kBKV - 1 <= blk_hi_min)) return false;
+          uint32_t top = 0;
 #pragma unroll 4
-        for (int i = 0; i < kBKV * CPR / 64; ++i) {
-          const u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16);
+          for (int i = 0; i < kBKV * CPR / 64; ++i) {
+            const u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) top = max(top, max((w[c] & 0x7fffu) << 16, w[c] & 0x7fff0000u));
-        }
-        return __builtin_amdgcn_ballot_w64(top >= 0x7f800000u) != 0;
-      };
-      auto clear_special = [&] {  // (a quarter of the tile a wave)
-        __syncthreads();
-#pragma unroll 1
-        for (int i = wave; i < kBKV * CPR / 64; i += 4) {
-          u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16);
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if ((w[c] & 0x7f80u) == 0x7f80u) w[c] &= 0xffff0000u;
-            if ((w[c] & 0x7f800000u) == 0x7f800000u) w[c] &= 0xffffu;
+            for (int c = 0; c < 4; ++c) top = max(top, max((w[c] & 0x7fffu) << 16, w[c] & 0x7fff0000u));
           }
-          *reinterpret_cast<OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16) = w;
+          return __builtin_amdgcn_ballot_w64(top >= 0x7f800000u) != 0;
+        };
+        auto clear_special = [&] {  // (a quarter of the tile a wave)
+          __syncthreads();
+#pragma unroll 1
+          for (int i = wave; i < kBKV * CPR / 64; i += 4) {
+            u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+              if ((w[c] & 0x7f80u) == 0x7f80u) w[c] &= 0xffff0000u;
+              if ((w[c] & 0x7f800000u) == 0x7f800000u) w[c] &= 0xffffu;
+            }
+            *reinterpret_cast<OPS_LDS u32x4*>(vs + (i * 64 + lane) * 16) = w;
+          }
+          __syncthreads();
+        };
+        if (!active) {
+          if (special()) clear_special();
+          continue;
         }
-        __syncthreads();
-      };
-      if (!active) {
-        if (special()) clear_special();
-        continue;
-      }
-      f32x16 st[2];
+        // no visible key is ahead of its query: |i - j| = i - j
+        const bool behind = kv0 + kBKV - 1 <= q_lo || (causal && pre <= kv0);
+        f32x16 st[2];
 #pragma unroll
-      for (int kb = 0; kb < 2; ++kb) {
-        st[kb] = f32x16{};
-        const int r = kb * 32 + fr;
+        for (int kb = 0; kb < 2; ++kb) {
+          st[kb] = f32x16{};
+          if constexpr (BIAS && !CAP) {
+            float off = (float)(kb * 32 + fr);
+            asm("" : "+v"(off));  // (the operands are put together here: kept, they would spill)
+            const bf16x8 a = __builtin_bit_cast(bf16x8, u32x4{pack_bf2(off, off), pack_bf2(off, 0.f), 0u, 0u});
+            const bf16x8 b = __builtin_bit_cast(bf16x8, u32x4{slope_hm, slope_lo, 0u, 0u});
+            st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, st[kb], 0, 0, 0);
+          }
+          const int r = kb * 32 + fr;
 #pragma unroll
-        for (int s = 0; s < DSTEPS; ++s) {
-          const int c = 2 * s + fh;
-          const bf16x8 kf = *reinterpret_cast<const OPS_LDS bf16x8*>(
-              ks + r * S::kRowBytes + ((c ^ k_swz<D>(r)) << 4));
-          st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], st[kb], 0, 0, 0);
+          for (int s = 0; s < DSTEPS; ++s) {
+            const int c = 2 * s + fh;
+            const bf16x8 kf = *reinterpret_cast<const OPS_LDS bf16x8*>(
+                ks + r * S::kRowBytes + ((c ^ k_swz<D>(r)) << 4));
+            st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], st[kb], 0, 0, 0);
+          }
         }
-      }
-      const bool masked = !(kv0 + kBKV <= pre || (kv0 >= wave_lo_max && kv0 + kBKV - 1 <= wave_hi_min));
-      // this lane's element (kb, e) is key key0 + off, off a constant
-      const int key0 = kv0 + fh * 4;
-      auto off_of = [](int kb, int e) { return kb * 32 + (e >> 2) * 8 + (e & 3); };
-      int to_pre = pre - key0, from = own_lo - key0, to = own_hi - key0;
-      auto sees = [&](int off) { return off < to_pre || (off >= from && off <= to); };
-      auto each = [&](auto&& f) {  // st[kb][e] = f(st[kb][e], off)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) st[kb][e] = f(st[kb][e], off_of(kb, e));
-      };
-      // 1. scores in log2 units (without cap and bias: raw), less the reference
-      // where that stays as it is
-      const bool settled = CAP && !BIAS && mods.cap_floor > -INFINITY && __builtin_amdgcn_ballot_w64(m_run == -INFINITY) == 0;
-      if constexpr (CAP) {
-        if (masked) each([&](float x, int off) { return sees(off) ? x : 0.f; });  // (no say in the choice)
-        float a = 0.f;
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int e = 0; e < 16; ++e) a = fmaxf(a, fabsf(st[kb][e]));
-        const bool small = a <= mods.cap_bound;
-        const float less = settled ? m_run : 0.f;
-        if (__builtin_amdgcn_ballot_w64(!small) == 0)
-          each([&](float x, int) { return mods.capped_small(x, less); });
-        else
-          each([&](float x, int) { return small ? mods.capped_small(x, less) : mods.capped(x, less); });
-      }
-      if constexpr (BIAS) {
-        const float d0 = (float)(key0 - q_pos);  // exact: below 2^24 keys either way
-        if constexpr (!CAP) each([&](float x, int) { return x * scale_log2; });
-        if (kv0 + kBKV - 1 <= q_lo || (causal && pre <= kv0)) {
-          // no visible key is ahead of its query: |i - j| = i - j
+        const bool masked = !(kv0 + kBKV <= pre || (kv0 >= wave_lo_max && kv0 + kBKV - 1 <= wave_hi_min));
+        // this lane's element (kb, e) is key key0 + off, off a constant
+        const int key0 = kv0 + fh * 4;
+        auto off_of = [](int kb, int e) { return kb * 32 + (e >> 2) * 8 + (e & 3); };
+        int to_pre = pre - key0, from = own_lo - key0, to = own_hi - key0;
+        auto sees = [&](int off) { return off < to_pre || (off >= from && off <= to); };
+        auto each = [&](auto&& f) {  // st[kb][e] = f(st[kb][e], off)
 #pragma unroll
           for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-            for (int gq = 0; gq < 4; ++gq) {
-              float bias = slope2 * (d0 + (float)(kb * 32 + gq * 8));
+            for (int e = 0; e < 16; ++e) st[kb][e] = f(st[kb][e], off_of(kb, e));
+        };
+        // 1. scores in log2 units (without cap and bias: raw), less the reference
+        // where that stays as it is
+        const bool settled =
+            CAP && !BIAS && mods.cap_floor > -INFINITY && __builtin_amdgcn_ballot_w64(m_run == -INFINITY) == 0;
+        if constexpr (CAP) {
+          if (masked) each([&](float x, int off) { return sees(off) ? x : 0.f; });  // (no say in the choice)
+          float a = 0.f;
 #pragma unroll
-              for (int e = 0; e < 4; ++e, bias += slope2) st[kb][gq * 4 + e] += bias;
-            }
-        } else {
-          each([&](float x, int off) { return fmaf(-slope2, fabsf(d0 + (float)off), x); });
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) a = fmaxf(a, fabsf(st[kb][e]));
+          const bool small = a <= mods.cap_bound;
+          const float less = settled ? m_run : 0.f;
+          if (__builtin_amdgcn_ballot_w64(!small) == 0)
+            each([&](float x, int) { return mods.capped_small(x, less); });
+          else
+            each([&](float x, int) { return small ? mods.capped_small(x, less) : mods.capped(x, less); });
         }
-      }
-      // (compared again: kept from above, 64 masks would spill)
-      if constexpr (CAP) asm("" : "+v"(to_pre), "+v"(from), "+v"(to));
-      if (masked) each([&](float x, int off) { return sees(off) ? x : -INFINITY; });
-      // 2. the reference moves only when the tile's max exceeds it by kLazy
-      if (!settled) {
-        float tmax = -INFINITY;
+        float base = 0.f;  // the rest of the bias, of every key of the tile
+        if constexpr (BIAS) {
+          const float d0 = (float)(key0 - q_pos);  // exact: below 2^24 keys either way
+          if constexpr (!CAP) {
+            base = slope2 * (float)(kv0 - q_pos);
+            // so far -(i - j); keys ahead take their distance twice to be j - i away
+            if (!behind) each([&](float x, int off) { return fmaf(-2.f * slope_raw, fmaxf(d0 + (float)off, 0.f), x); });
+          } else if (behind) {
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+              for (int gq = 0; gq < 4; ++gq) {
+                float bias = slope2 * (d0 + (float)(kb * 32 + gq * 8));
+#pragma unroll
+                for (int e = 0; e < 4; ++e, bias += slope2) st[kb][gq * 4 + e] += bias;
+              }
+          } else {
+            each([&](float x, int off) { return fmaf(-slope2, fabsf(d0 + (float)off), x); });
+          }
+        }
+        // (compared again: kept from above, 64 masks would spill)
+        if constexpr (CAP) asm("" : "+v"(to_pre), "+v"(from), "+v"(to));
+        if (masked) each([&](float x, int off) { return sees(off) ? x : -INFINITY; });
+        // 2. the reference moves only when the tile's max exceeds it by kLazy
+        if (!settled) {
+          float tmax = -INFINITY;
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, st[kb][e]);
+          tmax = fmaxf(tmax, other_half(tmax));
+          if constexpr (!CAP) tmax = fmaf(tmax, scale_log2, base);
+          if (tmax > m_run + kLazy) {
+            if constexpr (CAP && !BIAS) tmax = fmaxf(tmax, mods.cap_floor);
+            const float alpha = fast_exp2(m_run - tmax);  // 0 on the first tile
+            l_part *= alpha;
+#pragma unroll
+            for (int i = 0; i < DT; ++i) acc[i] *= alpha;
+            m_run = tmax;
+          }
+          const float m = m_run == -INFINITY ? 0.f : m_run;
+          each([&](float x, int) { return CAP ? x - m : fmaf(x, scale_log2, base - m); });
+        }
+        // 3. probabilities
+        float psum = 0.f;
+        bf16x8 pf[4];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) tmax = fmaxf(tmax, st[kb][e]);
-        tmax = fmaxf(tmax, other_half(tmax));
-        if constexpr (!CAP && !BIAS) tmax *= scale_log2;
-        if (tmax > m_run + kLazy) {
-          if constexpr (CAP && !BIAS) tmax = fmaxf(tmax, mods.cap_floor);
-          const float alpha = fast_exp2(m_run - tmax);  // 0 on the first tile
-          l_part *= alpha;
-#pragma unroll
-          for (int i = 0; i < DT; ++i) acc[i] *= alpha;
-          m_run = tmax;
-        }
-        const float m = m_run == -INFINITY ? 0.f : m_run;
-        each([&](float x, int) { return CAP || BIAS ? x - m : fmaf(x, scale_log2, -m); });
-      }
-      // 3. probabilities
-      float psum = 0.f;
-      bf16x8 pf[4];
-#pragma unroll
-      for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          const float p = fast_exp2(st[kb][e]);
-          psum += p;
-          pf[kb * 2 + (e >> 3)][e & 7] = (__bf16)p;
-        }
-      l_part += psum;
-      // O^T[d][i] += sum_key V^T[d][key] P^T[key][i]; the A operand (V^T, lane:
-      // d = 32 dt + fr, keys 16 s + 8 (e/4) + 4 fh + e%4) comes from two
-      // transposed reads of the row-major V tile.
-      auto v_frag = [&](int dt, int s) {
-        const int r0 = 16 * s + tr_key, r1 = r0 + 8;
-        const int cc = 32 * dt + tr_col;  // head-dim column of this lane's 8-byte chunk
-        const int c16 = cc >> 3, half = (cc >> 2) & 1;
-        const u32x2 lo = lds_read_tr16(vs + r0 * S::kRowBytes + ((c16 ^ v_swz<D>(r0)) << 4) + half * 8);
-        const u32x2 hi = lds_read_tr16(vs + r1 * S::kRowBytes + ((c16 ^ v_swz<D>(r1)) << 4) + half * 8);
-        return u32x4{lo[0], lo[1], hi[0], hi[1]};
-      };
-      auto as_bf16 = [](const u32x4& w) { return __builtin_bit_cast(bf16x8, w); };
-      if (special()) {
-        // the special elements, for the queries that see them
-#pragma unroll 1
-        for (int key = 0; key < kBKV; ++key) {
-          const OPS_LDS char* row = vs + key * S::kRowBytes;
-          const u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(row + (lane % CPR) * 16);
-          uint32_t top = 0;
-#pragma unroll
-          for (int c = 0; c < 4; ++c) top = max(top, max((w[c] & 0x7fffu) << 16, w[c] & 0x7fff0000u));
-          if (__builtin_amdgcn_ballot_w64(top >= 0x7f800000u) == 0) continue;
-          const int j = kv0 + key;
-          const bool see = j < pre || (j >= own_lo && j <= own_hi);
-#pragma unroll
-          for (int i = 0; i < DT * 4; ++i) {  // columns 8 i + 4 fh .. + 3
-            const bf16x4 x = *reinterpret_cast<const OPS_LDS bf16x4*>(row + ((i ^ v_swz<D>(key)) << 4) + fh * 8);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              acc[i >> 2][(i & 3) * 4 + e] += see && !(fabsf((float)x[e]) < INFINITY) ? (float)x[e] : 0.f;
+          for (int e = 0; e < 16; ++e) {
+            const float p = fast_exp2(st[kb][e]);
+            psum += p;
+            pf[kb * 2 + (e >> 3)][e & 7] = (__bf16)p;
           }
+        l_part += psum;
+        // O^T[d][i] += sum_key V^T[d][key] P^T[key][i]; the A operand (V^T, lane:
+        // d = 32 dt + fr, keys 16 s + 8 (e/4) + 4 fh + e%4) comes from two
+        // transposed reads of the row-major V tile.
+        auto v_frag = [&](int dt, int s) {
+          const int r0 = 16 * s + tr_key, r1 = r0 + 8;
+          const int cc = 32 * dt + tr_col;  // head-dim column of this lane's 8-byte chunk
+          const int c16 = cc >> 3, half = (cc >> 2) & 1;
+          const u32x2 lo = lds_read_tr16(vs + r0 * S::kRowBytes + ((c16 ^ v_swz<D>(r0)) << 4) + half * 8);
+          const u32x2 hi = lds_read_tr16(vs + r1 * S::kRowBytes + ((c16 ^ v_swz<D>(r1)) << 4) + half * 8);
+          return u32x4{lo[0], lo[1], hi[0], hi[1]};
+        };
+        auto as_bf16 = [](const u32x4& w) { return __builtin_bit_cast(bf16x8, w); };
+        if (special()) {
+          // the special elements, for the queries that see them
+#pragma unroll 1
+          for (int key = 0; key < kBKV; ++key) {
+            const OPS_LDS char* row = vs + key * S::kRowBytes;
+            const u32x4 w = *reinterpret_cast<const OPS_LDS u32x4*>(row + (lane % CPR) * 16);
+            uint32_t top = 0;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) top = max(top, max((w[c] & 0x7fffu) << 16, w[c] & 0x7fff0000u));
+            if (__builtin_amdgcn_ballot_w64(top >= 0x7f800000u) == 0) continue;
+            const int j = kv0 + key;
+            const bool see = j < pre || (j >= own_lo && j <= own_hi);
+#pragma unroll
+            for (int i = 0; i < DT * 4; ++i) {  // columns 8 i + 4 fh .. + 3
+              const bf16x4 x = *reinterpret_cast<const OPS_LDS bf16x4*>(row + ((i ^ v_swz<D>(key)) << 4) + fh * 8);
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                acc[i >> 2][(i & 3) * 4 + e] += see && !(fabsf((float)x[e]) < INFINITY) ? (float)x[e] : 0.f;
+            }
+          }
+          clear_special();
         }
-        clear_special();
-      }
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
+        for (int dt = 0; dt < DT; ++dt) {
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-          acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(v_frag(dt, s)), pf[s], acc[dt], 0, 0, 0);
+          for (int s = 0; s < 4; ++s)
+            acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16(v_frag(dt, s)), pf[s], acc[dt], 0, 0, 0);
+        }
       }
+
+      if (nkv == 0) break;
+      if (!careful) {
+        float any = 0.f;
+#pragma unroll
+        for (int i = 0; i < DT; ++i)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) any += acc[i][e];
+        const bool spoilt = __builtin_amdgcn_ballot_w64(q_pos < L && any != any) != 0;
+        if (lane == 0) spoiled[wave] = spoilt;
+      }
+      wait_vmem();      // (a stage load of a wave with no active step may still be in flight)
+      __syncthreads();  // (and the stages are free)
+      if (careful || (spoiled[0] | spoiled[1] | spoiled[2] | spoiled[3]) == 0) break;
     }
 
     // normalize and store: lane owns query q_pos; acc[dt][e] is
@@ -339,8 +385,6 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
           *reinterpret_cast<u32x2*>(orow + dt * 32 + gq * 8 + fh * 4) = out;
         }
     }
-    wait_vmem();      // (a stage load of a wave with no active step may still be in flight)
-    __syncthreads();  // the next tile reuses the LDS stages
   };
 
   if constexpr (!LIST) {
@@ -470,8 +514,8 @@ hipError_t launch_attn_prefill_mod(const void* q, const void* k, const void* v, 
       if (!g.list) part.x = (unsigned)(n * per);
       AttnMods at = mods;
       if (at.prefix) at.prefix += b;
-      e = launch_mode<decltype(mode)::value>(q, k, v, q_stride, kv_stride, o, cu + b, n, part, Hq, Hkv, D, scale, causal,
-                                             at, s);
+      e = launch_mode<decltype(mode)::value>(q, k, v, q_stride, kv_stride, o, cu + b, n, part, Hq, Hkv, D, scale,
+                                             causal, at, s);
     }
     return e;
   };

@@ -147,6 +147,7 @@ def test_attn_prefill_mod_refusals(lib):
     for bad in BAD_MODS:
         assert call(mods=_mods(**bad)) == 1, bad
         assert "attn_prefill_mod" in _err(lib)
+    assert call(scale=2.0 ** -65, mods=_mods(slopes=6 * G)) == 1 and "2^-64" in _err(lib)
     assert call(D=96) == 2
     assert call(T=0) == 0 and call(B=0) == 0
 
