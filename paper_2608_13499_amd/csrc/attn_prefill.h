@@ -387,6 +387,7 @@ __global__ __launch_bounds__(64) void attn_prefill_f32_row_kernel(
   __shared__ float qs[D];
   __shared__ float ps[64];
   const int t = blockIdx.x, h = blockIdx.y, lane = threadIdx.x;
+  if (MOD && t >= cu[B]) return;  // (padding)
   // prompt of token t
   int lo = 0, hi = B;  // cu[lo] <= t < cu[hi]
   while (hi - lo > 1) {

@@ -303,6 +303,33 @@ def test_prefill_prompts_past_one_grid(ops, dtype):
     near(f64(out.cpu()), ref, tolerance(ref, weighted, dtype, D, 70, dot, 5.0, 0.0), "prompts past one grid")
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("lens,pad", [([3, 1, 9], 5), ([3, 0], 60), ([70, 33], 200), ([300, 2, 40], 1), ([0, 0], 20)])
+def test_prefill_padded_batch(ops, dtype, lens, pad):
+    """Tokens past the last prompt: NaN there, in documents and in o, reach and lose nothing."""
+    import torch
+    Hq, Hkv, D, n = 4, 2, 64, sum(lens)
+    say(f"attn_prefill_mod {dtype}: {lens} and {pad} tokens of padding")
+    x = gen(67, "q", (n + pad, (Hq + 2 * Hkv) * D), dtype, 1.5)
+    x[n:] = float("nan")
+    dev = cuda(x)
+    q, k, v = (dev[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in ((0, 4), (4, 6), (6, 8)))
+    starts = np.zeros(n + pad, np.int64)
+    kw = dict(softcap=5.0, slopes=slopes_of(Hq), doc_starts=starts)
+    for causal in (True, False):
+        out = torch.full((n + pad, Hq, D), 7.0, dtype=dev.dtype, device="cuda")
+        ops.opscale_attn_prefill_mod(q, k, v, i32(wl.cu_seqlens(lens)), max(1, max(lens)), 0.125, causal, out=out, **on_gpu(kw))
+        torch.cuda.synchronize()
+        assert bool((out[n:] == 7.0).all())
+        if n == 0:
+            continue
+        qh, kh, vh = (f64(x[:n])[:, a * D:b * D].reshape(n, -1, D) for a, b in ((0, 4), (4, 6), (6, 8)))
+        ref, weighted = (step.attn_prefill_mod(qh, kh, t, wl.cu_seqlens(lens), 0.125, causal, **kw) for t in (vh, np.abs(vh)))
+        dot = 0.125 * np.abs(qh).sum(-1).max() * np.abs(kh).max()
+        near(f64(out[:n].cpu()), ref, tolerance(ref, weighted, dtype, D, max(lens), dot, 5.0, counted(kw, max(lens))),
+             f"padded, causal {causal}")
+
+
 def test_prefill_streams_and_graph(ops):
     import torch
     lens, Hq, Hkv, D = [200, 33, 64], 8, 2, 128
