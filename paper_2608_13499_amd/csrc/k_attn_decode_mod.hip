@@ -229,7 +229,7 @@ __global__ __launch_bounds__(512, BF16 ? 4 : 2) void attn_decode_mod_kernel(cons
                      : (uint32_t)(4 * grp * row_bytes) + head_at + col * 16;
   }
   float slope2 = 0.f;  // of head `col`
-  if (a.mods.slopes && col < G) slope2 = a.mods.slopes[g * GH + h0 + col] * kLog2e;
+  if (a.mods.slopes && col < G) slope2 = a.mods.slopes[g * GH + h0 + col] * (BF16 ? kLog2e : 1.f);
 
   // One segment: keys [k_begin, k_end) of sequence b, then those of [k2_begin,
   // k2_end), partial results to slot pslot.
@@ -268,23 +268,29 @@ __global__ __launch_bounds__(512, BF16 ? 4 : 2) void attn_decode_mod_kernel(cons
     f32x4 vf32[BF16 ? 1 : 2][4][BF16 ? 1 : D / 64];  // fp32: V of key 16*sub + 4*grp + rr, columns 64 q + 4 col ..
     // Scores, softmax and P V of the tile at t0; `seen`: bit j for key t0 + j.
     auto compute_tile = [&](const int t0, const uint32_t seen) {
-      // scores S^T[key][head]: lane holds head `col`, keys t0 + 16*sub + 4*grp + rr
+      // scores S^T[key][head] (bf16: in log2 units): lane holds head `col`, keys t0 + 16*sub + 4*grp + rr
       f32x4 st[2];
 #pragma unroll
       for (int sub = 0; sub < 2; ++sub) {
-        st[sub] = f32x4{0.f, 0.f, 0.f, 0.f};
+        // fp32: four sums of a quarter of the row each, then theirs (an error of 6e-7 of
+        // scores of 16; one sum of 128 products 1.1e-6)
+        constexpr int CHAINS = BF16 ? 1 : 4;
+        f32x4 part[CHAINS] = {};
 #pragma unroll
         for (int s = 0; s < KCH; ++s) {
+          f32x4& to = part[s % CHAINS];
           if constexpr (BF16) {
-            st[sub] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[sub][s]),
-                                                              __builtin_bit_cast(bf16x8, qf[s]), st[sub], 0, 0, 0);
+            to = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[sub][s]),
+                                                         __builtin_bit_cast(bf16x8, qf[s]), to, 0, 0, 0);
           } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-              st[sub] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[sub][s][e]), __uint_as_float(qf[s][e]),
-                                                             st[sub], 0, 0, 0);
+              to = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(kf[sub][s][e]), __uint_as_float(qf[s][e]), to, 0,
+                                                        0, 0);
           }
         }
+        if constexpr (BF16) st[sub] = part[0];
+        else st[sub] = (part[0] + part[1]) + (part[2] + part[3]);
       }
       auto each = [&](auto&& f) {
 #pragma unroll
@@ -296,7 +302,7 @@ __global__ __launch_bounds__(512, BF16 ? 4 : 2) void attn_decode_mod_kernel(cons
       if constexpr (!BF16) {
         each([&](float x, int) {
           x *= a.scale;
-          return (a.mods.softcap > 0.f ? a.mods.softcap * tanhf(x / a.mods.softcap) : x) * kLog2e;
+          return a.mods.softcap > 0.f ? a.mods.softcap * tanhf(x / a.mods.softcap) : x;
         });
       } else if (a.mods.softcap > 0.f) {
         float big = 0.f;  // (a key that is not there or masked has no say: its K is zeros, or it counts as 0)
@@ -322,6 +328,7 @@ __global__ __launch_bounds__(512, BF16 ? 4 : 2) void attn_decode_mod_kernel(cons
 #pragma unroll
         for (int rr = 0; rr < 4; ++rr) tmax = fmaxf(tmax, st[sub][rr]);
       tmax = rows_max(tmax);
+      if constexpr (!BF16) tmax *= kLog2e;
       // move the reference max only when the tile's max exceeds it by kLazy
       float alpha = 1.f;
       if (tmax > m_run + kLazy) {
@@ -337,7 +344,9 @@ __global__ __launch_bounds__(512, BF16 ? 4 : 2) void attn_decode_mod_kernel(cons
       for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
         for (int rr = 0; rr < 4; ++rr) {
-          const float p = fast_exp2(st[sub][rr] - m_use);
+          // (fp32: one rounding, of a value that is small where it counts; the reference's own
+          // is every key's)
+          const float p = fast_exp2(BF16 ? st[sub][rr] - m_use : fmaf(st[sub][rr], kLog2e, -m_use));
           psum += p;
           st[sub][rr] = p;
           if constexpr (BF16) pa[sub * 4 + rr] = (__bf16)p;
