@@ -260,11 +260,15 @@ __global__ __launch_bounds__(256, D == 64 ? 2 : 1) void attn_prefill_f32_kernel(
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) vf[dt][e] = vrow[dt * 32];
       }
-      f32x16 st = {};
+      f32x16 st = {}, odd = {};  // (MOD: two sums of half the row each, rounded less)
 #pragma unroll
       for (int c = 0; c < DC; ++c)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][e], qf[c][e], st, 0, 0, 0);
+        for (int e = 0; e < 4; ++e) {
+          if (MOD && (c & 1)) odd = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][e], qf[c][e], odd, 0, 0, 0);
+          else st = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[c][e], qf[c][e], st, 0, 0, 0);
+        }
+      if constexpr (MOD) st += odd;
       float tmax = -INFINITY;
       bool all_seen = true;
 #pragma unroll
