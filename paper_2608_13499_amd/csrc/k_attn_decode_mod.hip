@@ -28,11 +28,14 @@
 // an output index), exact tanhf, everything in fp32.
 //
 // A tile whose 32 keys are all visible, in valid pages of 16 slots or more, is
-// addressed from two scalar page bases with per-lane offsets that never change
-// (bf16, 256 sequences of 128 to 8192 tokens, 8 KV heads: per-key addresses from
-// page ids in LDS cost 740 us, these 694 us).  Any other tile looks its keys up one by one; what
-// is not there or masked is read as a row of zeros, so that it adds nothing whatever lies in
-// its place.
+// addressed from two scalar page bases with per-lane offsets that never change.
+// Any other tile looks its keys up one by one; what is not there or masked is read
+// as a row of zeros, so that it adds nothing whatever lies in its place.
+//
+// Measured, bf16, 32 + 8 heads of 128: 256 sequences of 128 to 8192 tokens, cap 50,
+// 692 us, 6.6 TB/s (740 with per-key addresses from page ids in LDS everywhere), and
+// 11 for the merge; four sequences of up to 32768 in a window, 14 + 5 us, the chains
+// of the two kernels.
 #include <climits>
 
 #include "attn_decode.h"
