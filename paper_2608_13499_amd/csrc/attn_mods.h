@@ -22,8 +22,8 @@ struct AttnMods {
   float softcap;
   // softcap * tanh(scale * x / softcap) of a raw score x = q . k, in log2 units:
   // cap_log2 * tanh, e^2y = 2^(cap_rate x), and for |x| <= cap_bound
-  // x * P(x^2) with P of degree 3
-  float cap_log2, cap_rate, cap_bound, cap_poly[4];
+  // x * P(x^2) with P of degree 3, for half of it of degree 2
+  float cap_log2, cap_rate, cap_bound, cap_poly[4], cap_near[3];
   // A capped score t lies within +-cap_log2 (C), so with C <= 75 a row's reference
   // r may be fixed at its first keys' largest t, or C - 60 if that is larger: the
   // probabilities 2^(t - r) are at most 2^60, and the row's largest at least
@@ -36,10 +36,23 @@ struct AttnMods {
     const float u = x * x;
     return fmaf(x, fmaf(u, fmaf(u, fmaf(u, cap_poly[3], cap_poly[2]), cap_poly[1]), cap_poly[0]), -less);
   }
+  __device__ __forceinline__ float capped_near(float x, float less) const {
+    const float u = x * x;
+    return fmaf(x, fmaf(u, fmaf(u, cap_near[2], cap_near[1]), cap_near[0]), -less);
+  }
   // To a few steps of fp32 at cap_log2, any x (an infinity gives +-cap_log2).
   __device__ __forceinline__ float capped(float x, float less) const {
     const float e = __builtin_amdgcn_exp2f(x * cap_rate);
     return fmaf(-2.f * cap_log2, __builtin_amdgcn_rcpf(1.f + e), cap_log2 - less);
+  }
+
+  // Of lanes within cap_bound and past it, both computed: the compiler would branch
+  // around each exponential (prefill of 8192 tokens, 32 heads of 128, cap 15: 787 us, so
+  // 891; decode, which waits for memory, is 1 % faster with the branches).
+  __device__ __forceinline__ float capped_mixed(float x, float less, bool small) const {
+    float far = capped(x, less);
+    asm("" : "+v"(far));
+    return small ? capped_small(x, less) : far;
   }
 
   // A score on the fp32 path: x = scale * q . k, d = |i - j|.
@@ -61,16 +74,20 @@ inline AttnMods make_attn_mods(const opscale_attn_mods* m, float scale) {
   a.window = m->window, a.softcap = m->softcap;
   if (m->softcap > 0.f) {
     constexpr double log2e = 1.4426950408889634;
-    // tanh(y) = y P(y^2) for |y| <= 1/2, to 5.5e-7 of itself (least largest
-    // relative error at this degree)
+    // tanh(y) = y P(y^2) for |y| <= 1/2, to 5.5e-7 of itself, and for |y| <= 1/4 to
+    // 3.7e-7 (least largest relative errors at these degrees)
     constexpr double p[4] = {0.99999946, -0.33326318, 0.13190297, -0.04440223};
+    constexpr double p2[3] = {0.99999964, -0.3332161, 0.12835266};
     const double cap = m->softcap, y = (double)scale / cap;  // y: of one raw unit
     a.cap_log2 = (float)(cap * log2e);
     a.cap_rate = (float)(2.0 * log2e * y);
     a.cap_bound = (float)(0.5 / y);
     a.cap_floor = cap * log2e <= 75.0 ? (float)(cap * log2e - 60.0) : -INFINITY;
     double f = cap * log2e * y;
-    for (int i = 0; i < 4; ++i, f *= y * y) a.cap_poly[i] = (float)(p[i] * f);
+    for (int i = 0; i < 4; ++i, f *= y * y) {
+      a.cap_poly[i] = (float)(p[i] * f);
+      if (i < 3) a.cap_near[i] = (float)(p2[i] * f);
+    }
   }
   return a;
 }

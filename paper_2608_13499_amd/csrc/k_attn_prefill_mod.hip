@@ -22,7 +22,8 @@ namespace opscale {
 //    the tile lie within half the cap takes a polynomial for tanh (it also keeps
 //    the digits of scores far below the cap), other lanes 1 - 2 / (1 + e^2x), an
 //    exponential and a reciprocal at a quarter of the rate each; a wave without such
-//    lanes skips that.
+//    lanes skips that, and one whose scores are all within a quarter takes a degree
+//    less (8192 tokens, 32 heads of 128: 696 us, 712 without).
 //  * A cap of up to 52 bounds the scores so that the reference of the first visible
 //    keys serves to the end (cap_floor): no maximum, no rescale, and the
 //    subtraction is the polynomial's last step.
@@ -269,10 +270,12 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
             for (int e = 0; e < 16; ++e) a = fmaxf(a, fabsf(st[kb][e]));
           const bool small = a <= mods.cap_bound;
           const float less = settled ? m_run : 0.f;
-          if (__builtin_amdgcn_ballot_w64(!small) == 0)
+          if (__builtin_amdgcn_ballot_w64(a > 0.5f * mods.cap_bound) == 0)
+            each([&](float x, int) { return mods.capped_near(x, less); });
+          else if (__builtin_amdgcn_ballot_w64(!small) == 0)
             each([&](float x, int) { return mods.capped_small(x, less); });
           else
-            each([&](float x, int) { return small ? mods.capped_small(x, less) : mods.capped(x, less); });
+            each([&](float x, int) { return mods.capped_mixed(x, less, small); });
         }
         float base = 0.f;  // the rest of the bias, of every key of the tile
         if constexpr (BIAS) {
