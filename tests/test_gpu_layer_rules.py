@@ -144,18 +144,21 @@ def _loop(ops, name, steps):
                    c["lens"], c["bs"], steps, c["sharing"])
 
 
-@pytest.mark.parametrize("name", CASES)
-def test_prompts_then_steps(ops, name):
+@pytest.mark.parametrize("name,pad", [(n, 0) for n in CASES] + [("cap_window", 23), ("bias_prefix", 1), ("f32", 100)])
+def test_prompts_then_steps(ops, name, pad):
+    """pad: tokens past the last prompt's, as a step of a fixed size has them (NaN here)."""
     import torch
     c, loop = _loop(ops, name, steps=3)
-    say(f"layer with rules: {name}")
+    say(f"layer with rules: {name}, {pad} tokens of padding")
     s, lens, dtype = loop.shape, c["lens"], c["dtype"]
     T, B, scale = sum(lens), len(lens), 1.0 / math.sqrt(s.head_dim)
     cu = wl.cu_seqlens(np.asarray(lens))
     pos = np.concatenate([np.arange(n) for n in lens])
     x = gen(loop.seed, "x", (T, s.hidden), dtype)
-    out = loop.prefill(cuda(x), None, i32(lens), T, max(lens))
+    padded = torch.cat([x, torch.full((pad, s.hidden), float("nan"), dtype=x.dtype)])
+    out = loop.prefill(cuda(padded), None, i32(lens), T + pad, max(lens))
     torch.cuda.synchronize()
+    out = {n: t[:T] for n, t in out.items()}
     q, k, v = loop.check_heads(out, pos, "prefill")
     kw = loop.attention_args()
     ref, weighted = (step.attn_prefill_mod(q, k, t, cu, scale, True, **kw) for t in (v, np.abs(v)))
@@ -221,6 +224,46 @@ def test_steps_as_a_graph(ops, name):
         assert graph.ctx.tolist() == [m + n + 1 for m in lens]
     assert torch.equal(graph.table, eager.table)
     assert torch.equal(graph.kc, eager.kc) and torch.equal(graph.vc, eager.vc)
+
+
+def test_two_loops_on_two_streams(ops):
+    """Loops that run at once on streams of their own give what each gives alone."""
+    import torch
+    say("two loops on two streams")
+    names, steps = ("cap_window", "bias_prefix", "f32"), 3
+
+    def run(loop, c, stream, out):
+        T, B = sum(c["lens"]), len(c["lens"])
+        with torch.cuda.stream(stream):
+            x = cuda(gen(7, "x", (T, loop.shape.hidden), c["dtype"]))
+            out.append(loop.prefill(x, None, i32(c["lens"]), T, max(c["lens"]))["y"])
+            yield
+            for n in range(steps):
+                xd, rd = (cuda(gen(8 + n, t, (B, loop.shape.hidden), c["dtype"])) for t in ("x", "attn_out"))
+                out.append(loop.decode(xd, rd, i32([1] * B))["y"])
+                yield
+
+    alone, together = [], []
+    for name in names:
+        c, loop = _loop(ops, name, steps)
+        out = []
+        for _ in run(loop, c, torch.cuda.current_stream(), out):
+            torch.cuda.synchronize()
+        alone.append((out, loop))
+    live = []
+    for name in names:
+        c, loop = _loop(ops, name, steps)
+        out, stream = [], torch.cuda.Stream()
+        stream.wait_stream(torch.cuda.current_stream())
+        together.append((out, loop))
+        live.append(run(loop, c, stream, out))
+    for _ in range(steps + 1):
+        for it in live:
+            next(it)
+    torch.cuda.synchronize()
+    for (a, la), (b, lb) in zip(alone, together):
+        assert all(torch.equal(x, y) for x, y in zip(a, b)) and len(a) == len(b) == steps + 1
+        assert torch.equal(la.kc, lb.kc) and torch.equal(la.vc, lb.vc) and torch.equal(la.table, lb.table)
 
 
 def test_refuses_norms_without_frequencies(ops):
