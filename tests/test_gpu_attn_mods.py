@@ -254,6 +254,46 @@ def test_prefill_masked_infinities_and_nan(ops, dtype, D):
         near(np.where(hit, ref, got), ref, tol, "the others")
 
 
+@pytest.mark.parametrize("schedule", [0, 1])
+@pytest.mark.parametrize("name,D", [("window", 128), ("docs", 64), ("docs_prefix_window", 128), ("open_window_bias", 64),
+                                    ("cap", 64)])
+def test_prefill_special_values_stay_with_their_queries(ops, tune, schedule, name, D):
+    """An infinity and a NaN in V, in several prompts and tiles: the queries that see them get
+    them in those columns, every other element what it is with zeros in their place."""
+    import torch
+    tune(prefill_schedule=schedule)
+    lens, Hq, Hkv = [150, 1, 333, 64, 20], 4, 2
+    say(f"attn_prefill_mod: special values, {name} D={D} schedule={schedule}")
+    kw, causal = rules(name, lens, Hq)
+    cu, T = wl.cu_seqlens(lens), sum(lens)
+    x = gen(68, "q", (T, (Hq + 2 * Hkv) * D), "bf16", 1.5)
+    at = [(70, 0, 3, float("inf")), (149, 1, 0, float("nan")), (151, 0, D - 1, float("-inf")), (151 + 63, 1, 5, float("nan")),
+          (151 + 200, 0, 17, float("inf")), (151 + 332, 1, 40, float("nan")), (T - 84, 0, 9, float("-inf"))]
+
+    def run(values):
+        y = x.clone()
+        for t, g, d, val in values:
+            y[t, (Hq + Hkv + g) * D + d] = val
+        dev = cuda(y)
+        q, k, w = (dev[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+        out = ops.opscale_attn_prefill_mod(q, k, w, i32(cu), max(lens), 1 / math.sqrt(D), causal, **on_gpu(kw))
+        torch.cuda.synchronize()
+        return f64(out.cpu())
+
+    clean, got = run([(t, g, d, 0.0) for t, g, d, _ in at]), run(at)
+    want = clean.copy()
+    for t, g, d, val in at:
+        b = int(np.searchsorted(cu, t, side="right")) - 1
+        for i in range(lens[b]):
+            row = int(cu[b]) + i
+            prefix = 0 if kw.get("prefix_lens") is None else int(kw["prefix_lens"][b])
+            start = 0 if kw.get("doc_starts") is None else int(kw["doc_starts"][row])
+            if t - cu[b] in step.visible(i, lens[b], causal, kw.get("window", 0), prefix, start):
+                want[row, g * (Hq // Hkv):(g + 1) * (Hq // Hkv), d] = val
+    assert np.isfinite(clean).all() and not np.isfinite(want).all()
+    np.testing.assert_array_equal(got, want)
+
+
 def test_prefill_offsets_past_32_bits(ops):
     """Token rows 2^17 elements apart: 5 GB from the first to the last."""
     import torch
