@@ -31,6 +31,12 @@ namespace opscale {
 //    it adds along a tile's keys comes out of the MFMAs with the scores, the rest
 //    goes into the subtraction of the reference.  Behind a cap it adds slope * (j - i),
 //    three steps from a group's first.
+//  * The row's sum adds the probabilities as they were rounded for P V: a query gives its
+//    keys weights that add up to one, and one that sees a single key gets that key's V.
+//    The rounding, to bf16, is the MFMA's price: in two pieces as decode has them,
+//    long prompts take 2.47 ms for 1.91 and documents 62 us for 49, for an rms error of
+//    1.66e-3 (the result's own rounding) in place of 2.09e-3 and 1.82e-3 (of sums of
+//    unrounded ones 2.28e-3 and 1.96e-3).
 //  * A masked key's probability is 0, but 0 times an infinity or NaN in its V row
 //    is not: see careful.
 //
@@ -320,18 +326,22 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
           const float m = m_run == -INFINITY ? 0.f : m_run;
           each([&](float x, int) { return CAP ? x - m : fmaf(x, scale_log2, base - m); });
         }
-        // 3. probabilities
-        float psum = 0.f;
+        // 3. probabilities, rounded to bf16 for P V, and the sum of what was rounded, in
+        // fp32 (the dot product's sums were off by up to 1.5 steps, downwards more often: so
+        // eight at most in a row)
+        float psum[2] = {};
         bf16x8 pf[4];
+        const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float p = fast_exp2(st[kb][e]);
-            psum += p;
-            pf[kb * 2 + (e >> 3)][e & 7] = (__bf16)p;
+          for (int e = 0; e < 16; e += 2) {
+            const bf16x2 p = {(__bf16)fast_exp2(st[kb][e]), (__bf16)fast_exp2(st[kb][e + 1])};
+            psum[kb] = __builtin_amdgcn_fdot2_f32_bf16(p, ones, psum[kb], false);
+            pf[kb * 2 + (e >> 3)][e & 7] = p[0];
+            pf[kb * 2 + (e >> 3)][(e & 7) + 1] = p[1];
           }
-        l_part += psum;
+        l_part += psum[0] + psum[1];
         // O^T[d][i] += sum_key V^T[d][key] P^T[key][i]; the A operand (V^T, lane:
         // d = 32 dt + fr, keys 16 s + 8 (e/4) + 4 fh + e%4) comes from two
         // transposed reads of the row-major V tile.

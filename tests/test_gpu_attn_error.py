@@ -63,3 +63,56 @@ def test_decode(ops, dtype, name, D):
                 want[b, h], bound[b, h] = row(f64(q)[b, h], k, v, n - 1, keys, scale, kw["softcap"],
                                               float(kw["slopes"][h]) if "slopes" in kw else 0.0, dtype, pieces=2)
         within(f64(got.cpu()), want, bound, f"std {std}")
+
+
+# ---------------------------------------------------------------- prefill ---
+def _prefill(ops, x, lens, Hq, Hkv, D, scale, kw, causal=True):
+    """The result for packed x [T, (Hq + 2 Hkv) * D], in float64."""
+    import torch
+    dev = cuda(x)
+    q, k, v = (dev[:, a * D:b * D].unflatten(1, (-1, D)) for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+    cu = np.r_[0, np.cumsum(lens)]
+    out = ops.opscale_attn_prefill_mod(q, k, v, i32(cu), max(lens), scale, causal, **on_gpu(kw))
+    torch.cuda.synchronize()
+    return f64(out.cpu())
+
+
+@pytest.mark.parametrize("name", RULES)
+@pytest.mark.parametrize("D", [64, 128])
+def test_prefill_equal_rows(ops, name, D):
+    """Where every key has the same V, each query that sees one gets it, bit by bit: its
+    weights add up to one within the sums' rounding, far below a step of bf16."""
+    lens, Hq, Hkv = [1, 2, 90, 300], 8, 2
+    kw = _modifiers(name, Hq, len(lens))
+    say(f"attn_prefill_mod bf16 D={D} {name}: equal rows of V")
+    for std in (0.3, 1.5):
+        x = gen(92, "q", (sum(lens), (Hq + 2 * Hkv) * D), "bf16", std)
+        x[:, (Hq + Hkv) * D:] = gen(92, "v_cache", (1, Hkv * D), "bf16")
+        got = _prefill(ops, x, lens, Hq, Hkv, D, 1 / math.sqrt(D), kw)
+        v = f64(x)[:, (Hq + Hkv) * D:].reshape(-1, Hkv, D)
+        np.testing.assert_array_equal(got, np.repeat(v, Hq // Hkv, axis=1))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", RULES)
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_prefill(ops, dtype, name, D, causal):
+    """bf16: the probabilities reach V in 8 bits, and their sum as they were rounded."""
+    lens, Hq, Hkv, scale = [1, 2, 5, 40, 150, 70], 8, 2, 1 / math.sqrt(D)
+    kw = _modifiers(name, Hq, len(lens))
+    say(f"attn_prefill_mod {dtype} D={D} {name} causal={causal}")
+    at = np.r_[0, np.cumsum(lens)]
+    rng = np.random.default_rng(7)
+    for std in (0.3, 1.5):
+        x = gen(93, "q", (sum(lens), (Hq + 2 * Hkv) * D), dtype, std)
+        got = _prefill(ops, x, lens, Hq, Hkv, D, scale, kw, causal)
+        q, k, v = (f64(x)[:, a * D:b * D].reshape(-1, b - a, D) for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+        rows = [(b, i, int(rng.integers(Hq))) for b, n in enumerate(lens) for i in range(n)]
+        want, bound = np.zeros((2, len(rows), D))
+        for r, (b, i, h) in enumerate(rows):
+            keys = _keys(kw, i, lens[b], causal)
+            g = h // (Hq // Hkv)
+            want[r], bound[r] = row(q[at[b] + i, h], k[at[b] + keys, g], v[at[b] + keys, g], i, keys, scale, kw["softcap"],
+                                    float(kw["slopes"][h]) if "slopes" in kw else 0.0, dtype)
+        within(np.stack([got[at[b] + i, h] for b, i, h in rows]), want, bound, f"std {std}")
