@@ -749,24 +749,8 @@ __global__ __launch_bounds__(64 * W) void attn_decode_mod_combine_kernel(const D
   for (int c = 0; c < DPL; ++c) orow[lane + c * 64] = (OUT)(acc[c] * inv);
 }
 
-// Workgroups per head group: as the plain operator's (at most one a CU, 64 a
-// sequence), one more a sequence for the aligned plan, and twice as many where a
-// wave would have two tiles at most: then the chain of a workgroup is the time.
-static int32_t mod_workgroups(int32_t B, int32_t max_context_len, int32_t window, int32_t groups, int waves) {
-  const int64_t b = std::max(1, B);
-  int64_t per_seq = (std::max(1, max_context_len) + (int64_t)kTile - 1) / kTile;
-  if (window > 0) per_seq = std::min<int64_t>(per_seq, window / kTile + 2);
-  const int64_t most = std::max(1, kMaxWorkgroups / std::max(1, groups));
-  const int64_t tiles = b * per_seq;
-  const int64_t cap = tiles <= 2 * waves * most ? 2 * most : most;
-  return (int32_t)std::min<int64_t>(cap, std::min<int64_t>(tiles, b * (cap / most) * kSeqWorkgroups) + b);
-}
-
 size_t decode_mod_workspace_bytes(int32_t B, int32_t Hq, int32_t D, int32_t max_context_len) {
-  // (whatever the window and the groups: at most twice kMaxWorkgroups)
-  const int64_t b = std::max(1, B), tiles = b * ((std::max(1, max_context_len) + (int64_t)kTile - 1) / kTile);
-  const int64_t nwg = std::min<int64_t>(2 * kMaxWorkgroups, std::min<int64_t>(tiles, 2 * b * kSeqWorkgroups) + b);
-  return decode_ws(nullptr, B, Hq, D, (int32_t)nwg).bytes;
+  return decode_ws(nullptr, B, Hq, D, mod_workgroups_most(B, max_context_len)).bytes;
 }
 
 hipError_t launch_attn_decode_mod(const void* q, int64_t q_stride, const void* kcache, const void* vcache,
@@ -778,7 +762,7 @@ hipError_t launch_attn_decode_mod(const void* q, int64_t q_stride, const void* k
   while ((1 << log2bs) < block_size) ++log2bs;
   const AttnMods mods = make_attn_mods(m, scale);
   const int HB = decode_heads_per_workgroup(Hkv), G = Hq / Hkv, blocks = (G + 15) / 16;
-  const int nwg = mod_workgroups(B, max_context_len, mods.window, Hkv / HB * blocks, kWaves / HB);
+  const int nwg = mod_workgroups(B, max_context_len, mods.window, mods.prefix, Hkv / HB * blocks, kWaves / HB);
   const DecodeWs w = decode_ws(ws, B, Hq, D, nwg);
   DecodeArgs a{};
   a.q = q, a.kc = kcache, a.vc = vcache, a.q_stride = q_stride, a.table = table, a.ctx = ctx, a.Hkv = Hkv, a.GH = G;

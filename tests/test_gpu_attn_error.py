@@ -8,7 +8,7 @@ import pytest
 from attn_error import row
 from oracle import step
 from parity_util import cuda, f64, gen, say
-from test_gpu_attn_mods import f32, i32, on_gpu, ops, paged, slopes_of  # noqa: F401
+from test_gpu_attn_mods import check_decode, i32, on_gpu, ops, paged, slopes_of  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -116,3 +116,13 @@ def test_prefill(ops, dtype, name, D, causal):
             want[r], bound[r] = row(q[at[b] + i, h], k[at[b] + keys, g], v[at[b] + keys, g], i, keys, scale, kw["softcap"],
                                     float(kw["slopes"][h]) if "slopes" in kw else 0.0, dtype)
         within(np.stack([got[at[b] + i, h] for b, i, h in rows]), want, bound, f"std {std}")
+
+
+@pytest.mark.parametrize("window", [1, 16, 200])
+@pytest.mark.parametrize("Hq,Hkv", [(8, 8), (14, 2), (4, 1)])
+def test_decode_long_prefix_behind_a_short_window(ops, window, Hq, Hkv):
+    """Nearly all the keys lie in the prefix, few in the window."""
+    ctx = [9000, 40, 7000]
+    kw = dict(window=window, prefix_lens=np.array([8500, 40, 0]), softcap=30.0)
+    check_decode(ops, "bf16", ctx, Hq, Hkv, 128, 16, kw)
+    check_decode(ops, "f32", ctx[:1], Hq, Hkv, 64, 16, dict(kw, prefix_lens=kw["prefix_lens"][:1]))
