@@ -399,7 +399,7 @@ opscale_status opscale_block_tables(const int32_t* context_lens, const int32_t* 
  * A query that sees no key gets a zero row.
  */
 typedef struct {
-  float softcap;              /* 0: none; finite and >= 0 */
+  float softcap;              /* 0: none; finite and >= 0 (2^40 scale or more counts as none) */
   int32_t window;             /* 0: none; >= 0 */
   const float* slopes;        /* DEVICE fp32 [Hq], magnitudes below 2^32, or NULL */
   const int32_t* prefix_lens; /* DEVICE int32 [B] or NULL (0); values outside [0, length] count as the nearer end */

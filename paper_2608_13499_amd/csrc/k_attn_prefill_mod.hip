@@ -549,7 +549,7 @@ hipError_t launch_attn_prefill_mod(const void* q, const void* k, const void* v, 
     }
     return e;
   };
-  switch (attn_mode(m)) {
+  switch (attn_mode(mods)) {
     case kMod: return launch(std::integral_constant<int, kMod>{});
     case kMod | kCap: return launch(std::integral_constant<int, kMod | kCap>{});
     case kMod | kBias: return launch(std::integral_constant<int, kMod | kBias>{});

@@ -126,3 +126,45 @@ def test_decode_long_prefix_behind_a_short_window(ops, window, Hq, Hkv):
     kw = dict(window=window, prefix_lens=np.array([8500, 40, 0]), softcap=30.0)
     check_decode(ops, "bf16", ctx, Hq, Hkv, 128, 16, kw)
     check_decode(ops, "f32", ctx[:1], Hq, Hkv, 64, 16, dict(kw, prefix_lens=kw["prefix_lens"][:1]))
+
+
+# ------------------------------------------------------- caps and values at the ends ---
+def _held(ops, dtype, x, lens, Hq, Hkv, D, scale, cap, what, every=1):
+    """Prefill of packed x, and decode of each prompt's last token over the same keys, within
+    the bounds of each element."""
+    import torch
+    q, k, v = (f64(x)[:, a * D:b * D].reshape(-1, b - a, D) for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+    at, kw = np.r_[0, np.cumsum(lens)], dict(softcap=cap, window=0)
+    got = _prefill(ops, x, lens, Hq, Hkv, D, scale, kw)
+    rows = [(b, i, h) for b, n in enumerate(lens) for i in range(n - 1, -1, -every) for h in range(Hq)]
+    keep = [row(q[at[b] + i, h], k[at[b]:at[b] + i + 1, h * Hkv // Hq], v[at[b]:at[b] + i + 1, h * Hkv // Hq], i,
+                np.arange(i + 1), scale, cap, dtype=dtype) for b, i, h in rows]
+    want, bound = (np.stack(t) for t in zip(*keep))
+    within(np.stack([got[at[b] + i, h] for b, i, h in rows]), want, bound, f"prefill, {what}")
+    bs = 16
+    pages = [-(-n // bs) for n in lens]
+    first = np.r_[0, np.cumsum(pages)]
+    table = np.array([[first[b] + min(j, p - 1) for j in range(max(pages))] for b, p in enumerate(pages)])
+    shape = (int(first[-1]), bs, Hkv, D)
+    kc, vc = (torch.zeros(shape, dtype=x.dtype) for _ in range(2))
+    for b, n in enumerate(lens):
+        for c, lo in ((kc, Hq), (vc, Hq + Hkv)):
+            c.view(-1, Hkv, D)[first[b] * bs:first[b] * bs + n] = x[at[b]:at[b + 1], lo * D:(lo + Hkv) * D].unflatten(1, (-1, D))
+    last = x[at[1:] - 1, :Hq * D].unflatten(1, (-1, D)).contiguous()
+    got = ops.opscale_attn_decode_mod(cuda(last), cuda(kc), cuda(vc), i32(table), i32(lens), max(lens), scale, softcap=cap)
+    torch.cuda.synchronize()
+    pick = [r for r, (b, i, h) in enumerate(rows) if i == lens[b] - 1]
+    within(f64(got.cpu()).reshape(-1, D), want[pick], bound[pick], f"decode, {what}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cap", [1e-44, 1e-30, 1e-12, 1e-9, 1e-8, 1e5, 1e8, 1e12, 1e20, 3e38])
+def test_caps_far_from_the_scores(ops, dtype, cap):
+    """Some heads' queries are zeros, beside heads whose scores pass any small cap."""
+    lens, Hq, Hkv = [70, 1, 130], 8, 2
+    say(f"{dtype}: a cap of {cap}")
+    for D, scale in ((128, 0.09), (64, 1e-3)):
+        x = gen(94, "q", (sum(lens), (Hq + 2 * Hkv) * D), dtype, 1.5)
+        x[:, :3 * D] = 0.0
+        x[::2, 4 * D:5 * D] = 0.0
+        _held(ops, dtype, x, lens, Hq, Hkv, D, scale, float(np.float32(cap)), f"D={D} scale={scale}", every=3)
