@@ -415,6 +415,8 @@ typedef struct {
  * least 2^-64).  cu_seqlens[B] may be less than total_tokens, as opscale_block_tables
  * pads a step: the rows of o past it are left as they were.  A masked key has no
  * part in a row, whatever its K and V rows hold (infinities and NaN among it).
+ * bf16 behind a cap of up to 52: elements of V below 2^-56 may round to zero where
+ * all of a row's scores lie near -softcap.
  */
 opscale_status opscale_attn_prefill_mod(const void* q, const void* k, const void* v, int64_t q_row_stride,
                                         int64_t kv_row_stride, void* o, const int32_t* cu_seqlens, int32_t B,

@@ -20,8 +20,9 @@ struct CapTerms {
   // A capped score t lies within +-cap_log2 (C), so with C <= 75 a row's reference
   // r may be fixed at its first keys' largest t, or C - 60 if that is larger: the
   // probabilities 2^(t - r) are at most 2^60, and the row's largest at least
-  // 2^(60 - 2C) >= 2^-90, with 36 powers of two of fp32 below it.  C - 60, or
-  // -infinity for larger caps, whose rows need a running maximum.
+  // 2^(60 - 2C) >= 2^-90, with 36 powers of two of fp32 below it (what their products
+  // with V leave of that, the kernel looks after).  C - 60, or -infinity for larger caps,
+  // whose rows need a running maximum.
   float cap_floor;
 };
 

@@ -52,6 +52,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
     int64_t q_stride, int64_t kv_stride, __bf16* __restrict__ o, const int32_t* __restrict__ cu,
     int B, int Hq, int Hkv, int hpb, float scale_log2, int causal, const AttnMods mods) {
   constexpr bool CAP = (MODE & kCap) != 0, BIAS = (MODE & kBias) != 0;
+  constexpr bool FIXED = CAP && !BIAS;  // the reference may be fixed
   using S = PrefillSmem<D>;
   constexpr int CPR = D / 8;          // 16-byte chunks per row
   constexpr int DSTEPS = D / 16;      // MFMA k-steps over the head dim
@@ -62,7 +63,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
   // denominator use the same reference.
   constexpr float kLazy = 8.f;
   __shared__ __attribute__((aligned(16))) char smem_raw[S::kTotal];
-  __shared__ int spoiled[4];  // per wave
+  __shared__ int spoiled[4];  // per wave: 1 an infinity or NaN, 2 a row of small probabilities
+  __shared__ int large;       // an element of V is finite and past 2^37
   OPS_LDS char* smem = (OPS_LDS char*)smem_raw;
 
   const int G = Hq / Hkv;
@@ -171,6 +173,12 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
     // NaN.  So a query tile whose result holds a NaN is computed again, carefully.
     // (Packed documents, 10189 tokens of 16 heads of 64: 55 us; with care taken on the
     // first pass, every partly masked V tile searched, 10 more.)
+    // Below a fixed reference probabilities reach 2^60, so that an element of V past 2^37
+    // may overflow the sums: a tile whose result holds an infinity is computed again too,
+    // and if the careful pass leaves one and there are such elements once more, with the
+    // running maximum; at once, where a row's probabilities add up to less than 2^-50 (all
+    // its scores near -cap), whose products with small elements of V would leave fp32 below.
+    float floor = FIXED ? mods.cap_floor : -INFINITY;
     for (bool careful = false;; careful = true) {
 #pragma unroll
       for (int i = 0; i < DT; ++i) acc[i] = f32x16{};
@@ -191,7 +199,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
         // way past it for such tiles, to sum them otherwise, kept two copies of the
         // accumulators, 64 register moves a tile.)  The same on every wave:
         auto special = [&] {
-          if (!careful || kv0 + kBKV <= pre || (kv0 >= blk_lo_max && kv0 + kBKV - 1 <= blk_hi_min)) return false;
+          if (__builtin_expect(!careful, 1) || kv0 + kBKV <= pre || (kv0 >= blk_lo_max && kv0 + kBKV - 1 <= blk_hi_min)) return false;
           uint32_t top = 0;
 #pragma unroll 4
           for (int i = 0; i < kBKV * CPR / 64; ++i) {
@@ -232,14 +240,21 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
             const bf16x8 b = __builtin_bit_cast(bf16x8, u32x4{slope_hm, slope_lo, 0u, 0u});
             st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, st[kb], 0, 0, 0);
           }
-          const int r = kb * 32 + fr;
+        }
+        // (behind a cap the K reads stay one step ahead of their MFMAs by order: left to itself
+        // the compiler here and there waits for each before its MFMA, long prompts 2 % slower)
+        auto k_frag = [&](int kb, int s) {
+          const int r = kb * 32 + fr, c = 2 * s + fh;
+          return *reinterpret_cast<const OPS_LDS bf16x8*>(ks + r * S::kRowBytes + ((c ^ k_swz<D>(r)) << 4));
+        };
+        bf16x8 kf[2][2] = {{k_frag(0, 0), k_frag(1, 0)}};
 #pragma unroll
-          for (int s = 0; s < DSTEPS; ++s) {
-            const int c = 2 * s + fh;
-            const bf16x8 kf = *reinterpret_cast<const OPS_LDS bf16x8*>(
-                ks + r * S::kRowBytes + ((c ^ k_swz<D>(r)) << 4));
-            st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[s], st[kb], 0, 0, 0);
-          }
+        for (int s = 0; s < DSTEPS; ++s) {
+          if (s + 1 < DSTEPS) kf[(s + 1) & 1][0] = k_frag(0, s + 1), kf[(s + 1) & 1][1] = k_frag(1, s + 1);
+          if constexpr (FIXED) __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int kb = 0; kb < 2; ++kb)
+            st[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[s & 1][kb], qf[s], st[kb], 0, 0, 0);
         }
         const bool masked = !(kv0 + kBKV <= pre || (kv0 >= wave_lo_max && kv0 + kBKV - 1 <= wave_hi_min));
         // this lane's element (kb, e) is key key0 + off, off a constant
@@ -266,7 +281,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
         // 1. scores in log2 units (without cap and bias: raw), less the reference
         // where that stays as it is
         const bool settled =
-            CAP && !BIAS && mods.cap_floor > -INFINITY && __builtin_amdgcn_ballot_w64(m_run == -INFINITY) == 0;
+            FIXED && floor > -INFINITY && __builtin_amdgcn_ballot_w64(m_run == -INFINITY) == 0;
         if constexpr (CAP) {
           if (masked) hide(0.f);  // (no say in the choice)
           float a = 0.f;
@@ -316,7 +331,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
           tmax = fmaxf(tmax, other_half(tmax));
           if constexpr (!CAP) tmax = fmaf(tmax, scale_log2, base);
           if (tmax > m_run + kLazy) {
-            if constexpr (CAP && !BIAS) tmax = fmaxf(tmax, mods.cap_floor);
+            if constexpr (FIXED) tmax = fmaxf(tmax, floor);
             const float alpha = fast_exp2(m_run - tmax);  // 0 on the first tile
             l_part *= alpha;
 #pragma unroll
@@ -385,18 +400,39 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
       }
 
       if (nkv == 0) break;
-      if (!careful) {
+      if (!careful || FIXED) {
         float any = 0.f;
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e) any += acc[i][e];
-        const bool spoilt = __builtin_amdgcn_ballot_w64(q_pos < L && any != any) != 0;
+        int spoilt = __builtin_amdgcn_ballot_w64(q_pos < L && (FIXED ? !(fabsf(any) < INFINITY) : any != any)) != 0;
+        if constexpr (FIXED) {
+          const float sum = l_part + other_half(l_part);
+          if (__builtin_amdgcn_ballot_w64(q_pos < L && sum > 0.f && sum < 0x1p-50f) != 0) spoilt = 2;
+          if (threadIdx.x == 0) large = 0;
+        }
         if (lane == 0) spoiled[wave] = spoilt;
       }
       wait_vmem();      // (a stage load of a wave with no active step may still be in flight)
       __syncthreads();  // (and the stages are free)
-      if (careful || (spoiled[0] | spoiled[1] | spoiled[2] | spoiled[3]) == 0) break;
+      const int worst = spoiled[0] | spoiled[1] | spoiled[2] | spoiled[3];
+      if (worst == 0 || (careful && !(FIXED && floor > -INFINITY))) break;
+      if constexpr (FIXED) {
+        if (careful) {
+#pragma unroll 1
+          for (int64_t x = threadIdx.x; x < (int64_t)L * CPR; x += 256) {
+            const u32x4 w = *reinterpret_cast<const u32x4*>(v + (seq0 + x / CPR) * kv_stride + (int64_t)g * D +
+                                                            x % CPR * 8);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+              if ((w[c] & 0x7fffu) - 0x5200u < 0x2d80u || (w[c] >> 16 & 0x7fffu) - 0x5200u < 0x2d80u) large = 1;
+          }
+          __syncthreads();
+          if (large == 0) break;
+        }
+        if (careful || worst > 1) floor = -INFINITY;
+      }
     }
 
     // normalize and store: lane owns query q_pos; acc[dt][e] is

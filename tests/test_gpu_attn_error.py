@@ -168,3 +168,50 @@ def test_caps_far_from_the_scores(ops, dtype, cap):
         x[:, :3 * D] = 0.0
         x[::2, 4 * D:5 * D] = 0.0
         _held(ops, dtype, x, lens, Hq, Hkv, D, scale, float(np.float32(cap)), f"D={D} scale={scale}", every=3)
+
+
+def _apart(seed, lens, Hq, Hkv, D, far, std_v):
+    """Packed bf16 rows whose keys lie along one direction, so that the raw scores of
+    every query are about far[j] sqrt(D) for key j of its prompt; V of std_v."""
+    x = gen(seed, "q", (sum(lens), (Hq + 2 * Hkv) * D), "bf16", 0.3).float()
+    u = gen(seed, "k", (D,), "f32").sign()
+    at = 0
+    for n in lens:
+        x[at:at + n, :Hq * D] += 3.0 * u.repeat(Hq)
+        for j in range(n):
+            x[at + j, Hq * D:(Hq + Hkv) * D] += far(j) / (3.0 * math.sqrt(D)) * u.repeat(Hkv)
+        at += n
+    x[:, (Hq + Hkv) * D:] = gen(seed, "v_cache", (sum(lens), Hkv * D), "f32") * std_v
+    return x.bfloat16()
+
+
+@pytest.mark.parametrize("cap", [5.0, 30.0, 50.0, 52.0, 80.0])
+@pytest.mark.parametrize("D", [64, 128])
+def test_large_and_small_values_behind_a_cap(ops, cap, D):
+    """V near the ends of bf16, where scores lie near -cap first and near cap later, and
+    where all of them lie near -cap."""
+    lens, Hq, Hkv = [200, 1, 70, 300], 4, 2
+    for name, far, std_v in (("rising, large V", lambda j: -400.0 if j < 80 else 400.0, 2.0 ** 100),
+                             ("rising, V of 2^75", lambda j: -400.0 if j < 80 else 400.0, 2.0 ** 75),
+                             ("rising in part, V of 2^100", lambda j: -200.0 + 2 * j, 2.0 ** 100),
+                             ("low, small V", lambda j: -400.0, 2.0 ** -100),
+                             ("low, V of 2^-50", lambda j: -400.0 + j % 7, 2.0 ** -50),
+                             ("low, large V", lambda j: -400.0 + j % 5, 2.0 ** 100)):
+        say(f"cap {cap} D={D}: {name}")
+        x = _apart(95, lens, Hq, Hkv, D, far, std_v)
+        _held(ops, "bf16", x, lens, Hq, Hkv, D, 1 / math.sqrt(D), cap, name, every=7)
+
+
+@pytest.mark.parametrize("cap", [30.0, 50.0])
+def test_large_values_beside_an_infinity(ops, cap):
+    """An infinity that only the last query sees leaves the large finite results of the others."""
+    lens, Hq, Hkv, D = [200], 4, 2, 128
+    say(f"cap {cap}: large V beside an infinity")
+    x = _apart(96, lens, Hq, Hkv, D, lambda j: -400.0 if j < 80 else 400.0, 2.0 ** 100)
+    bad = x.clone()
+    bad[199, (Hq + Hkv) * D + 5] = float("inf")
+    kw = dict(softcap=cap, window=0)
+    clean, got = (_prefill(ops, y, lens, Hq, Hkv, D, 1 / math.sqrt(D), kw) for y in (x, bad))
+    assert np.isfinite(clean).all() and (got[199, :2, 5] == np.inf).all()
+    clean[199, :2, 5] = np.inf
+    np.testing.assert_array_equal(got, clean)
