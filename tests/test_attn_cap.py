@@ -29,18 +29,22 @@ def terms(tmp_path_factory):
     d = tmp_path_factory.mktemp("cap")
     src, so = str(d / "cap.cpp"), str(d / "cap.so")
     with open(src, "w") as f:
-        f.write('#include "attn_cap.h"\nextern "C" void cap(double c, double s, opscale::CapTerms* t) '
-                '{ *t = opscale::cap_terms(c, s); }\n')
+        f.write('#include "attn_cap.h"\nextern "C" {\nvoid cap(double c, double s, opscale::CapTerms* t) '
+                '{ *t = opscale::cap_terms(c, s); }\n'
+                'const double* half() { return opscale::kTanhHalf; }\n'
+                'const double* quarter() { return opscale::kTanhQuarter; }\n}\n')
     subprocess.run([CXX, "-std=c++17", "-O1", "-shared", "-fPIC", f"-I{CSRC}", src, "-o", so], check=True)
     lib = ctypes.CDLL(so)
     lib.cap.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.POINTER(Terms)]
     lib.cap.restype = None
+    lib.half.restype = lib.quarter.restype = ctypes.POINTER(ctypes.c_double)
 
     def call(cap, scale):
         t = Terms()
         lib.cap(float(f32(cap)), float(f32(scale)), ctypes.byref(t))
         return t
 
+    call.lib = lib
     return call
 
 
@@ -90,8 +94,20 @@ def test_any_cap_of_any_score(terms, scale, cap):
     z = np.float64(x) * (float(f32(scale)) / float(f32(cap)))
     want = float(f32(cap)) * LOG2E * np.tanh(z)
     inside = np.abs(np.float64(x)) <= t.cap_bound
-    # polynomials: 5.5e-7 (9.2 steps) and their terms' roundings; past them: of 1 / (1 + e), e and
-    # the exponent (up to 2^4.. of its own steps where e is near 1: |2 z| steps at most 2)
+    # polynomials: 5.45e-7 (9.2 steps) and their terms' roundings; past them the roundings of
+    # e, 1 + e, its reciprocal and the last sum, each a step of the cap or two
     tol = np.where(inside, 14 * U * np.abs(want), 8 * U * float(t.cap_log2)) + 2.0 ** -140
     worst = np.abs(got - want) / tol
     assert worst.max() <= 1.0, (float(worst.max()), float(x[worst.argmax()]), float(z[worst.argmax()]))
+
+
+@pytest.mark.parametrize("name,n,reach,error", [("half", 4, 0.5, 5.45e-7), ("quarter", 3, 0.25, 3.96e-7)])
+def test_polynomials(terms, name, n, reach, error):
+    """Their stated errors; and as these are the least possible, they are reached n + 1 times,
+    with alternating signs."""
+    c = getattr(terms.lib, name)()[:n]
+    y = np.linspace(1e-6, reach, 400001)
+    e = sum(k * y ** (2 * i) for i, k in enumerate(c)) / (np.tanh(y) / y) - 1
+    assert 0.99 * error < np.abs(e).max() <= 1.001 * error
+    signs = np.sign(e[np.abs(e) > 0.99 * np.abs(e).max()])
+    assert 1 + int((np.diff(signs) != 0).sum()) == n + 1
