@@ -215,3 +215,26 @@ def test_large_values_beside_an_infinity(ops, cap):
     assert np.isfinite(clean).all() and (got[199, :2, 5] == np.inf).all()
     clean[199, :2, 5] = np.inf
     np.testing.assert_array_equal(got, clean)
+
+
+@pytest.mark.parametrize("lens", [[9, 3, 1, 16], [40, 12], [64], [300] + [4] * 60])
+@pytest.mark.parametrize("name", ["cap", "bias", "prefix_window"])
+def test_prefill_f32_short_prompts(ops, lens, name):
+    """Prompts of a wave a token and head, alone and beside a long one."""
+    Hq, Hkv, D, scale = 4, 2, 64, 0.125
+    kw = _modifiers(name, Hq, len(lens))
+    if "prefix_lens" in kw:
+        kw["prefix_lens"] = np.minimum(kw["prefix_lens"], lens)
+    say(f"attn_prefill_mod f32 {lens[:5]} {name}")
+    at = np.r_[0, np.cumsum(lens)]
+    x = gen(97, "q", (sum(lens), (Hq + 2 * Hkv) * D), "f32", 1.5)
+    got = _prefill(ops, x, lens, Hq, Hkv, D, scale, kw)
+    q, k, v = (f64(x)[:, a * D:b * D].reshape(-1, b - a, D) for a, b in ((0, Hq), (Hq, Hq + Hkv), (Hq + Hkv, Hq + 2 * Hkv)))
+    rows = [(b, i, h) for b, n in enumerate(lens) for i in range(n) for h in range(Hq)]
+    want, bound = np.zeros((2, len(rows), D))
+    for r, (b, i, h) in enumerate(rows):
+        prefix = int(kw["prefix_lens"][b]) if "prefix_lens" in kw else 0
+        keys = step.visible(i, lens[b], True, kw["window"], prefix, 0)
+        want[r], bound[r] = row(q[at[b] + i, h], k[at[b] + keys, h // 2], v[at[b] + keys, h // 2], i, keys, scale,
+                                kw["softcap"], float(kw["slopes"][h]) if "slopes" in kw else 0.0)
+    within(np.stack([got[at[b] + i, h] for b, i, h in rows]), want, bound, "short prompts")
