@@ -333,7 +333,8 @@ opscale_status opscale_rope_frequencies(double* inv_freq, float* magnitude, int3
  *   (a, b) <- m (a cos t - b sin t, b cos t + a sin t),  t = positions[t] * inv_freq[i],  i < rot / 2,
  * where pair i is (x[i], x[i + rot/2]) (interleaved == 0) or (x[2i], x[2i + 1])
  * (interleaved != 0), m is `magnitude` (not applied to elements rot .. D-1), and the
- * result is rounded once.  The angle is formed and reduced modulo 2 pi in fp64.
+ * result is rounded once.  The angle is formed and reduced modulo 2 pi in fp64, its
+ * sine and cosine and their product with m are fp32.
  * q: [T, Hq, D], k: [T, Hkv, D], token t, head h at q + t * q_row_stride + h * D
  *   (elements; views into the QKV linear's output are fine).
  * q_out, k_out: the results, with row strides of their own; q_out == q (same
@@ -346,8 +347,8 @@ opscale_status opscale_rope_frequencies(double* inv_freq, float* magnitude, int3
  *   (padding).  Without caches v, slot_mapping and the block arguments are ignored.
  *   Tokens sharing a slot race.
  * D a multiple of 16 in [32, 256], rot a multiple of 16 up to D (else
- * OPSCALE_ERR_UNSUPPORTED); tensors 16-byte aligned, strides multiples of 16
- * bytes; eps finite and >= 0; magnitude finite.
+ * OPSCALE_ERR_UNSUPPORTED; the attention calls take D 64 and 128); tensors 16-byte
+ * aligned, strides multiples of 16 bytes; eps finite and >= 0; magnitude finite.
  */
 opscale_status opscale_qk_norm_rope(const void* q, const void* k, int64_t q_row_stride, int64_t k_row_stride,
                                     void* q_out, void* k_out, int64_t q_out_row_stride, int64_t k_out_row_stride,
@@ -376,6 +377,10 @@ opscale_status opscale_qk_norm_rope(const void* q, const void* k, int64_t q_row_
  * slots (*free_next > num_free says how many pages are missing); so are the slots
  * of tokens past max_blocks_per_seq pages, and of pages that are negative.  The cache write
  * skips such slots and attention such pages.
+ * Several new tokens of a request with context_lens[b] > 0 (a chunk of a prompt, a
+ * cached beginning) get their tables and cache rows here, but no attention call reads
+ * the cache for more than one token a request: opscale_attn_prefill and _mod attend to
+ * the call's own tokens only, opscale_attn_decode and _mod take one query.
  * All arrays DEVICE int32: context_lens, new_lens, kv_lens [B]; block_table [B,
  * max_blocks_per_seq]; free_blocks [num_free]; free_begin, free_next [1];
  * positions, slot_mapping [max_tokens].  An output overlaps nothing else.
@@ -415,7 +420,10 @@ typedef struct {
  * least 2^-64).  cu_seqlens[B] may be less than total_tokens, as opscale_block_tables
  * pads a step: the rows of o past it are left as they were.  A masked key has no
  * part in a row, whatever its K and V rows hold (infinities and NaN among it).
- * bf16 behind a cap of up to 52: elements of V below 2^-56 may round to zero where
+ * The keys are the call's own tokens: what a request has in the cache from before is
+ * not seen, nor counted in positions, prefix_lens and doc_starts.
+ * bf16: the probabilities are rounded to bf16 for their product with V, and summed so.
+ * Behind a cap of up to 52: elements of V below 2^-56 may round to zero where
  * all of a row's scores lie near -softcap.
  */
 opscale_status opscale_attn_prefill_mod(const void* q, const void* k, const void* v, int64_t q_row_stride,

@@ -678,7 +678,8 @@ def opscale_attn_prefill_mod(q, k, v, cu_seqlens, max_seqlen: int, scale: float,
     softcap by a tanh, lowered by slopes[h] (float32 [Hq]) a key of distance; a key
     is seen in the prefix (prefix_lens int32 [B]), or in the query's document
     (doc_starts int32 [T], its first key, local to the prompt), fewer than `window`
-    keys away and, causal, not ahead.  A query that sees no key gets zeros."""
+    keys away and, causal, not ahead.  A query that sees no key gets zeros.  The keys
+    are the call's own tokens, not what the cache holds of a prompt from before."""
     lib = load()
     dev, dt, dtype = _current(), _dt(q), q.dtype
     if q.dim() != 3 or k.dim() != 3:

@@ -1,9 +1,10 @@
 // Grouped-query prefill attention over a ragged batch of prompts: what the plain
 // operator (k_attn_prefill.hip) and the one with score modifiers and masks
-// (k_attn_prefill_mod.hip) share.
+// (k_attn_prefill_mod.hip) share, that is the shape of their bf16 kernels, which stand
+// in those files, and the fp32 kernels, which stand below.
 //
-// bf16 path (D = 64 or 128): one workgroup of 4 waves per (prompt, KV head,
-// query tile).  The waves are the query heads of one GQA group (up to 4) times
+// bf16 (D = 64 or 128): one workgroup of 4 waves per (prompt, KV head, query
+// tile).  The waves are the query heads of one GQA group (up to 4) times
 // query sub-tiles of 32 rows, so every K/V tile staged in LDS is shared by all
 // the heads that read it.  Per 64-key K/V tile a wave computes the transposed
 // score tile S^T = K Q^T on MFMA 32x32x16 (A = K rows from LDS, B = its 32
@@ -23,10 +24,8 @@
 // highest level first, so the most expensive tiles (the ends of the longest
 // prompts, which see the most keys) start earliest.  A block whose level is
 // beyond its prompt exits at once; levels past gridDim.y are looped, so the
-// result never depends on max_seqlen.
-//
-// fp32 path: one wave per (token, head), keys 64 at a time, exact expf; it
-// serves the fp32 parity configuration.
+// result never depends on max_seqlen.  Prompts of uneven lengths take a work list of
+// the tiles there are instead (prefill_grid).
 #pragma once
 #include <algorithm>
 #include <cstdlib>

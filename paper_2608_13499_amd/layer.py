@@ -106,8 +106,10 @@ def prefill_layer(shape: LayerShape, w, x, residual, positions, cu_seqlens, max_
                   slot_mapping, stream=None, rules=None):
     """One layer over a ragged prefill batch x [T, H].  positions / slot_mapping:
     int32 [T] on the GPU (position of each token in its prompt, cache slot of
-    each token); cu_seqlens int32 [B + 1].  rules: a dict of the step's slopes,
-    prefix_lens and doc_starts, each as in opscale_attn_prefill_mod."""
+    each token); cu_seqlens int32 [B + 1].  Attention sees the step's own tokens
+    only, so each prompt is whole: one whose beginning is in the cache already
+    would lose those keys.  rules: a dict of the step's slopes, prefix_lens and
+    doc_starts, each as in opscale_attn_prefill_mod."""
     h1, qkv, residual = _front(shape, w, x, residual, stream)
     q, k, v = _split(shape, qkv)
     _place(shape, w, q, k, v, positions, k_cache, v_cache, slot_mapping, stream)
