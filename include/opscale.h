@@ -333,8 +333,8 @@ opscale_status opscale_rope_frequencies(double* inv_freq, float* magnitude, int3
  *   (a, b) <- m (a cos t - b sin t, b cos t + a sin t),  t = positions[t] * inv_freq[i],  i < rot / 2,
  * where pair i is (x[i], x[i + rot/2]) (interleaved == 0) or (x[2i], x[2i + 1])
  * (interleaved != 0), m is `magnitude` (not applied to elements rot .. D-1), and the
- * result is rounded once.  The angle is formed and reduced modulo 2 pi in fp64, its
- * sine and cosine and their product with m are fp32.
+ * result is rounded once.  The angle, its sine and cosine and their product with m
+ * are formed in fp64 and rounded to fp32.
  * q: [T, Hq, D], k: [T, Hkv, D], token t, head h at q + t * q_row_stride + h * D
  *   (elements; views into the QKV linear's output are fine).
  * q_out, k_out: the results, with row strides of their own; q_out == q (same

@@ -11,9 +11,10 @@
 // Bound by memory for many tokens (8871 of 64 + 8 heads of 128 with their cache: 69
 // us, 5.5 TB/s, what a copy reaches), by the chain of loads, angles and stores for one
 // (3.3 us, an empty launch's).  A workgroup takes `tpw` tokens: its heads' rows are requested first, and
-// while they are on their way each angle of those tokens is formed once (fp64
-// product and reduction, fp32 sine and cosine) into LDS, where every head reads
-// it.  The norm's gains sit in registers: a thread's place in its head is the same
+// while they are on their way each angle of those tokens is formed once into LDS,
+// where every head reads it: in fp64 up to the sine and cosine times the magnitude,
+// which are rounded once (fp32 heads: an rms error of 3.3e-8, with fp32 functions
+// of the reduced angle 5.0e-8 and 0.3 us less of 10.2, 1023 tokens of 28 + 4).  The norm's gains sit in registers: a thread's place in its head is the same
 // in every pass.
 #include <algorithm>
 #include <type_traits>
@@ -130,11 +131,10 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(const QkArgs a) {
   for (int i = threadIdx.x; i < nt * half; i += 256) {
     const int tl = i / half;
     const double ang = (double)a.pos[t0 + tl] * a.freq[i - tl * half];
-    const float r = (float)(ang - kTwoPi * rint(ang * (1.0 / kTwoPi)));
-    float sn, cs;
-    sincosf(r, &sn, &cs);
-    sine[i] = sn * a.magnitude;
-    cosine[i] = cs * a.magnitude;
+    double sn, cs;
+    sincospi((ang - kTwoPi * rint(ang * (1.0 / kTwoPi))) * (2.0 / kTwoPi), &sn, &cs);
+    sine[i] = (float)(sn * a.magnitude);
+    cosine[i] = (float)(cs * a.magnitude);
   }
   __syncthreads();
   for (;;) {
