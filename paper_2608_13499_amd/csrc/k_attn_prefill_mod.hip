@@ -40,12 +40,13 @@ namespace opscale {
 //  * A masked key's probability is 0, but 0 times an infinity or NaN in its V row
 //    is not: see careful.
 //
-// Measured: two prompts of 8192, 64 + 8 heads of 128, cap 50, window 4096: 1.94 ms,
-// 850 TFLOP/s; the MFMAs busy 42 % of it, the VALU about 70 %.  Packed documents
-// (10189 tokens, 16 heads of 64, bias, prefix): 55 us, 315 TFLOP/s of what is seen;
-// half the time VALU work, a third of that masks and addresses, tiles seen in part.
-// Sixteen ragged prompts (4436 tokens, 32 + 8 heads of 128, cap): 53 us, the chain
-// of the longest prompt's tiles (15 of 2 us, two workgroups a CU) and its set-up.
+// Measured: two prompts of 8192, 64 + 8 heads of 128, cap 50, window 4096: 1.87 to
+// 2.0 ms from card to card, 820 to 880 TFLOP/s; the MFMAs busy 42 % of it, the VALU
+// about 70 %.  Packed documents (10189 tokens, 16 heads of 64, bias, prefix): 55 us,
+// 315 TFLOP/s of what is seen; half the time VALU work, a third of that masks and
+// addresses, tiles seen in part.  Sixteen ragged prompts (4436 tokens, 32 + 8 heads of
+// 128, cap): 52 us, the chain of the longest prompt's tiles (15 of 2 us, two workgroups
+// a CU) and its set-up.
 template <int D, bool LIST, int MODE>
 __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
     const __bf16* __restrict__ q, const __bf16* __restrict__ k, const __bf16* __restrict__ v,

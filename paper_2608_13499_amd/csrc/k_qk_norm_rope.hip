@@ -14,8 +14,9 @@
 // while they are on their way each angle of those tokens is formed once into LDS,
 // where every head reads it: in fp64 up to the sine and cosine times the magnitude,
 // which are rounded once (fp32 heads: an rms error of 3.3e-8, with fp32 functions
-// of the reduced angle 5.0e-8 and 0.3 us less of 10.2, 1023 tokens of 28 + 4).  The norm's gains sit in registers: a thread's place in its head is the same
-// in every pass.
+// of the reduced angle 5.0e-8 and 0.3 us less of 10.2, 1023 tokens of 28 + 4).  The
+// norm's gains sit in registers: a thread's place in its head is the same in every
+// pass.
 #include <algorithm>
 #include <type_traits>
 
