@@ -64,8 +64,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
   // denominator use the same reference.
   constexpr float kLazy = 8.f;
   __shared__ __attribute__((aligned(16))) char smem_raw[S::kTotal];
-  __shared__ int spoiled[4];  // per wave: 1 an infinity or NaN, 2 a row of small probabilities
-  __shared__ int large;       // an element of V is finite and past 2^37
+  __shared__ int spoiled[4];  // per wave: 1 a NaN, 2 the fixed reference does not serve
   OPS_LDS char* smem = (OPS_LDS char*)smem_raw;
 
   const int G = Hq / Hkv;
@@ -174,11 +173,11 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
     // NaN.  So a query tile whose result holds a NaN is computed again, carefully.
     // (Packed documents, 10189 tokens of 16 heads of 64: 55 us; with care taken on the
     // first pass, every partly masked V tile searched, 10 more.)
-    // Below a fixed reference probabilities reach 2^60, so that an element of V past 2^37
-    // may overflow the sums: a tile whose result holds an infinity is computed again too,
-    // and if the careful pass leaves one and there are such elements once more, with the
-    // running maximum; at once, where a row's probabilities add up to less than 2^-50 (all
-    // its scores near -cap), whose products with small elements of V would leave fp32 below.
+    // Below a fixed reference probabilities reach 2^60, so that large elements of V may
+    // overflow the sums, and where all of a row's scores lie near -cap they stay so small
+    // that products with small elements leave fp32 below.  So it is computed again with
+    // the running maximum where a row's probabilities add up to more than 2^28 and its
+    // result is not finite, or to less than 2^-50.
     float floor = FIXED ? mods.cap_floor : -INFINITY;
     for (bool careful = false;; careful = true) {
 #pragma unroll
@@ -243,7 +242,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
           }
         }
         // (behind a cap the K reads stay one step ahead of their MFMAs by order: left to itself
-        // the compiler here and there waits for each before its MFMA, long prompts 2 % slower)
+        // the compiler here and there waits for each before its MFMA, long prompts 1 to 2 % slower)
         auto k_frag = [&](int kb, int s) {
           const int r = kb * 32 + fr, c = 2 * s + fh;
           return *reinterpret_cast<const OPS_LDS bf16x8*>(ks + r * S::kRowBytes + ((c ^ k_swz<D>(r)) << 4));
@@ -401,39 +400,26 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void attn_prefill_mod_kernel(
       }
 
       if (nkv == 0) break;
-      if (!careful || FIXED) {
+      if (!careful) {
         float any = 0.f;
 #pragma unroll
         for (int i = 0; i < DT; ++i)
 #pragma unroll
           for (int e = 0; e < 16; ++e) any += acc[i][e];
-        int spoilt = __builtin_amdgcn_ballot_w64(q_pos < L && (FIXED ? !(fabsf(any) < INFINITY) : any != any)) != 0;
+        int spoilt = __builtin_amdgcn_ballot_w64(q_pos < L && any != any) != 0;
         if constexpr (FIXED) {
           const float sum = l_part + other_half(l_part);
-          if (__builtin_amdgcn_ballot_w64(q_pos < L && sum > 0.f && sum < 0x1p-50f) != 0) spoilt = 2;
-          if (threadIdx.x == 0) large = 0;
+          const bool over = sum > 0x1p28f && !(fabsf(any) < INFINITY), under = sum > 0.f && sum < 0x1p-50f;
+          if (floor > -INFINITY && __builtin_amdgcn_ballot_w64(q_pos < L && (over || under)) != 0) spoilt = 2;
         }
         if (lane == 0) spoiled[wave] = spoilt;
       }
       wait_vmem();      // (a stage load of a wave with no active step may still be in flight)
       __syncthreads();  // (and the stages are free)
+      if (careful) break;
       const int worst = spoiled[0] | spoiled[1] | spoiled[2] | spoiled[3];
-      if (worst == 0 || (careful && !(FIXED && floor > -INFINITY))) break;
-      if constexpr (FIXED) {
-        if (careful) {
-#pragma unroll 1
-          for (int64_t x = threadIdx.x; x < (int64_t)L * CPR; x += 256) {
-            const u32x4 w = *reinterpret_cast<const u32x4*>(v + (seq0 + x / CPR) * kv_stride + (int64_t)g * D +
-                                                            x % CPR * 8);
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-              if ((w[c] & 0x7fffu) - 0x5200u < 0x2d80u || (w[c] >> 16 & 0x7fffu) - 0x5200u < 0x2d80u) large = 1;
-          }
-          __syncthreads();
-          if (large == 0) break;
-        }
-        if (careful || worst > 1) floor = -INFINITY;
-      }
+      if (worst == 0) break;
+      if (worst > 1) floor = -INFINITY;
     }
 
     // normalize and store: lane owns query q_pos; acc[dt][e] is
