@@ -450,6 +450,108 @@ opscale_status opscale_attn_decode_mod(const void* q, int64_t q_row_stride, cons
                                        size_t workspace_bytes, hipStream_t stream, opscale_timing* timing);
 
 /* ---------------------------------------------------------------------------
+ * The layer in fewer bits: linears of 8-bit operands and a KV cache in 4 bits.
+ * Linears and decode attention are bound by the bytes of weights and cache, or by the
+ * matrix rate, which 8-bit operands double.
+ *
+ * e4m3: a sign, 4 bits of exponent, 3 of fraction; largest value 448; no infinities,
+ *   0x7f and 0xff are NaN.  e2m1: a sign, 2 bits of exponent, 1 of fraction: 0, 0.5, 1,
+ *   1.5, 2, 3, 4, 6 and their negatives (codes 0 to 7, + 8).
+ * What is quantised here has a power-of-two scale 2^e for each block of elements, so that
+ * x 2^-e is exact and an element is rounded once, to the nearest value, ties to even:
+ *   e = the least integer in [lowest, highest] with max |x| <= most * 2^e,
+ * where no integer is, the highest (larger elements then saturate).
+ * ------------------------------------------------------------------------- */
+
+/*
+ * Activations to e4m3 with a scale for each token and 128 of its elements
+ * (most = 448, lowest -100, highest 120):
+ *   q[m, k] = e4m3(x[m, k] 2^-e),  scales[k / 128, m] = 2^e.
+ * x: [M, K], rows of x_row_stride elements; q: [M, K] bytes, dense; scales: fp32
+ * [ceil(K / 128), M].  A block that holds an infinity or NaN has the scale NaN (its codes
+ * then have no meaning).  K a multiple of 16, up to 2^20; x and q 16-byte aligned, x_row_stride a multiple
+ * of 16 bytes; nothing overlaps.
+ */
+opscale_status opscale_quantize_fp8(const void* x, int64_t x_row_stride, void* q, float* scales, int64_t M, int64_t K,
+                                    opscale_dtype dt, hipStream_t stream, opscale_timing* timing);
+
+/* Bytes of device workspace opscale_linear_fp8 can use for these sizes (the fp32
+ * partial results of a K split; 0 when the planned path splits nothing). */
+size_t opscale_linear_fp8_workspace_size(int64_t M, int64_t N, int64_t K, opscale_dtype dt);
+
+/*
+ * Linear projection of e4m3 operands with block scales:
+ *   y[m, n] = sum_b x_scales[b, m] w_scales[n / 128, b] sum_{k in block b} x[m, k] W[n, k] (+ bias[n]),
+ * block b being elements 128 b .. 128 b + 127 of K.
+ * x: [M, K] bytes with x_scales fp32 [ceil(K / 128), M], as opscale_quantize_fp8 leaves
+ * them (any fp32 scales will do); W: [N, K] bytes with w_scales fp32 [ceil(N / 128),
+ * ceil(K / 128)]; bias: [N] of dt, or NULL; y: [M, N] of dt, overlapping nothing else.
+ * Scales and sums over the blocks are fp32.  bf16 results: the inner sums are those of
+ * the fp8 matrix instructions, which cut each product to 2^-13 of the largest of its eight
+ * (k = 8 i .. 8 i + 7); fp32 results: the products are whole and summed in fp32.
+ * K a multiple of 16, up to 2^20; N * sizeof(dt) a multiple of 16; M, N below 2^30 and
+ * M * N up to 2^40; x, W, y, bias and workspace 16-byte aligned.
+ * workspace: as opscale_linear's (NULL: no K split; otherwise at least
+ * opscale_linear_fp8_workspace_size(M, N, K, dt) bytes, else OPSCALE_ERR_WORKSPACE).
+ * Splits are summed in a fixed order: deterministic.
+ */
+opscale_status opscale_linear_fp8(const void* x, const float* x_scales, const void* W, const float* w_scales,
+                                  const void* bias, void* y, int64_t M, int64_t N, int64_t K, opscale_dtype dt,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream, opscale_timing* timing);
+
+/*
+ * A paged KV cache in 4 bits: e2m1 elements with a scale for each 32 consecutive elements
+ * of a head (most = 7: 6 is half a step of 4 to 6 away from it; lowest -100, highest 125).
+ * k_cache, v_cache: [num_blocks, Hkv, block_size * (D / 2 + D / 32)] bytes.  Of a page and
+ * head, first the codes of its block_size rows (element 2 i of a row in the low four bits
+ * of its byte i, 2 i + 1 in the high four), then a byte e + 127 for each group and row
+ * ([D / 32][block_size]).  The byte 255 makes a group NaN: it held an infinity or NaN.
+ * block_size a power of two in [16, 1024]; D 64 or 128.
+ */
+
+/*
+ * opscale_reshape_and_cache to such a cache: the K and V rows of token t (k, v: [T, Hkv,
+ * D], rows of kv_row_stride elements) go to slot slot_mapping[t], quantised.  A token
+ * whose slot is outside [0, num_blocks * block_size) is skipped (padding).  num_blocks *
+ * block_size < 2^31.  The caches overlap nothing else.  Tokens sharing a slot race.
+ */
+opscale_status opscale_kv_write_fp4(const void* k, const void* v, int64_t kv_row_stride, void* k_cache, void* v_cache,
+                                    const int32_t* slot_mapping, int64_t T, int32_t Hkv, int32_t D, int32_t block_size,
+                                    int64_t num_blocks, opscale_dtype dt, hipStream_t stream, opscale_timing* timing);
+
+/*
+ * Such a cache's rows as dt, packed: row cu_seqlens[b] + i of k and v is key first_keys[b] + i
+ * of sequence b, for cu_seqlens[b] <= row < cu_seqlens[b + 1].
+ * cu_seqlens: DEVICE int32 [B + 1], cu_seqlens[0] = 0, non-decreasing, cu_seqlens[B] <=
+ * total_tokens (the rows past it are left as they were); first_keys: DEVICE int32 [B], or
+ * NULL (0); block_table: DEVICE int32 [B, max_blocks_per_seq].
+ * k, v: [total_tokens, Hkv, D], rows of kv_row_stride elements (both may be views into
+ * one tensor); they overlap nothing else.  A key below 0, past max_blocks_per_seq pages, or
+ * whose page is outside [0, num_blocks) reads as zeros.  Values past bf16's or fp32's range
+ * do not arise from opscale_kv_write_fp4.
+ */
+opscale_status opscale_kv_read_fp4(const void* k_cache, const void* v_cache, const int32_t* block_table,
+                                   const int32_t* cu_seqlens, const int32_t* first_keys, void* k, void* v,
+                                   int64_t kv_row_stride, int32_t B, int64_t total_tokens, int32_t Hkv, int32_t D,
+                                   int32_t block_size, int32_t max_blocks_per_seq, int64_t num_blocks, opscale_dtype dt,
+                                   hipStream_t stream, opscale_timing* timing);
+
+/* Bytes of device workspace that opscale_attn_decode_fp4 needs for these sizes. */
+size_t opscale_attn_decode_fp4_workspace_size(int32_t B, int32_t Hq, int32_t D, int32_t max_context_len);
+
+/*
+ * opscale_attn_decode_mod over such a cache (its arguments, modifiers, masks and
+ * conditions; block_size at least 16; q and o are dt).  The cache's values enter as they
+ * are, probabilities as two bf16 pieces (fp32: queries and probabilities as three).
+ */
+opscale_status opscale_attn_decode_fp4(const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache,
+                                       const int32_t* block_table, const int32_t* context_lens, void* o, int32_t B,
+                                       int32_t Hq, int32_t Hkv, int32_t D, int32_t block_size,
+                                       int32_t max_blocks_per_seq, int64_t num_blocks, int32_t max_context_len,
+                                       float scale, const opscale_attn_mods* mods, opscale_dtype dt, void* workspace,
+                                       size_t workspace_bytes, hipStream_t stream, opscale_timing* timing);
+
+/* ---------------------------------------------------------------------------
  * Operator profiling (Section 4.2 "Operator Profiling": per-operator compute
  * time T_v and memory M_v; Appendix C "Dataflow Characteristics": the payload
  * an operator hands to the next one, the basis of C_v).
@@ -467,7 +569,12 @@ typedef enum {
   OPSCALE_OP_QK_NORM_ROPE = 9,
   OPSCALE_OP_BLOCK_TABLES = 10,
   OPSCALE_OP_ATTN_PREFILL_MOD = 11,
-  OPSCALE_OP_ATTN_DECODE_MOD = 12
+  OPSCALE_OP_ATTN_DECODE_MOD = 12,
+  OPSCALE_OP_QUANTIZE_FP8 = 13,
+  OPSCALE_OP_LINEAR_FP8 = 14,
+  OPSCALE_OP_KV_WRITE_FP4 = 15,
+  OPSCALE_OP_KV_READ_FP4 = 16,
+  OPSCALE_OP_ATTN_DECODE_FP4 = 17
 } opscale_op;
 
 /* One operator call: the argument list of the matching entry point. */
@@ -528,7 +635,21 @@ typedef struct {
       const int32_t *block_table, *context_lens; void* o;
       int32_t B, Hq, Hkv, D, block_size, max_blocks_per_seq; int64_t num_blocks;
       int32_t max_context_len; float scale; opscale_attn_mods mods; void* workspace; size_t workspace_bytes;
-    } attn_decode_mod;
+    } attn_decode_mod, attn_decode_fp4;
+    struct { const void* x; int64_t x_row_stride; void* q; float* scales; int64_t M, K; } quantize_fp8;
+    struct {
+      const void* x; const float* x_scales; const void* W; const float* w_scales; const void* bias; void* y;
+      int64_t M, N, K; void* workspace; size_t workspace_bytes;
+    } linear_fp8;
+    struct {
+      const void *k, *v; int64_t kv_row_stride; void *k_cache, *v_cache; const int32_t* slot_mapping;
+      int64_t T; int32_t Hkv, D, block_size; int64_t num_blocks;
+    } kv_write_fp4;
+    struct {
+      const void *k_cache, *v_cache; const int32_t *block_table, *cu_seqlens, *first_keys; void *k, *v;
+      int64_t kv_row_stride; int32_t B; int64_t total_tokens; int32_t Hkv, D, block_size, max_blocks_per_seq;
+      int64_t num_blocks;
+    } kv_read_fp4;
   } u;
 } opscale_op_desc;
 
@@ -554,8 +675,8 @@ typedef struct {
  * (flush_buf's contents are don't-care).
  * Each iteration is timed alone with device events.  Fills `out` with the
  * timing distribution, the algorithmic work and the roofline fraction against
- * MI355X peaks (bf16 matrix 2.5 PFLOP/s, fp32 matrix 157.3 TFLOP/s, HBM
- * 8 TB/s).  Blocking.  iters must be >= 1.
+ * MI355X peaks (bf16 matrix 2.5 PFLOP/s, fp32 matrix 157.3 TFLOP/s, the linear of
+ * e4m3 operands 5.0 PFLOP/s, HBM 8 TB/s).  Blocking.  iters must be >= 1.
  */
 opscale_status opscale_op_profile(const opscale_op_desc* desc, int32_t warmup, int32_t iters,
                                   void* flush_buf, size_t flush_bytes, hipStream_t stream,

@@ -3,8 +3,8 @@ ragged causal GQA prefill attention and paged decode attention, plus RoPE, the
 paged KV-cache write and residual-add RMSNorm, the mixture-of-experts FFN
 (top-k routing, fused expert MLPs), and the attention path of other layers (head
 norms with scaled and partial rotations, a step's tables, attention with score
-caps, distance biases, windows, prefixes and documents), as hand-written HIP
-kernels behind the C ABI in include/opscale.h.  This package holds the HIP sources
+caps, distance biases, windows, prefixes and documents), and the layer in fewer bits
+(linears of e4m3 operands, a KV cache in 4 bits), as hand-written HIP kernels behind the C ABI in include/opscale.h.  This package holds the HIP sources
 (csrc/), their build script, the ctypes binding, a layer chained from the
 entry points (layer), the operator profiler (profiler) and spatial sharing
 over CU-masked streams (spatial)."""
@@ -20,6 +20,9 @@ from ._lib import (  # noqa: F401
     desc_rmsnorm, desc_linear, desc_swiglu, desc_attn_prefill, desc_attn_decode,
     desc_rope, desc_reshape_and_cache, desc_add_rmsnorm,
     desc_qk_norm_rope, desc_block_tables, desc_attn_prefill_mod, desc_attn_decode_mod,
+    opscale_quantize_fp8, opscale_linear_fp8, opscale_linear_fp8_workspace_size, opscale_kv_write_fp4,
+    opscale_kv_read_fp4, opscale_attn_decode_fp4, opscale_attn_decode_fp4_workspace_size,
+    desc_quantize_fp8, desc_linear_fp8, desc_kv_write_fp4, desc_kv_read_fp4, desc_attn_decode_fp4,
     opscale_moe_topk, opscale_fused_moe_workspace_size, opscale_fused_moe, desc_fused_moe,
     Corun, opscale_cu_layout, opscale_cu_mask_build, opscale_cu_stream_create, opscale_cu_stream_destroy,
     opscale_cu_stream_mask, opscale_cu_probe, opscale_probe_mfma, opscale_probe_hbm, opscale_corun_profile,

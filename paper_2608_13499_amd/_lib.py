@@ -17,7 +17,8 @@ LIB_PATH = os.path.join(_HERE, "libopscale.so")
 OPSCALE_OK, OPSCALE_ERR_INVALID_ARG, OPSCALE_ERR_UNSUPPORTED, OPSCALE_ERR_WORKSPACE, OPSCALE_ERR_HIP = range(5)
 OPSCALE_F32, OPSCALE_BF16 = 0, 1
 (OP_RMSNORM, OP_LINEAR, OP_SWIGLU, OP_ATTN_PREFILL, OP_ATTN_DECODE, OP_ROPE, OP_RESHAPE_AND_CACHE,
- OP_ADD_RMSNORM, OP_FUSED_MOE, OP_QK_NORM_ROPE, OP_BLOCK_TABLES, OP_ATTN_PREFILL_MOD, OP_ATTN_DECODE_MOD) = range(13)
+ OP_ADD_RMSNORM, OP_FUSED_MOE, OP_QK_NORM_ROPE, OP_BLOCK_TABLES, OP_ATTN_PREFILL_MOD, OP_ATTN_DECODE_MOD,
+ OP_QUANTIZE_FP8, OP_LINEAR_FP8, OP_KV_WRITE_FP4, OP_KV_READ_FP4, OP_ATTN_DECODE_FP4) = range(18)
 (TUNE_GEMM_TILE, TUNE_GEMM_SKINNY, TUNE_GEMM_SPLITK, TUNE_GEMM_TAIL, TUNE_SKINNY_NG, TUNE_PREFILL_SCHEDULE,
  TUNE_MOE_FUSE, TUNE_GEMM_DECODE) = range(8)
 TUNE_AUTO = -1
@@ -114,12 +115,30 @@ class _DecodeModArgs(ctypes.Structure):
     _fields_ = [*_DecodeArgs._fields_[:-2], ("mods", AttnMods), *_DecodeArgs._fields_[-2:]]
 
 
+class _QuantizeFp8Args(ctypes.Structure):
+    _fields_ = [("x", c_vp), ("x_row_stride", c_i64), ("q", c_vp), ("scales", c_vp), ("M", c_i64), ("K", c_i64)]
+
+
+class _LinearFp8Args(ctypes.Structure):
+    _fields_ = [("x", c_vp), ("x_scales", c_vp), ("W", c_vp), ("w_scales", c_vp), ("bias", c_vp), ("y", c_vp),
+                ("M", c_i64), ("N", c_i64), ("K", c_i64), ("workspace", c_vp), ("workspace_bytes", c_sz)]
+
+
+class _KvReadFp4Args(ctypes.Structure):
+    _fields_ = [("k_cache", c_vp), ("v_cache", c_vp), ("block_table", c_vp), ("cu_seqlens", c_vp),
+                ("first_keys", c_vp), ("k", c_vp), ("v", c_vp), ("kv_row_stride", c_i64), ("B", c_i32),
+                ("total_tokens", c_i64), ("Hkv", c_i32), ("D", c_i32), ("block_size", c_i32),
+                ("max_blocks_per_seq", c_i32), ("num_blocks", c_i64)]
+
+
 class _OpUnion(ctypes.Union):
     _fields_ = [("rmsnorm", _RmsnormArgs), ("linear", _LinearArgs), ("swiglu", _SwigluArgs),
                 ("attn_prefill", _PrefillArgs), ("attn_decode", _DecodeArgs), ("rope", _RopeArgs),
                 ("reshape_and_cache", _CacheWriteArgs), ("add_rmsnorm", _AddRmsnormArgs),
                 ("fused_moe", _FusedMoeArgs), ("qk_norm_rope", _QkNormRopeArgs), ("block_tables", _BlockTablesArgs),
-                ("attn_prefill_mod", _PrefillModArgs), ("attn_decode_mod", _DecodeModArgs)]
+                ("attn_prefill_mod", _PrefillModArgs), ("attn_decode_mod", _DecodeModArgs),
+                ("quantize_fp8", _QuantizeFp8Args), ("linear_fp8", _LinearFp8Args), ("kv_write_fp4", _CacheWriteArgs),
+                ("kv_read_fp4", _KvReadFp4Args), ("attn_decode_fp4", _DecodeModArgs)]
 
 
 class OpDesc(ctypes.Structure):
@@ -187,6 +206,18 @@ EXPORTS = {
                                          ctypes.POINTER(Timing)]),
     "opscale_attn_decode_mod_workspace_size": (c_sz, [c_i32, c_i32, c_i32, c_i32]),
     "opscale_attn_decode_mod": (c_i32, [c_vp, c_i64, c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32,
+                                        c_i32, c_i64, c_i32, c_f32, ctypes.POINTER(AttnMods), c_i32, c_vp, c_sz, c_vp,
+                                        ctypes.POINTER(Timing)]),
+    "opscale_quantize_fp8": (c_i32, [c_vp, c_i64, c_vp, c_vp, c_i64, c_i64, c_i32, c_vp, ctypes.POINTER(Timing)]),
+    "opscale_linear_fp8_workspace_size": (c_sz, [c_i64, c_i64, c_i64, c_i32]),
+    "opscale_linear_fp8": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64, c_i64, c_i64, c_i32, c_vp, c_sz, c_vp,
+                                   ctypes.POINTER(Timing)]),
+    "opscale_kv_write_fp4": (c_i32, [c_vp, c_vp, c_i64, c_vp, c_vp, c_vp, c_i64, c_i32, c_i32, c_i32, c_i64, c_i32,
+                                     c_vp, ctypes.POINTER(Timing)]),
+    "opscale_kv_read_fp4": (c_i32, [c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64, c_i32, c_i64, c_i32, c_i32, c_i32,
+                                    c_i32, c_i64, c_i32, c_vp, ctypes.POINTER(Timing)]),
+    "opscale_attn_decode_fp4_workspace_size": (c_sz, [c_i32, c_i32, c_i32, c_i32]),
+    "opscale_attn_decode_fp4": (c_i32, [c_vp, c_i64, c_vp, c_vp, c_vp, c_vp, c_vp, c_i32, c_i32, c_i32, c_i32, c_i32,
                                         c_i32, c_i64, c_i32, c_f32, ctypes.POINTER(AttnMods), c_i32, c_vp, c_sz, c_vp,
                                         ctypes.POINTER(Timing)]),
     "opscale_rope_frequencies": (c_i32, [ctypes.POINTER(c_f64), ctypes.POINTER(c_f32), c_i32, c_f64, c_i32, c_f64,
@@ -742,6 +773,184 @@ def opscale_attn_decode_mod(q, k_cache, v_cache, block_table, context_lens, max_
     return (out, t) if timed else out
 
 
+# ----------------------------------------------------- the layer in fewer bits --
+_u8 = _e4m3 = None  # torch's dtypes, filled on first use
+
+
+def _current_narrow() -> int:
+    """The current GPU; fills the narrow dtypes."""
+    global _u8, _e4m3
+    if _u8 is None:
+        import torch
+        _u8, _e4m3 = torch.uint8, torch.float8_e4m3fn
+    return _current()
+
+
+def _matrix(name, t_, dtype, dev):
+    """(rows, columns, row stride) of t_ [M, K] with contiguous rows."""
+    if t_.dim() != 2 or t_.dtype != dtype or t_.get_device() != dev or (t_.stride(1) != 1 and t_.shape[1] > 1):
+        _refuse(name, t_, f"{dtype} [M, K] with contiguous rows", dev)
+    M, K = t_.shape
+    return M, K, t_.stride(0) if M > 1 else K
+
+
+def opscale_quantize_fp8(x, q=None, scales=None, stream=None, timed: bool = False):
+    """x [M, K] (rows may be strided) as float8_e4m3fn [M, K] and float32 power-of-two
+    scales [ceil(K / 128), M], one for each row and 128 of its elements.  Returns
+    (q, scales)."""
+    lib = load()
+    dev, dt = _current_narrow(), _dt(x)
+    M, K, xs = _matrix("x", x, x.dtype, dev)
+    nkb = (K + 127) // 128
+    if q is None:
+        q = x.new_empty((M, K), dtype=_e4m3)
+    if scales is None:
+        scales = x.new_empty((nkb, M), dtype=_f32)
+    t = Timing() if timed else None
+    _check(lib.opscale_quantize_fp8(x.data_ptr(), xs, _cache("q", q, (M, K), _e4m3, dev),
+                                    _cache("scales", scales, (nkb, M), _f32, dev), M, K, dt, _stream(stream),
+                                    ctypes.byref(t) if t else None))
+    return ((q, scales), t) if timed else (q, scales)
+
+
+def opscale_linear_fp8_workspace_size(M: int, N: int, K: int, dtype=None) -> int:
+    import torch
+    dt = OPSCALE_F32 if dtype == torch.float32 else OPSCALE_BF16
+    return load().opscale_linear_fp8_workspace_size(M, N, K, dt)
+
+
+def opscale_linear_fp8(x, x_scales, W, w_scales, bias=None, dtype=None, y=None, workspace=None, stream=None,
+                       timed: bool = False):
+    """y[M, N] = x[M, K] W[N, K]^T (+ bias) of float8_e4m3fn operands, x_scales float32
+    [ceil(K / 128), M] (opscale_quantize_fp8) and w_scales float32 [ceil(N / 128),
+    ceil(K / 128)].  dtype: of y and bias (y's, or bfloat16).  `workspace` (a uint8 GPU
+    tensor) is allocated by torch when None; False passes none."""
+    lib = load()
+    dev = _current_narrow()
+    if x.dim() != 2 or W.dim() != 2 or W.shape[1] != x.shape[1]:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"x {tuple(x.shape)} and W {tuple(W.shape)} must be [M, K] and [N, K]")
+    (M, K), N = x.shape, W.shape[0]
+    nkb, nnb = (K + 127) // 128, (N + 127) // 128
+    if y is None:
+        if dtype is None:
+            import torch
+            dtype = torch.bfloat16
+        y = x.new_empty((M, N), dtype=dtype)
+    elif dtype is not None and dtype != y.dtype:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"y is {y.dtype}, dtype {dtype}")
+    dt = _dt(y)
+    if workspace is None:
+        need = lib.opscale_linear_fp8_workspace_size(M, N, K, dt)
+        ws, nbytes = (_scratch(need, x, stream), need) if need else (None, 0)
+    elif workspace is False:
+        ws, nbytes = None, 0
+    else:
+        ws, nbytes = workspace, workspace.numel() * workspace.element_size()
+        _flat("workspace", ws, ws.numel(), ws.dtype, dev)
+    t = Timing() if timed else None
+    _check(lib.opscale_linear_fp8(_cache("x", x, (M, K), _e4m3, dev), _cache("x_scales", x_scales, (nkb, M), _f32, dev),
+                                  _cache("W", W, (N, K), _e4m3, dev),
+                                  _cache("w_scales", w_scales, (nnb, nkb), _f32, dev),
+                                  None if bias is None else _flat("bias", bias, N, y.dtype, dev),
+                                  _cache("y", y, (M, N), y.dtype, dev), M, N, K, dt, _ptr(ws), nbytes, _stream(stream),
+                                  ctypes.byref(t) if t else None))
+    return (y, t) if timed else y
+
+
+def _fp4_caches(k_cache, v_cache, dev):
+    """(num_blocks, block_size, Hkv, D, addresses) of uint8 caches [num_blocks, Hkv, block_size, D / 2 + D / 32]."""
+    if k_cache.dim() != 4 or k_cache.shape[3] * 32 % 17:
+        _refuse("k_cache", k_cache, "uint8 [num_blocks, Hkv, block_size, D / 2 + D / 32]", dev)
+    shape = nb, Hkv, bs, row = k_cache.shape
+    return nb, bs, Hkv, row * 32 // 17, _cache("k_cache", k_cache, shape, _u8, dev), _cache("v_cache", v_cache, shape, _u8, dev)
+
+
+def opscale_kv_write_fp4(k, v, k_cache, v_cache, slot_mapping, stream=None, timed: bool = False):
+    """Write k, v [T, Hkv, D] (token dimension may be strided) in 4 bits, with a scale for
+    each 32 elements, into paged caches, uint8 [num_blocks, Hkv, block_size, D / 2 + D /
+    32], at the int32 slots; slots outside the cache are skipped."""
+    lib = load()
+    dev, dt = _current_narrow(), _dt(k)
+    nb, bs, Hkv, D, kc, vc = _fp4_caches(k_cache, v_cache, dev)
+    shape = k.shape[0], Hkv, D
+    ks, vs = _rows("k", k, shape, k.dtype, dev), _rows("v", v, shape, k.dtype, dev)
+    if ks != vs:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "k and v must share a row stride")
+    t = Timing() if timed else None
+    _check(lib.opscale_kv_write_fp4(k.data_ptr(), v.data_ptr(), ks, kc, vc,
+                                    _flat("slot_mapping", slot_mapping, shape[0], _i32, dev), shape[0], Hkv, D, bs, nb,
+                                    dt, _stream(stream), ctypes.byref(t) if t else None))
+    return t if timed else None
+
+
+def opscale_kv_read_fp4(k_cache, v_cache, block_table, cu_seqlens, total_tokens: int, first_keys=None, dtype=None,
+                        k=None, v=None, stream=None, timed: bool = False):
+    """The rows of such caches, packed: rows cu_seqlens[b] .. cu_seqlens[b + 1] - 1 of k and
+    v [total_tokens, Hkv, D] are the keys of sequence b from first_keys[b] (int32, or 0)
+    on.  k and v (token dimension may be strided) or their dtype (bfloat16) may be given.
+    Returns (k, v)."""
+    lib = load()
+    dev = _current_narrow()
+    nb, bs, Hkv, D, kc, vc = _fp4_caches(k_cache, v_cache, dev)
+    shape = total_tokens, Hkv, D
+    if (k is None) != (v is None):
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "k and v are given both or neither")
+    if k is None:
+        if dtype is None:
+            import torch
+            dtype = torch.bfloat16
+        k, v = k_cache.new_empty(shape, dtype=dtype), k_cache.new_empty(shape, dtype=dtype)
+    elif dtype is not None and dtype != k.dtype:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"k is {k.dtype}, dtype {dtype}")
+    dt = _dt(k)
+    ks, vs = _rows("k", k, shape, k.dtype, dev), _rows("v", v, shape, k.dtype, dev)
+    if ks != vs:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "k and v must share a row stride")
+    if block_table.dim() != 2:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "block_table must be [B, max_blocks_per_seq]")
+    B, cols = block_table.shape
+    first = None if first_keys is None else _flat("first_keys", first_keys, B, _i32, dev)
+    t = Timing() if timed else None
+    _check(lib.opscale_kv_read_fp4(kc, vc, _flat("block_table", block_table, B * cols, _i32, dev),
+                                   _flat("cu_seqlens", cu_seqlens, B + 1, _i32, dev), first, k.data_ptr(), v.data_ptr(),
+                                   ks, B, total_tokens, Hkv, D, bs, cols, nb, dt, _stream(stream),
+                                   ctypes.byref(t) if t else None))
+    return ((k, v), t) if timed else (k, v)
+
+
+def opscale_attn_decode_fp4_workspace_size(B: int, Hq: int, D: int, max_context_len: int) -> int:
+    return int(load().opscale_attn_decode_fp4_workspace_size(B, Hq, D, max_context_len))
+
+
+def opscale_attn_decode_fp4(q, k_cache, v_cache, block_table, context_lens, max_context_len: int, scale: float,
+                            softcap: float = 0.0, slopes=None, window: int = 0, prefix_lens=None, doc_starts=None,
+                            workspace=None, out=None, stream=None, timed: bool = False):
+    """opscale_attn_decode_mod over caches in 4 bits (opscale_kv_write_fp4)."""
+    lib = load()
+    dt, dtype = _dt(q), q.dtype
+    dev = _current_narrow()
+    nb, bs, Hkv, D, kc, vc = _fp4_caches(k_cache, v_cache, dev)
+    if q.dim() != 3 or q.shape[2] != D or block_table.dim() != 2:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"q must be [B, Hq, {D}], block_table [B, max_blocks]")
+    shape = B, Hq, D = q.shape
+    qs = _rows("q", q, shape, dtype, dev)
+    cols = block_table.shape[1]
+    table = _flat("block_table", block_table, B * cols, _i32, dev)
+    ctx = _flat("context_lens", context_lens, B, _i32, dev)
+    mods = _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, B, dev)
+    if out is None:
+        out = q.new_empty(shape)
+    if workspace is None:
+        workspace = _scratch(lib.opscale_attn_decode_fp4_workspace_size(B, Hq, D, max_context_len), q, stream)
+    nbytes = workspace.numel() * workspace.element_size()
+    t = Timing() if timed else None
+    _check(lib.opscale_attn_decode_fp4(q.data_ptr(), qs, kc, vc, table, ctx, _flat("out", out, B * Hq * D, dtype, dev),
+                                       B, Hq, Hkv, D, bs, cols, nb, max_context_len, scale, mods, dt,
+                                       _flat("workspace", workspace, workspace.numel(), workspace.dtype, dev), nbytes,
+                                       _stream(stream), ctypes.byref(t) if t else None))
+    return (out, t) if timed else out
+
+
 def opscale_block_tables(context_lens, new_lens, block_table, free_blocks, free_begin, block_size: int,
                          max_tokens: int, out=None, stream=None, timed: bool = False):
     """The tables of a step: request b has context_lens[b] tokens in the cache and
@@ -1051,6 +1260,54 @@ def desc_attn_decode_mod(q, k_cache, v_cache, block_table, context_lens, out, ma
     nb, bs, Hkv, _ = k_cache.shape
     _heads_view("q", q, Hq, D)
     d.u.attn_decode_mod = _DecodeModArgs(_ptr(q), q.stride(0), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
+                                         _ptr(context_lens), _ptr(out), B, Hq, Hkv, D, bs, block_table.shape[1], nb,
+                                         max_context_len, scale,
+                                         AttnMods(softcap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(doc_starts)),
+                                         _ptr(workspace), workspace.numel() * workspace.element_size())
+    return d
+
+
+def desc_quantize_fp8(x, q, scales) -> OpDesc:
+    d = OpDesc(op=OP_QUANTIZE_FP8, dt=_dt(x))
+    M, K = x.shape
+    d.u.quantize_fp8 = _QuantizeFp8Args(_ptr(x), x.stride(0), _ptr(q), _ptr(scales), M, K)
+    return d
+
+
+def desc_linear_fp8(x, x_scales, W, w_scales, y, bias=None, workspace=None) -> OpDesc:
+    d = OpDesc(op=OP_LINEAR_FP8, dt=_dt(y))
+    M, K = x.shape
+    d.u.linear_fp8 = _LinearFp8Args(_ptr(x), _ptr(x_scales), _ptr(W), _ptr(w_scales), _ptr(bias), _ptr(y), M, W.shape[0],
+                                    K, _ptr(workspace),
+                                    0 if workspace is None else workspace.numel() * workspace.element_size())
+    return d
+
+
+def desc_kv_write_fp4(k, v, k_cache, v_cache, slot_mapping) -> OpDesc:
+    d = OpDesc(op=OP_KV_WRITE_FP4, dt=_dt(k))
+    T, Hkv, D = k.shape
+    d.u.kv_write_fp4 = _CacheWriteArgs(_ptr(k), _ptr(v), k.stride(0), _ptr(k_cache), _ptr(v_cache), _ptr(slot_mapping), T,
+                                       Hkv, D, k_cache.shape[2], k_cache.shape[0])
+    return d
+
+
+def desc_kv_read_fp4(k_cache, v_cache, block_table, cu_seqlens, k, v, first_keys=None) -> OpDesc:
+    d = OpDesc(op=OP_KV_READ_FP4, dt=_dt(k))
+    T, Hkv, D = k.shape
+    B, cols = block_table.shape
+    d.u.kv_read_fp4 = _KvReadFp4Args(_ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(cu_seqlens), _ptr(first_keys),
+                                     _ptr(k), _ptr(v), k.stride(0), B, T, Hkv, D, k_cache.shape[2], cols,
+                                     k_cache.shape[0])
+    return d
+
+
+def desc_attn_decode_fp4(q, k_cache, v_cache, block_table, context_lens, out, max_context_len, scale, workspace,
+                         softcap=0.0, slopes=None, window=0, prefix_lens=None, doc_starts=None) -> OpDesc:
+    d = OpDesc(op=OP_ATTN_DECODE_FP4, dt=_dt(q))
+    B, Hq, D = q.shape
+    nb, Hkv, bs, _ = k_cache.shape
+    _heads_view("q", q, Hq, D)
+    d.u.attn_decode_fp4 = _DecodeModArgs(_ptr(q), q.stride(0), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
                                          _ptr(context_lens), _ptr(out), B, Hq, Hkv, D, bs, block_table.shape[1], nb,
                                          max_context_len, scale,
                                          AttnMods(softcap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(doc_starts)),

@@ -65,6 +65,9 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 
 int esize(opscale_dtype dt) { return dt == OPSCALE_BF16 ? 2 : 4; }
 
+// Bytes of a slot and head of a cache in 4 bits.
+int64_t fp4_row(int64_t D) { return D / 2 + D / 32; }
+
 bool dtype_ok(opscale_dtype dt) { return dt == OPSCALE_F32 || dt == OPSCALE_BF16; }
 
 // [a, a+na) and [b, b+nb) overlap?
@@ -180,7 +183,7 @@ Work work_decode(const std::vector<int32_t>& ctx, int64_t Hq, int64_t Hkv, int64
 
 Work work_decode_mod(const std::vector<int32_t>& ctx, const std::vector<int32_t>& prefix,
                      const std::vector<int32_t>& starts, int64_t window, int64_t Hq, int64_t Hkv, int64_t D, int s,
-                     int64_t bs, int64_t max_blocks) {
+                     int64_t row_bytes, int64_t bs, int64_t max_blocks) {
   double keys = 0, pages = 0;
   const int64_t B = (int64_t)ctx.size();
   for (int64_t b = 0; b < B; ++b) {
@@ -191,7 +194,7 @@ Work work_decode_mod(const std::vector<int32_t>& ctx, const std::vector<int32_t>
     keys += (double)seen;
     pages += (double)((seen + bs - 1) / bs);
   }
-  const double by = s * (2.0 * Hkv * D * keys + 2.0 * B * Hq * D) + 4.0 * (pages + B);
+  const double by = 2.0 * Hkv * (double)row_bytes * keys + 2.0 * s * B * Hq * D + 4.0 * (pages + B);
   return {4.0 * D * Hq * keys, by, 0, (int64_t)by, s * B * Hq * D};
 }
 
@@ -248,6 +251,21 @@ Work work_fused_moe(const std::vector<int32_t>& ids, int64_t T, int64_t H, int64
   const double by = (double)weight + 2.0 * s * T * H + 8.0 * (double)ids.size();
   return {pairs * (6.0 * H * F + 6.0 * F), by, weight, (int64_t)s * T * H + 8 * (int64_t)ids.size(),
           (int64_t)s * T * H};
+}
+
+Work work_quantize_fp8(int64_t M, int64_t K, int s) {
+  const int64_t out = M * K + 4 * M * ((K + 127) / 128);
+  return {2.0 * M * K, (double)(s * M * K + out), 0, s * M * K + out, out};
+}
+Work work_linear_fp8(int64_t M, int64_t N, int64_t K, int s, bool bias) {
+  const int64_t nkb = (K + 127) / 128, weight = N * K + 4 * nkb * ((N + 127) / 128) + (bias ? s * N : 0);
+  const int64_t moved = M * K + 4 * nkb * M + s * M * N;
+  return {2.0 * M * N * K, (double)(weight + moved), weight, moved, s * M * N};
+}
+// (cached: bytes of a slot and head)
+Work work_kv_fp4(int64_t T, int64_t Hkv, int64_t D, int s, int64_t cached, int64_t indices, bool write) {
+  const int64_t dense = 2 * s * T * Hkv * D, held = 2 * T * Hkv * cached;
+  return {2.0 * T * Hkv * D, (double)(dense + held + 4 * indices), 0, dense + held, write ? 0 : dense};
 }
 
 opscale_status copy_ints(std::vector<int32_t>& dst, const int32_t* src, int64_t n, hipStream_t s) {
@@ -421,23 +439,25 @@ opscale_status check_decode(const void* q, int64_t qs, const void* kc, const voi
   return OPSCALE_OK;
 }
 
-opscale_status check_decode_mod(const void* q, int64_t qs, const void* kc, const void* vc, const int32_t* table,
-                                const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t bs,
-                                int32_t max_blocks, int64_t num_blocks, int32_t max_ctx, float scale,
-                                const opscale_attn_mods* m, opscale_dtype dt, void* ws, size_t ws_bytes) {
+// row_bytes: of a slot and head in each cache
+opscale_status check_decode_cached(const char* who, const void* q, int64_t qs, const void* kc, const void* vc,
+                                   const int32_t* table, const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv,
+                                   int32_t D, int32_t bs, int32_t max_blocks, int64_t num_blocks, int32_t max_ctx,
+                                   float scale, const opscale_attn_mods* m, opscale_dtype dt, void* ws, size_t ws_bytes,
+                                   int64_t row_bytes) {
   opscale_status st = check_decode(q, qs, kc, vc, table, ctx, o, B, Hq, Hkv, D, bs, max_blocks, num_blocks, max_ctx,
                                    scale, dt, ws, ws_bytes, true);
-  if (st == OPSCALE_OK) st = check_mods("attn_decode_mod", m);
+  if (st == OPSCALE_OK) st = check_mods(who, m);
   if (st != OPSCALE_OK || B == 0) return st;
   const int s = esize(dt);
   if ((int64_t)max_blocks * bs > kMaxDim - 1024 || num_blocks > kMaxDim || num_blocks * bs > ((int64_t)1 << 36))
-    return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: max_blocks_per_seq=%d num_blocks=%lld of %d (at most 2^31 - 1024 "
-                "keys a sequence, 2^31 blocks and 2^36 slots)", max_blocks, (long long)num_blocks, bs);
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: max_blocks_per_seq=%d num_blocks=%lld of %d (at most 2^31 - 1024 "
+                "keys a sequence, 2^31 blocks and 2^36 slots)", who, max_blocks, (long long)num_blocks, bs);
   struct Range {
     const void* p;
     int64_t n;
   };
-  const int64_t cache = num_blocks * bs * Hkv * D * s;
+  const int64_t cache = num_blocks * bs * Hkv * row_bytes;
   const Range in[] = {{q, ((B - 1) * qs + (int64_t)Hq * D) * s}, {kc, cache}, {vc, cache}, {table, 4ll * B * max_blocks},
                       {ctx, 4ll * B}, {m ? m->slopes : nullptr, 4ll * Hq}, {m ? m->prefix_lens : nullptr, 4ll * B},
                       {m ? m->doc_starts : nullptr, 4ll * B}};
@@ -445,10 +465,38 @@ opscale_status check_decode_mod(const void* q, int64_t qs, const void* kc, const
   const Range work{ws, (int64_t)opscale::decode_mod_workspace_bytes(B, Hq, D, max_ctx)};
   for (const Range& r : in)
     if (r.p && (overlap(r.p, r.n, out.p, out.n) || overlap(r.p, r.n, work.p, work.n)))
-      return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: o and the workspace must not overlap an input");
+      return fail(OPSCALE_ERR_INVALID_ARG, "%s: o and the workspace must not overlap an input", who);
   if (overlap(out.p, out.n, work.p, work.n))
-    return fail(OPSCALE_ERR_INVALID_ARG, "attn_decode_mod: o overlaps the workspace");
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: o overlaps the workspace", who);
   return OPSCALE_OK;
+}
+
+opscale_status check_decode_mod(const void* q, int64_t qs, const void* kc, const void* vc, const int32_t* table,
+                                const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t bs,
+                                int32_t max_blocks, int64_t num_blocks, int32_t max_ctx, float scale,
+                                const opscale_attn_mods* m, opscale_dtype dt, void* ws, size_t ws_bytes) {
+  return check_decode_cached("attn_decode_mod", q, qs, kc, vc, table, ctx, o, B, Hq, Hkv, D, bs, max_blocks, num_blocks,
+                             max_ctx, scale, m, dt, ws, ws_bytes, (int64_t)D * esize(dt));
+}
+
+// Heads, pages and sizes of such a cache.
+opscale_status check_fp4_cache(const char* who, int32_t Hkv, int32_t D, int32_t bs) {
+  if (Hkv <= 0 || D <= 0 || (int64_t)Hkv * D > (1 << 20))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes Hkv=%d D=%d", who, Hkv, D);
+  if (D != 64 && D != 128) return fail(OPSCALE_ERR_UNSUPPORTED, "%s: head_dim %d (supported: 64, 128)", who, D);
+  if (bs < 16 || bs > 1024 || (bs & (bs - 1)))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: block_size %d must be a power of two in [16, 1024]", who, bs);
+  return OPSCALE_OK;
+}
+
+opscale_status check_decode_fp4(const void* q, int64_t qs, const void* kc, const void* vc, const int32_t* table,
+                                const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t bs,
+                                int32_t max_blocks, int64_t num_blocks, int32_t max_ctx, float scale,
+                                const opscale_attn_mods* m, opscale_dtype dt, void* ws, size_t ws_bytes) {
+  const opscale_status st = check_fp4_cache("attn_decode_fp4", Hkv, D, bs);
+  if (st != OPSCALE_OK) return st;
+  return check_decode_cached("attn_decode_fp4", q, qs, kc, vc, table, ctx, o, B, Hq, Hkv, D, bs, max_blocks, num_blocks,
+                             max_ctx, scale, m, dt, ws, ws_bytes, fp4_row(D));
 }
 
 opscale_status check_rope(void* q, void* k, int64_t qs, int64_t ks, const int32_t* pos, int64_t T, int32_t Hq,
@@ -616,6 +664,117 @@ opscale_status check_block_tables(const int32_t* ctx, const int32_t* fresh, int3
   return OPSCALE_OK;
 }
 
+opscale_status check_quantize_fp8(const void* x, int64_t xs, const void* q, const float* scales, int64_t M, int64_t K,
+                                  opscale_dtype dt) {
+  const char* who = "quantize_fp8";
+  if (!dtype_ok(dt)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, (int)dt);
+  const int s = esize(dt);
+  if (M < 0 || K <= 0 || M >= kMaxDim || K > (1 << 20) || K % 16 || (M + 15) / 16 * ((K + 511) / 512) >= kMaxDim)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes M=%lld K=%lld (K a multiple of 16, up to 2^20)", who, (long long)M,
+                (long long)K);
+  if (M == 0) return OPSCALE_OK;
+  if (xs < K || xs * s % 16 || xs > ((int64_t)1 << 32))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: x_row_stride=%lld must cover a row and be a multiple of 16 bytes", who,
+                (long long)xs);
+  if (!x || !q || !scales) return fail(OPSCALE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (!aligned16(x) || !aligned16(q) || (reinterpret_cast<uintptr_t>(scales) & 3))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: x and q must be 16-byte aligned, scales 4-byte", who);
+  const int64_t nx = ((M - 1) * xs + K) * s, nq = M * K, nsc = 4 * M * ((K + 127) / 128);
+  if (overlap(q, nq, x, nx) || overlap(scales, nsc, x, nx) || overlap(q, nq, scales, nsc))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: x, q and scales must not overlap", who);
+  return OPSCALE_OK;
+}
+
+opscale_status check_linear_fp8(const void* x, const float* xs, const void* W, const float* ws, const void* bias, void* y,
+                                int64_t M, int64_t N, int64_t K, opscale_dtype dt, const void* work, size_t work_bytes,
+                                opscale::LinearFp8Plan* plan) {
+  const char* who = "linear_fp8";
+  if (!dtype_ok(dt)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, (int)dt);
+  const int s = esize(dt);
+  if (M < 0 || N <= 0 || K <= 0 || M >= (1 << 30) || N >= (1 << 30) || K > (1 << 20) || M > ((int64_t)1 << 40) / N)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes M=%lld N=%lld K=%lld", who, (long long)M, (long long)N, (long long)K);
+  if (K % 16 || N * s % 16)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: K and N times sizeof(dt) must be multiples of 16 (K=%lld N=%lld)", who,
+                (long long)K, (long long)N);
+  if (M == 0) return OPSCALE_OK;
+  if (!x || !xs || !W || !ws || !y) return fail(OPSCALE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (!aligned16(x) || !aligned16(W) || !aligned16(y) || (bias && !aligned16(bias)) ||
+      ((reinterpret_cast<uintptr_t>(xs) | reinterpret_cast<uintptr_t>(ws)) & 3))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: x, W, bias and y must be 16-byte aligned, scales 4-byte", who);
+  struct Range {
+    const void* p;
+    int64_t n;
+  };
+  const int64_t nkb = (K + 127) / 128, ny = M * N * s;
+  const Range in[] = {{x, M * K}, {W, N * K}, {xs, 4 * nkb * M}, {ws, 4 * nkb * ((N + 127) / 128)}, {bias, N * s}};
+  for (const Range& r : in)
+    if (r.p && overlap(y, ny, r.p, r.n)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: y must not overlap an input", who);
+  *plan = opscale::plan_linear_fp8(M, N, K, work != nullptr);
+  if (plan->ws_bytes > 0) {
+    if (work_bytes < plan->ws_bytes)
+      return fail(OPSCALE_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, work_bytes, plan->ws_bytes);
+    if (!aligned16(work)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: workspace must be 16-byte aligned", who);
+    const int64_t nw = (int64_t)plan->ws_bytes;
+    bool bad = overlap(work, nw, y, ny);
+    for (const Range& r : in) bad = bad || (r.p && overlap(work, nw, r.p, r.n));
+    if (bad) return fail(OPSCALE_ERR_INVALID_ARG, "%s: the workspace overlaps a tensor", who);
+  }
+  return OPSCALE_OK;
+}
+
+opscale_status check_kv_write_fp4(const void* k, const void* v, int64_t kvs, const void* kc, const void* vc,
+                                  const int32_t* slots, int64_t T, int32_t Hkv, int32_t D, int32_t bs, int64_t nb,
+                                  opscale_dtype dt) {
+  const char* who = "kv_write_fp4";
+  if (!dtype_ok(dt)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, (int)dt);
+  const opscale_status st = check_fp4_cache(who, Hkv, D, bs);
+  if (st != OPSCALE_OK) return st;
+  const int s = esize(dt);
+  if (T < 0 || T >= kMaxDim || nb < 1 || nb >= kMaxDim / bs)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes T=%lld num_blocks=%lld of %d", who, (long long)T, (long long)nb, bs);
+  if (T == 0) return OPSCALE_OK;
+  if (kvs < (int64_t)Hkv * D || kvs * s % 16 || kvs > ((int64_t)1 << 32))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: kv_row_stride=%lld must cover the heads and be a multiple of 16 bytes", who,
+                (long long)kvs);
+  if (!k || !v || !kc || !vc || !slots) return fail(OPSCALE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (!aligned16(k) || !aligned16(v) || !aligned16(kc) || !aligned16(vc) || (reinterpret_cast<uintptr_t>(slots) & 3))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned, slots 4-byte", who);
+  const int64_t cache = nb * bs * Hkv * fp4_row(D), in = ((T - 1) * kvs + (int64_t)Hkv * D) * s;
+  bool bad = overlap(kc, cache, vc, cache);
+  for (const void* c : {kc, vc}) bad = bad || overlap(c, cache, k, in) || overlap(c, cache, v, in) || overlap(c, cache, slots, 4 * T);
+  if (bad) return fail(OPSCALE_ERR_INVALID_ARG, "%s: the caches must not overlap another tensor", who);
+  return OPSCALE_OK;
+}
+
+opscale_status check_kv_read_fp4(const void* kc, const void* vc, const int32_t* table, const int32_t* cu,
+                                 const int32_t* first, const void* k, const void* v, int64_t kvs, int32_t B, int64_t T,
+                                 int32_t Hkv, int32_t D, int32_t bs, int32_t max_blocks, int64_t nb, opscale_dtype dt) {
+  const char* who = "kv_read_fp4";
+  if (!dtype_ok(dt)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, (int)dt);
+  const opscale_status st = check_fp4_cache(who, Hkv, D, bs);
+  if (st != OPSCALE_OK) return st;
+  const int s = esize(dt);
+  if (B < 0 || T < 0 || T >= kMaxDim)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes B=%d total_tokens=%lld", who, B, (long long)T);
+  if (B == 0 || T == 0) return OPSCALE_OK;
+  if (max_blocks < 1 || nb < 1 || nb > kMaxDim || nb * bs > ((int64_t)1 << 36))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: max_blocks_per_seq=%d num_blocks=%lld of %d", who, max_blocks, (long long)nb, bs);
+  if (kvs < (int64_t)Hkv * D || kvs * s % 16 || kvs > ((int64_t)1 << 32))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: kv_row_stride=%lld must cover the heads and be a multiple of 16 bytes", who,
+                (long long)kvs);
+  if (!kc || !vc || !table || !cu || !k || !v) return fail(OPSCALE_ERR_INVALID_ARG, "%s: null pointer", who);
+  if (!aligned16(k) || !aligned16(v) || !aligned16(kc) || !aligned16(vc) ||
+      ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(cu) | reinterpret_cast<uintptr_t>(first)) & 3))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: tensors must be 16-byte aligned, indices 4-byte", who);
+  const int64_t cache = nb * bs * Hkv * fp4_row(D), row = (int64_t)Hkv * D * s, out = (T - 1) * kvs * s + row;
+  bool bad = rows_overlap(k, kvs * s, row, v, kvs * s, row, T);
+  for (const void* o : {k, v})
+    bad = bad || overlap(o, out, kc, cache) || overlap(o, out, vc, cache) || overlap(o, out, table, 4ll * B * max_blocks) ||
+          overlap(o, out, cu, 4ll * (B + 1)) || (first && overlap(o, out, first, 4ll * B));
+  if (bad) return fail(OPSCALE_ERR_INVALID_ARG, "%s: k and v must not overlap another tensor", who);
+  return OPSCALE_OK;
+}
+
 opscale_status check_add_rmsnorm(const void* x, void* res, const void* w, void* y, int64_t M, int64_t H, float eps,
                                  opscale_dtype dt) {
   opscale_status st = check_rmsnorm(x, w, y, M, H, eps, dt);
@@ -683,13 +842,14 @@ opscale_status work_of_prefill_mod(const int32_t* cu_seqlens, int32_t B, int64_t
 }
 opscale_status work_of_decode_mod(const int32_t* context_lens, int32_t B, int32_t Hq, int32_t Hkv, int32_t D, int32_t bs,
                                   int32_t max_blocks, const opscale_attn_mods* m, opscale_dtype dt, hipStream_t stream,
-                                  Work* wk) {
+                                  Work* wk, bool fp4 = false) {
   std::vector<int32_t> ctx, prefix, starts;
   opscale_status st = copy_ints(ctx, context_lens, B, stream);
   if (st == OPSCALE_OK && m && m->prefix_lens) st = copy_ints(prefix, m->prefix_lens, B, stream);
   if (st == OPSCALE_OK && m && m->doc_starts) st = copy_ints(starts, m->doc_starts, B, stream);
   if (st == OPSCALE_OK)
-    *wk = work_decode_mod(ctx, prefix, starts, m ? m->window : 0, Hq, Hkv, D, esize(dt), bs, max_blocks);
+    *wk = work_decode_mod(ctx, prefix, starts, m ? m->window : 0, Hq, Hkv, D, esize(dt),
+                          fp4 ? fp4_row(D) : (int64_t)D * esize(dt), bs, max_blocks);
   return st;
 }
 
@@ -1062,6 +1222,122 @@ opscale_status opscale_attn_decode_mod(const void* q, int64_t q_row_stride, cons
   return st;
 }
 
+opscale_status opscale_quantize_fp8(const void* x, int64_t x_row_stride, void* q, float* scales, int64_t M, int64_t K,
+                                    opscale_dtype dt, hipStream_t stream, opscale_timing* timing) {
+  opscale_status st = check_quantize_fp8(x, x_row_stride, q, scales, M, K, dt);
+  if (st != OPSCALE_OK) return st;
+  zero_timing(timing);
+  if (M == 0) return OPSCALE_OK;
+  st = run_timed(stream, timing, "quantize_fp8 launch", [&] {
+    return opscale::launch_quantize_fp8(x, x_row_stride, q, scales, M, K, dt == OPSCALE_BF16, stream);
+  });
+  if (st == OPSCALE_OK && timing) {
+    const Work wk = work_quantize_fp8(M, K, esize(dt));
+    timing->alg_flops = wk.flops;
+    timing->alg_bytes = wk.bytes;
+  }
+  return st;
+}
+
+size_t opscale_linear_fp8_workspace_size(int64_t M, int64_t N, int64_t K, opscale_dtype dt) {
+  if (M <= 0 || N <= 0 || K <= 0 || !dtype_ok(dt)) return 0;
+  return opscale::plan_linear_fp8(M, N, K, true).ws_bytes;
+}
+
+opscale_status opscale_linear_fp8(const void* x, const float* x_scales, const void* W, const float* w_scales,
+                                  const void* bias, void* y, int64_t M, int64_t N, int64_t K, opscale_dtype dt,
+                                  void* workspace, size_t workspace_bytes, hipStream_t stream, opscale_timing* timing) {
+  opscale::LinearFp8Plan plan{};
+  opscale_status st = check_linear_fp8(x, x_scales, W, w_scales, bias, y, M, N, K, dt, workspace, workspace_bytes, &plan);
+  if (st != OPSCALE_OK) return st;
+  zero_timing(timing);
+  if (M == 0) return OPSCALE_OK;
+  st = run_timed(stream, timing, "linear_fp8 launch", [&] {
+    return opscale::launch_linear_fp8(plan, x, x_scales, W, w_scales, bias, y, M, N, K, dt == OPSCALE_BF16, workspace,
+                                      stream);
+  });
+  if (st == OPSCALE_OK && timing) {
+    const Work wk = work_linear_fp8(M, N, K, esize(dt), bias != nullptr);
+    timing->alg_flops = wk.flops;
+    timing->alg_bytes = wk.bytes;
+  }
+  return st;
+}
+
+opscale_status opscale_kv_write_fp4(const void* k, const void* v, int64_t kv_row_stride, void* k_cache, void* v_cache,
+                                    const int32_t* slot_mapping, int64_t T, int32_t Hkv, int32_t D, int32_t block_size,
+                                    int64_t num_blocks, opscale_dtype dt, hipStream_t stream, opscale_timing* timing) {
+  opscale_status st = check_kv_write_fp4(k, v, kv_row_stride, k_cache, v_cache, slot_mapping, T, Hkv, D, block_size,
+                                         num_blocks, dt);
+  if (st != OPSCALE_OK) return st;
+  zero_timing(timing);
+  if (T == 0) return OPSCALE_OK;
+  st = run_timed(stream, timing, "kv_write_fp4 launch", [&] {
+    return opscale::launch_kv_write_fp4(k, v, kv_row_stride, k_cache, v_cache, slot_mapping, T, Hkv, D, block_size,
+                                        num_blocks, dt == OPSCALE_BF16, stream);
+  });
+  if (st == OPSCALE_OK && timing) {
+    const Work wk = work_kv_fp4(T, Hkv, D, esize(dt), fp4_row(D), T, true);
+    timing->alg_flops = wk.flops;
+    timing->alg_bytes = wk.bytes;
+  }
+  return st;
+}
+
+opscale_status opscale_kv_read_fp4(const void* k_cache, const void* v_cache, const int32_t* block_table,
+                                   const int32_t* cu_seqlens, const int32_t* first_keys, void* k, void* v,
+                                   int64_t kv_row_stride, int32_t B, int64_t total_tokens, int32_t Hkv, int32_t D,
+                                   int32_t block_size, int32_t max_blocks_per_seq, int64_t num_blocks, opscale_dtype dt,
+                                   hipStream_t stream, opscale_timing* timing) {
+  opscale_status st = check_kv_read_fp4(k_cache, v_cache, block_table, cu_seqlens, first_keys, k, v, kv_row_stride, B,
+                                        total_tokens, Hkv, D, block_size, max_blocks_per_seq, num_blocks, dt);
+  if (st != OPSCALE_OK) return st;
+  zero_timing(timing);
+  if (B == 0 || total_tokens == 0) return OPSCALE_OK;
+  st = run_timed(stream, timing, "kv_read_fp4 launch", [&] {
+    return opscale::launch_kv_read_fp4(k_cache, v_cache, block_table, cu_seqlens, first_keys, k, v, kv_row_stride, B,
+                                       total_tokens, Hkv, D, block_size, max_blocks_per_seq, num_blocks,
+                                       dt == OPSCALE_BF16, stream);
+  });
+  if (st == OPSCALE_OK && timing) {
+    const Work wk = work_kv_fp4(total_tokens, Hkv, D, esize(dt), fp4_row(D), total_tokens / block_size + 2ll * B, false);
+    timing->alg_flops = wk.flops;
+    timing->alg_bytes = wk.bytes;
+  }
+  return st;
+}
+
+size_t opscale_attn_decode_fp4_workspace_size(int32_t B, int32_t Hq, int32_t D, int32_t max_context_len) {
+  return opscale_attn_decode_mod_workspace_size(B, Hq, D, max_context_len);
+}
+
+opscale_status opscale_attn_decode_fp4(const void* q, int64_t q_row_stride, const void* k_cache, const void* v_cache,
+                                       const int32_t* block_table, const int32_t* context_lens, void* o, int32_t B,
+                                       int32_t Hq, int32_t Hkv, int32_t D, int32_t block_size,
+                                       int32_t max_blocks_per_seq, int64_t num_blocks, int32_t max_context_len,
+                                       float scale, const opscale_attn_mods* mods, opscale_dtype dt, void* workspace,
+                                       size_t workspace_bytes, hipStream_t stream, opscale_timing* timing) {
+  opscale_status st = check_decode_fp4(q, q_row_stride, k_cache, v_cache, block_table, context_lens, o, B, Hq, Hkv, D,
+                                       block_size, max_blocks_per_seq, num_blocks, max_context_len, scale, mods, dt,
+                                       workspace, workspace_bytes);
+  if (st != OPSCALE_OK) return st;
+  zero_timing(timing);
+  if (B == 0) return OPSCALE_OK;
+  st = run_timed(stream, timing, "attn_decode_fp4 launch", [&] {
+    return opscale::launch_attn_decode_fp4(q, q_row_stride, k_cache, v_cache, block_table, context_lens, o, B, Hq, Hkv,
+                                           D, block_size, max_blocks_per_seq, num_blocks, max_context_len, scale, mods,
+                                           dt == OPSCALE_BF16, workspace, stream);
+  });
+  if (st == OPSCALE_OK && timing) {
+    Work wk{};
+    st = work_of_decode_mod(context_lens, B, Hq, Hkv, D, block_size, max_blocks_per_seq, mods, dt, stream, &wk, true);
+    if (st != OPSCALE_OK) return st;
+    timing->alg_flops = wk.flops;
+    timing->alg_bytes = wk.bytes;
+  }
+  return st;
+}
+
 opscale_status opscale_rope_frequencies(double* inv_freq, float* magnitude, int32_t rot, double theta,
                                         opscale_rope_scaling scaling, double factor, double low, double high,
                                         int64_t original_len) {
@@ -1383,6 +1659,74 @@ opscale_status prepare_op(const opscale_op_desc* d, hipStream_t stream, const ch
       if (st != OPSCALE_OK) return st;
       break;
     }
+    case OPSCALE_OP_QUANTIZE_FP8: {
+      const auto& a = d->u.quantize_fp8;
+      st = check_quantize_fp8(a.x, a.x_row_stride, a.q, a.scales, a.M, a.K, dt);
+      if (st != OPSCALE_OK) return st;
+      if (a.M == 0) return fail(OPSCALE_ERR_INVALID_ARG, "%s: empty problem", who);
+      launch = [=] { return opscale::launch_quantize_fp8(a.x, a.x_row_stride, a.q, a.scales, a.M, a.K, bf16, stream); };
+      wk = work_quantize_fp8(a.M, a.K, esize(dt));
+      break;
+    }
+    case OPSCALE_OP_LINEAR_FP8: {
+      const auto& a = d->u.linear_fp8;
+      opscale::LinearFp8Plan plan{};
+      st = check_linear_fp8(a.x, a.x_scales, a.W, a.w_scales, a.bias, a.y, a.M, a.N, a.K, dt, a.workspace,
+                            a.workspace_bytes, &plan);
+      if (st != OPSCALE_OK) return st;
+      if (a.M == 0) return fail(OPSCALE_ERR_INVALID_ARG, "%s: empty problem", who);
+      launch = [=] {
+        return opscale::launch_linear_fp8(plan, a.x, a.x_scales, a.W, a.w_scales, a.bias, a.y, a.M, a.N, a.K, bf16,
+                                          a.workspace, stream);
+      };
+      wk = work_linear_fp8(a.M, a.N, a.K, esize(dt), a.bias != nullptr);
+      break;
+    }
+    case OPSCALE_OP_KV_WRITE_FP4: {
+      const auto& a = d->u.kv_write_fp4;
+      st = check_kv_write_fp4(a.k, a.v, a.kv_row_stride, a.k_cache, a.v_cache, a.slot_mapping, a.T, a.Hkv, a.D,
+                              a.block_size, a.num_blocks, dt);
+      if (st != OPSCALE_OK) return st;
+      if (a.T == 0) return fail(OPSCALE_ERR_INVALID_ARG, "%s: empty problem", who);
+      launch = [=] {
+        return opscale::launch_kv_write_fp4(a.k, a.v, a.kv_row_stride, a.k_cache, a.v_cache, a.slot_mapping, a.T, a.Hkv,
+                                            a.D, a.block_size, a.num_blocks, bf16, stream);
+      };
+      wk = work_kv_fp4(a.T, a.Hkv, a.D, esize(dt), fp4_row(a.D), a.T, true);
+      break;
+    }
+    case OPSCALE_OP_KV_READ_FP4: {
+      const auto& a = d->u.kv_read_fp4;
+      st = check_kv_read_fp4(a.k_cache, a.v_cache, a.block_table, a.cu_seqlens, a.first_keys, a.k, a.v, a.kv_row_stride,
+                             a.B, a.total_tokens, a.Hkv, a.D, a.block_size, a.max_blocks_per_seq, a.num_blocks, dt);
+      if (st != OPSCALE_OK) return st;
+      if (a.B == 0 || a.total_tokens == 0) return fail(OPSCALE_ERR_INVALID_ARG, "%s: empty problem", who);
+      launch = [=] {
+        return opscale::launch_kv_read_fp4(a.k_cache, a.v_cache, a.block_table, a.cu_seqlens, a.first_keys, a.k, a.v,
+                                           a.kv_row_stride, a.B, a.total_tokens, a.Hkv, a.D, a.block_size,
+                                           a.max_blocks_per_seq, a.num_blocks, bf16, stream);
+      };
+      wk = work_kv_fp4(a.total_tokens, a.Hkv, a.D, esize(dt), fp4_row(a.D), a.total_tokens / a.block_size + 2ll * a.B, false);
+      break;
+    }
+    case OPSCALE_OP_ATTN_DECODE_FP4: {
+      const auto a = d->u.attn_decode_fp4;
+      st = check_decode_fp4(a.q, a.q_row_stride, a.k_cache, a.v_cache, a.block_table, a.context_lens, a.o, a.B, a.Hq,
+                            a.Hkv, a.D, a.block_size, a.max_blocks_per_seq, a.num_blocks, a.max_context_len, a.scale,
+                            &a.mods, dt, a.workspace, a.workspace_bytes);
+      if (st != OPSCALE_OK) return st;
+      if (a.B == 0) return fail(OPSCALE_ERR_INVALID_ARG, "%s: empty problem", who);
+      launch = [=] {
+        return opscale::launch_attn_decode_fp4(a.q, a.q_row_stride, a.k_cache, a.v_cache, a.block_table, a.context_lens,
+                                               a.o, a.B, a.Hq, a.Hkv, a.D, a.block_size, a.max_blocks_per_seq,
+                                               a.num_blocks, a.max_context_len, a.scale, &a.mods, bf16, a.workspace,
+                                               stream);
+      };
+      st = work_of_decode_mod(a.context_lens, a.B, a.Hq, a.Hkv, a.D, a.block_size, a.max_blocks_per_seq, &a.mods, dt,
+                              stream, &wk, true);
+      if (st != OPSCALE_OK) return st;
+      break;
+    }
     default:
       return fail(OPSCALE_ERR_INVALID_ARG, "%s: unknown op %d", who, (int)d->op);
   }
@@ -1438,8 +1782,8 @@ opscale_status opscale_op_profile(const opscale_op_desc* d, int32_t warmup, int3
   for (float x : us) mean += x;
   mean /= (double)us.size();
 
-  // MI355X peaks: bf16 dense matrix 2.5 PFLOP/s, fp32 matrix 157.3 TFLOP/s, HBM 8 TB/s.
-  const double peak_flops = bf16 ? 2.5e15 : 157.3e12;
+  // MI355X peaks: bf16 dense matrix 2.5 PFLOP/s, fp32 matrix 157.3 TFLOP/s, 8-bit matrix 5.0 PFLOP/s, HBM 8 TB/s.
+  const double peak_flops = d->op == OPSCALE_OP_LINEAR_FP8 ? 5.0e15 : bf16 ? 2.5e15 : 157.3e12;
   const double peak_bw = 8.0e12;
   const double t_s = (double)pct(0.5) * 1e-6;
   opscale_profile p{};

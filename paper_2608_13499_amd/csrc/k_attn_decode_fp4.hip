@@ -1,0 +1,513 @@
+// Paged decode attention over a cache of e2m1 elements (quant.h: the format), with the
+// score modifiers and masks of k_attn_decode_mod.hip, on the same plan and merge
+// (attn_decode_split.h).
+//
+// A workgroup of eight waves takes HB KV heads, 8 / HB waves to a head, and up to 16 of
+// its query heads (the columns of the MFMA; more go to further workgroups).  A wave
+// step is a tile of 32 keys, two runs of 16 consecutive slots, each in one page (a page
+// has 16 slots or more).  Their codes and scale bytes come by LDS DMA into a ring of
+// the wave's own, kStages - 1 tiles ahead, so that nothing but a counted wait stands
+// between a tile and the next; no barrier in the loop.
+//  * Scores S^T = K Q^T on MFMA 16x16x32: a lane holds a quarter row of a key, one
+//    scale for heads of 128, widened to bf16, which holds every value of the cache.
+//  * P V: a lane holds one dword of codes (D / 16 neighbouring elements) of eight keys.
+//    Widened, two neighbouring elements of a key lie in one register; a byte
+//    permutation of two keys' registers gives the operands of two MFMAs, whose column
+//    `col` is element (D / 16) col + i of the head for the i-th.
+// bf16 takes its probabilities in two bf16 pieces, as decode with modifiers does.  fp32
+// queries are three bf16 pieces, exactly, and their probabilities too: the products with
+// the cache's values are whole, and summed in fp32.
+#include "attn_decode_split.h"
+#include "quant.h"
+
+namespace opscale {
+
+namespace {
+constexpr int kRing = 4;  // tiles in a wave's ring
+template <int D>
+struct Fp4Ring {
+  static constexpr int kRun = 16 * D / 2;              // codes of 16 rows
+  static constexpr int kV = 2 * kRun, kScales = 4 * kRun;  // a stage: K codes, V codes, scale bytes
+  static constexpr int kStage = 4 * kRun + 256;
+  // the merge: 16 heads of D floats a wave
+  static constexpr int kWave = kRing * kStage > 16 * D * 4 ? kRing * kStage : 16 * D * 4;
+  static constexpr int kLoads = 5;                     // DMA loads of a tile
+};
+
+// The chunk of 16 bytes of row r of K (heads of 128: four a row) is stored at chunk
+// c ^ kSwz[r / 4]: each pass of the fragment reads then touches every bank once.
+__device__ __forceinline__ int k_swz(int r) { return (4 - (r >> 2)) & 3; }
+
+// Two bf16 (in a register) of element pair `b` of codes, times 2^(byte - 127); the byte lies
+// in bits 23 to 30 of `scale`, the only ones that the conversion reads.
+template <int B>
+__device__ __forceinline__ uint32_t widen_fp4(uint32_t codes, uint32_t scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, __uint_as_float(scale), B));
+}
+}  // namespace
+
+template <bool BF16, int D, int HB, bool INL>
+__global__ __launch_bounds__(512, 2) void attn_decode_fp4_kernel(const DecodeArgs a) {
+  using P = Fp4Page<D>;
+  using R = Fp4Ring<D>;
+  constexpr int ES = BF16 ? 2 : 4;
+  constexpr int KD = D / 4;          // elements of a key in a lane (scores)
+  constexpr int KC = KD / 8;         // MFMAs over the head dim
+  constexpr int DT = D / 16;         // elements of a lane's dword (P V): one MFMA each
+  constexpr int QP = BF16 ? 1 : 3;   // bf16 pieces of a query
+  constexpr int PP = BF16 ? 2 : 3;   // and of a probability
+  constexpr int WPH = kWaves / HB;
+  constexpr float kLazy = 8.f;
+  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  __shared__ PlanLds<INL> plan;
+  __shared__ float ml_s[kWaves][16][2];  // the waves' max and sum of each head
+
+  const int wgi = blockIdx.x, hg = blockIdx.y;
+  const int GH = a.GH, h0 = 16 * (int)blockIdx.z, G = min(16, GH - h0);
+  const int log2bs = a.log2bs, bs = 1 << log2bs;
+  const int max_keys = a.max_blocks << log2bs;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int col = lane & 15, grp = lane >> 4;
+
+  Share sh;
+  if (!plan_share<INL, WPH>(a, plan, wgi, wave, lane, max_keys, &sh)) return;
+  const int64_t t_lo = sh.t_lo, t_hi = sh.t_hi;
+  auto TC = [&](int i) -> int64_t {
+    if constexpr (INL) return uniform64(plan.tcs[i]);
+    else return uniform64(a.tcs[i]);
+  };
+
+  const int g = hg * HB + wave % HB;  // this wave's KV head
+  const int wt = wave / HB;           // its share of the head's key tiles
+  OPS_LDS char* ring = (OPS_LDS char*)smem_raw + wave * R::kWave;
+  const uint8_t* kc = static_cast<const uint8_t*>(a.kc);
+  const uint8_t* vc = static_cast<const uint8_t*>(a.vc);
+  const int page_bytes = P::bytes(log2bs);
+
+  // DMA sources within a run of 16 rows.  K: chunk lane % CPR of row lane / CPR, swizzled.  V: row
+  // 4 (slot % 4) + slot / 4 in place `slot`, so that the four groups' reads of a key each
+  // (rows 4 grp + rr) lie side by side.
+  constexpr int CPR = D / 32;  // 16-byte chunks of a row
+  const int lr = lane / CPR, lc = lane % CPR;
+  const uint32_t k_from = (uint32_t)(lr * P::kRow + (D == 128 ? lc ^ k_swz(lr) : lc) * 16);
+  const uint32_t v_from = (uint32_t)((4 * (lr & 3) + ((lr >> 2) & 3)) * P::kRow + lc * 16);
+  // Scale bytes: 16 lanes for each of (run 0: K, V; run 1: K, V), dword col % 4 of group col / 4.
+  const int s_group = min(col >> 2, P::kGroups - 1);
+  const uint32_t s_from = (uint32_t)((P::kRow << log2bs) + (s_group << log2bs) + (col & 3) * 4);
+  const uint8_t* s_base = (grp & 1 ? vc : kc) + s_from;
+  // and where they are read: K, a byte of this lane's key; V, the dword of its four keys
+  const int ks_at = R::kScales + ((grp * KD / kFp4Group) * 16 + col);
+  const int vs_at = R::kScales + 64 + ((col * DT / kFp4Group) * 16 + 4 * grp);
+  const int k_at = D == 128 ? col * P::kRow + ((grp ^ k_swz(col)) << 4) : col * P::kRow + grp * 8;
+  const int v_at = R::kV + grp * P::kRow + col * (DT / 2);
+
+  float slope2 = 0.f;  // of head `col`
+  if (a.mods.slopes && col < G) slope2 = a.mods.slopes[g * GH + h0 + col] * (BF16 ? kLog2e : 1.f);
+
+  // One segment: keys [k_begin, k_end) of sequence b, then those of [k2_begin, k2_end), partial
+  // results to slot pslot.
+  auto segment = [&](const int b, int k_begin, int k_end, const int k2_begin, const int k2_end, const int n,
+                     const int pre, const int lo, const int64_t pslot) {
+    bf16x8 qf[QP][KC];  // the query heads as the MFMA B operand (column = head)
+    {
+      const char* qrow = static_cast<const char*>(a.q) +
+                         ((int64_t)b * a.q_stride + ((int64_t)g * GH + h0 + (col < G ? col : 0)) * D + grp * KD) * ES;
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        float x[8];
+        load8<BF16>(qrow, c * 8, x);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          float rest = col < G ? x[e] : 0.f;
+#pragma unroll
+          for (int p = 0; p < QP; ++p) {
+            qf[p][c][e] = (__bf16)rest;
+            rest -= (float)qf[p][c][e];
+          }
+        }
+      }
+    }
+    const int32_t* trow = a.table + (int64_t)b * a.max_blocks;
+    float m_run = -INFINITY, l_part = 0.f;  // reference of head `col`, this lane's keys' sum
+    f32x4 acc[DT];                          // O[head 4*grp + r][element DT * col + i]
+#pragma unroll
+    for (int i = 0; i < DT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+    // The page ids of the 64 pages that hold the tile to be loaded next, and of the 64 after
+    // them, a lane each (as they come: nothing waits for the later ones before their turn).
+    int pages = -1, pages_next = -1, window = 0;
+    auto load_pages = [&](int w) {
+      const int i = w * 64 + lane;
+      return i < a.max_blocks ? trow[i] : -1;
+    };
+    uint32_t valid_ring = 0;  // a byte a stage: which of its runs lie in valid pages
+    // Tile t0 into a stage.  Every tile issues the same loads, which the counted wait
+    // relies on: what is not there reads as zeros (codes) or as any bytes (scales, masked).
+    auto issue = [&](int t0, int end, int stage) {
+      OPS_LDS char* st = ring + stage * R::kStage;
+      int page[2] = {-1, -1};
+      if (t0 < end) {
+        const int w = t0 >> (log2bs + 6);
+        if (w != window) {
+          pages = pages_next;
+          window = w;
+          pages_next = load_pages(w + 1);
+        }
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub) page[sub] = __builtin_amdgcn_readlane(pages, ((t0 + 16 * sub) >> log2bs) & 63);
+      }
+      int64_t base[2];
+      uint32_t valid = 0;
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const bool ok = (uint32_t)page[sub] < (uint64_t)a.num_blocks;
+        valid |= (uint32_t)ok << sub;
+        base[sub] = ok ? ((int64_t)page[sub] * a.Hkv + g) * page_bytes : 0;
+        const int row = ok ? (t0 + 16 * sub) & (bs - 1) : 0;
+        const int64_t at = base[sub] + row * P::kRow;
+        const __amdgpu_buffer_rsrc_t kr = make_rsrc(kc + at, ok ? R::kRun : 0);
+        const __amdgpu_buffer_rsrc_t vr = make_rsrc(vc + at, ok ? R::kRun : 0);
+        if (D == 128 || lane < 32) {
+          buffer_load16_lds<2>(kr, st + sub * R::kRun, k_from);
+          buffer_load16_lds<2>(vr, st + R::kV + sub * R::kRun, v_from);
+        }
+        base[sub] += row;
+      }
+      const uint8_t* sp = s_base + (grp < 2 ? base[0] : base[1]);
+      __builtin_amdgcn_global_load_lds(sp, st + R::kScales, 4, 0, 0);
+      valid_ring = (valid_ring & ~(0xffu << (8 * stage))) | (valid << (8 * stage));
+    };
+
+    // Scores, softmax and P V of the tile at t0, in a stage.
+    auto compute = [&](const int t0, const int end, const int stage) {
+      const OPS_LDS char* st = ring + stage * R::kStage;
+      // bit j: key t0 + j is seen (the tile's keys below `x`: the low x - t0 bits)
+      auto below = [&](int x) -> uint32_t {
+        const int d = min(max(x - t0, 0), 32);
+        return d == 32 ? 0xffffffffu : (1u << d) - 1;
+      };
+      const uint32_t valid = valid_ring >> (8 * stage);
+      const uint32_t seen = below(end) & (below(pre) | ~below(lo)) &
+                            ((valid & 1 ? 0xffffu : 0u) | (valid & 2 ? 0xffff0000u : 0u));
+      const uint32_t bits = seen >> (4 * grp);  // bit 16*sub + rr: this lane's keys
+      f32x4 st2[2];
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const uint32_t scale = (uint32_t)*reinterpret_cast<const OPS_LDS uint8_t*>(st + ks_at + 128 * sub) << 23;
+        uint32_t codes[KC];
+        if constexpr (D == 128) {
+          const u32x4 v = *reinterpret_cast<const OPS_LDS u32x4*>(st + k_at + sub * R::kRun);
+#pragma unroll
+          for (int c = 0; c < KC; ++c) codes[c] = v[c];
+        } else {
+          const u32x2 v = *reinterpret_cast<const OPS_LDS u32x2*>(st + k_at + sub * R::kRun);
+#pragma unroll
+          for (int c = 0; c < KC; ++c) codes[c] = v[c];
+        }
+        f32x4 s{};
+        bf16x8 kf[KC];
+#pragma unroll
+        for (int c = 0; c < KC; ++c)
+          kf[c] = __builtin_bit_cast(bf16x8, u32x4{widen_fp4<0>(codes[c], scale), widen_fp4<1>(codes[c], scale),
+                                                   widen_fp4<2>(codes[c], scale), widen_fp4<3>(codes[c], scale)});
+#pragma unroll
+        for (int p = QP - 1; p >= 0; --p)  // the smallest pieces first
+#pragma unroll
+          for (int c = 0; c < KC; ++c) s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[c], qf[p][c], s, 0, 0, 0);
+        st2[sub] = s;
+      }
+      auto each = [&](auto&& f) {
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr) st2[sub][rr] = f(st2[sub][rr], sub * 16 + rr);
+      };
+      if constexpr (!BF16) {
+        each([&](float x, int) {
+          x *= a.scale;
+          return a.mods.softcap > 0.f ? a.mods.softcap * tanhf(x / a.mods.softcap) : x;
+        });
+      } else if (a.mods.softcap > 0.f) {
+        float big = 0.f;
+        if (seen != 0xffffffffu) each([&](float x, int j) { return (bits >> j) & 1 ? x : 0.f; });
+#pragma unroll
+        for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+          for (int rr = 0; rr < 4; ++rr) big = fmaxf(big, fabsf(st2[sub][rr]));
+        const bool small = big <= a.mods.cap_bound;
+        if (__builtin_amdgcn_ballot_w64(!small) == 0) each([&](float x, int) { return a.mods.capped_small(x, 0.f); });
+        else each([&](float x, int) { return small ? a.mods.capped_small(x, 0.f) : a.mods.capped(x, 0.f); });
+      } else {
+        each([&](float x, int) { return x * a.scale_log2; });
+      }
+      if (a.mods.slopes) {
+        const float d0 = (float)(n - 1 - t0 - 4 * grp);
+        each([&](float x, int j) { return fmaf(-slope2, d0 - (float)j, x); });
+      }
+      if (seen != 0xffffffffu) each([&](float x, int j) { return (bits >> j) & 1 ? x : -INFINITY; });
+      float tmax = -INFINITY;
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) tmax = fmaxf(tmax, st2[sub][rr]);
+      tmax = rows_max(tmax);
+      if constexpr (!BF16) tmax *= kLog2e;
+      // move the reference max only when the tile's max exceeds it by kLazy
+      float alpha = 1.f;
+      if (tmax > m_run + kLazy) {
+        alpha = fast_exp2(m_run - tmax);
+        m_run = tmax;
+      }
+      const float m_use = m_run == -INFINITY ? 0.f : m_run;
+      bf16x8 pa[PP];  // P as the MFMA A operand: slot e is key 4*grp + e%4 + 16*(e/4)
+      float psum = 0.f;
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub)
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) {
+          const float p = fast_exp2(BF16 ? st2[sub][rr] - m_use : fmaf(st2[sub][rr], kLog2e, -m_use));
+          psum += p;
+          float rest = p;
+#pragma unroll
+          for (int i = 0; i < PP; ++i) {
+            pa[i][sub * 4 + rr] = (__bf16)rest;
+            rest -= (float)pa[i][sub * 4 + rr];
+          }
+        }
+      l_part = l_part * alpha + psum;
+      if (__builtin_amdgcn_ballot_w64(alpha != 1.f)) {
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) {
+          const float f = __shfl(alpha, grp * 4 + rr, 64);
+#pragma unroll
+          for (int i = 0; i < DT; ++i) acc[i][rr] *= f;
+        }
+      }
+      // V: keys 4*grp + rr of each run; their scale bytes moved to bits 23 to 30
+      uint32_t codes[8], scale[8];
+#pragma unroll
+      for (int sub = 0; sub < 2; ++sub) {
+        const uint32_t sv = *reinterpret_cast<const OPS_LDS uint32_t*>(st + vs_at + 128 * sub);
+        scale[4 * sub] = sv << 23, scale[4 * sub + 1] = sv << 15, scale[4 * sub + 2] = sv << 7, scale[4 * sub + 3] = sv >> 1;
+#pragma unroll
+        for (int rr = 0; rr < 4; ++rr) {
+          const OPS_LDS char* p = st + v_at + sub * R::kRun + 4 * rr * P::kRow;
+          codes[4 * sub + rr] = D == 128 ? *reinterpret_cast<const OPS_LDS uint32_t*>(p)
+                                         : (uint32_t)*reinterpret_cast<const OPS_LDS uint16_t*>(p);
+        }
+      }
+      // (a key that is not seen may lie in a group that holds NaN: 0 * NaN)
+      if (seen != 0xffffffffu)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) scale[e] = (bits >> ((e >> 2) * 16 + (e & 3))) & 1 ? scale[e] : 0u;
+      auto pair = [&](auto b_c) {  // elements 2 b and 2 b + 1 of the lane's dword
+        constexpr int b = decltype(b_c)::value;
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = widen_fp4<b>(codes[e], scale[e]);
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          u32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            v[e] = __builtin_amdgcn_perm(w[2 * e + 1], w[2 * e], half ? 0x07060302u : 0x05040100u);
+#pragma unroll
+          for (int i = PP - 1; i >= 0; --i)
+            acc[2 * b + half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pa[i], __builtin_bit_cast(bf16x8, v),
+                                                                        acc[2 * b + half], 0, 0, 0);
+        }
+      };
+      pair(std::integral_constant<int, 0>{});
+      pair(std::integral_constant<int, 1>{});
+      if constexpr (DT == 8) {
+        pair(std::integral_constant<int, 2>{});
+        pair(std::integral_constant<int, 3>{});
+      }
+    };
+
+    for (int range = 0; range < 2; ++range) {
+      if (range == 1) {
+        k_begin = k2_begin;
+        k_end = k2_end;
+      }
+      constexpr int STEP = WPH * kTile;
+      const int first = k_begin + wt * kTile;
+      if (first >= k_end) continue;
+      window = first >> (log2bs + 6);
+      pages = load_pages(window);
+      pages_next = load_pages(window + 1);
+#pragma unroll
+      for (int i = 0; i < kRing - 1; ++i) issue(min((int64_t)first + i * STEP, (int64_t)k_end), k_end, i);
+      int stage = 0;
+      for (int t0 = first; t0 < k_end; t0 += STEP) {
+        asm volatile("" ::: "memory");
+        wait_vmcnt_le<R::kLoads*(kRing - 2)>();
+        asm volatile("" ::: "memory");
+        issue((int)min((int64_t)t0 + (kRing - 1) * STEP, (int64_t)k_end), k_end, (stage + kRing - 1) % kRing);
+        compute(t0, k_end, stage);
+        stage = (stage + 1) % kRing;
+      }
+      wait_vmem();  // the loads past the last tile land in the ring
+    }
+
+    // ---- merge the waves sharing a head (WPH > 1) through LDS, write partials,
+    // head-major: entry (head, slot) at head * (nwg + B) + slot
+    const float l_run = rows_sum(l_part);
+    const int64_t nslots = (int64_t)a.nwg + a.B;
+    if constexpr (WPH == 1) {
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr) {
+        const int hh = 4 * grp + rr;
+        if (hh < G) {
+          float* to = a.ws_o + ((int64_t)(g * GH + h0 + hh) * nslots + pslot) * D + DT * col;
+#pragma unroll
+          for (int i = 0; i < DT; i += 4)
+            *reinterpret_cast<f32x4*>(to + i) = f32x4{acc[i][rr], acc[i + 1][rr], acc[i + 2][rr], acc[i + 3][rr]};
+        }
+      }
+      if (col < G && grp == 0) {
+        const int64_t slot = (int64_t)(g * GH + h0 + col) * nslots + pslot;
+        a.ws_ml[slot * 2 + 0] = m_run;
+        a.ws_ml[slot * 2 + 1] = l_run;
+      }
+    } else {
+      // (each wave writes its own ring: [head][D])
+      static_assert(16 * D * 4 <= R::kWave, "the merge fits the rings");
+      float* mine = reinterpret_cast<float*>(smem_raw + wave * R::kWave);
+#pragma unroll
+      for (int rr = 0; rr < 4; ++rr) {
+        const int hh = 4 * grp + rr;
+        if (hh < G)
+#pragma unroll
+          for (int i = 0; i < DT; ++i) mine[hh * D + DT * col + i] = acc[i][rr];
+      }
+      if (grp == 0) {
+        ml_s[wave][col][0] = m_run;
+        ml_s[wave][col][1] = l_run;
+      }
+      __syncthreads();
+      constexpr int STEP = kWaves * 64 / D;
+      const int d = threadIdx.x % D;
+      for (int hh = threadIdx.x / D; hh < G; hh += STEP) {
+#pragma unroll
+        for (int hl = 0; hl < HB; ++hl) {
+          float M = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < WPH; ++w) M = fmaxf(M, ml_s[w * HB + hl][hh][0]);
+          float o = 0.f, l = 0.f;
+#pragma unroll
+          for (int w = 0; w < WPH; ++w) {
+            const float* e = ml_s[w * HB + hl][hh];
+            const float f = e[0] == -INFINITY ? 0.f : fast_exp2(e[0] - M);
+            o += f * reinterpret_cast<const float*>(smem_raw + (w * HB + hl) * R::kWave)[hh * D + d];
+            l += f * e[1];
+          }
+          const int64_t slot = (int64_t)((hg * HB + hl) * GH + h0 + hh) * nslots + pslot;
+          a.ws_o[slot * D + d] = o;
+          if (d == 0) {
+            a.ws_ml[slot * 2 + 0] = M;
+            a.ws_ml[slot * 2 + 1] = l;
+          }
+        }
+      }
+      __syncthreads();  // before the next segment's tiles take the rings
+    }
+  };  // segment
+
+  const bool aligned = INL && a.aligned;  // (one piece, of b_first)
+  for (int b = sh.b_first; b < a.B; ++b) {
+    int64_t v0 = t_lo, v1 = t_hi;
+    if (!aligned) {
+      const int64_t tb = TC(b);
+      if (tb >= t_hi) break;
+      v0 = max(t_lo, tb) - tb, v1 = min(t_hi, TC(b + 1)) - tb;
+      if (v0 >= v1) continue;  // a sequence that sees no key
+    }
+    DecodeSpan s;
+    if constexpr (INL) {
+      s = make_span(aligned ? sh.own_n : __builtin_amdgcn_readfirstlane(plan.n[b]),
+                    aligned ? sh.own_pre : __builtin_amdgcn_readfirstlane(plan.pre[b]),
+                    aligned ? sh.own_lo : __builtin_amdgcn_readfirstlane(plan.lo[b]));
+    } else {
+      s = decode_span(a.mods, a.ctx, max_keys, __builtin_amdgcn_readfirstlane(b));
+    }
+    const int shift = s.first_tile - s.pre_tiles, x0 = (int)v0, x1 = (int)v1;
+    segment(b, min(x0, s.pre_tiles) * kTile, min(min(x1, s.pre_tiles) * kTile, s.n),
+            (max(x0, s.pre_tiles) + shift) * kTile, min((max(x1, s.pre_tiles) + shift) * kTile, s.n), s.n, s.pre, s.lo,
+            aligned ? wgi : (int64_t)wgi + b);
+    if (aligned) break;
+  }
+}
+
+namespace {
+
+template <bool BF16, int D, int HB, bool INL>
+hipError_t launch_split(const DecodeArgs& a, dim3 grid, hipStream_t s) {
+  constexpr int lds = kWaves * Fp4Ring<D>::kWave;
+  static const hipError_t attr = hipFuncSetAttribute(
+      reinterpret_cast<const void*>(attn_decode_fp4_kernel<BF16, D, HB, INL>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (attr != hipSuccess) return attr;
+  hipLaunchKernelGGL((attn_decode_fp4_kernel<BF16, D, HB, INL>), grid, dim3(kWaves * 64), lds, s, a);
+  return hipGetLastError();
+}
+template <bool BF16, int D, int HB>
+hipError_t launch_split_b(const DecodeArgs& a, dim3 grid, hipStream_t s) {
+  return a.B <= kInlineB ? launch_split<BF16, D, HB, true>(a, grid, s) : launch_split<BF16, D, HB, false>(a, grid, s);
+}
+template <bool BF16, int D>
+hipError_t launch_split_h(const DecodeArgs& a, int HB, dim3 grid, hipStream_t s) {
+  switch (HB) {
+    case 1: return launch_split_b<BF16, D, 1>(a, grid, s);
+    case 2: return launch_split_b<BF16, D, 2>(a, grid, s);
+    case 4: return launch_split_b<BF16, D, 4>(a, grid, s);
+    default: return launch_split_b<BF16, D, 8>(a, grid, s);
+  }
+}
+template <class OUT, int D>
+hipError_t launch_combine(const DecodeArgs& a, void* o, int Hq, int waves, hipStream_t s) {
+  const dim3 grid((unsigned)Hq, (unsigned)a.B);
+  OUT* out = static_cast<OUT*>(o);
+  if (a.B > kInlineB)
+    hipLaunchKernelGGL((attn_decode_mod_combine_kernel<OUT, D, false, 1>), grid, dim3(64), 0, s, a, out, Hq, waves);
+  else if (a.nwg > 16 * a.B)
+    hipLaunchKernelGGL((attn_decode_mod_combine_kernel<OUT, D, true, 4>), grid, dim3(256), 0, s, a, out, Hq, waves);
+  else
+    hipLaunchKernelGGL((attn_decode_mod_combine_kernel<OUT, D, true, 1>), grid, dim3(64), 0, s, a, out, Hq, waves);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attn_decode_fp4(const void* q, int64_t q_stride, const void* kcache, const void* vcache,
+                                  const int32_t* table, const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv,
+                                  int32_t D, int32_t block_size, int32_t max_blocks, int64_t num_blocks,
+                                  int32_t max_context_len, float scale, const opscale_attn_mods* m, bool bf16, void* ws,
+                                  hipStream_t s) {
+  int log2bs = 0;
+  while ((1 << log2bs) < block_size) ++log2bs;
+  const AttnMods mods = make_attn_mods(m, scale);
+  const int HB = decode_heads_per_workgroup(Hkv), G = Hq / Hkv, blocks = (G + 15) / 16;
+  const int nwg = mod_workgroups(B, max_context_len, mods.window, mods.prefix, Hkv / HB * blocks, kWaves / HB);
+  const DecodeWs w = decode_ws(ws, B, Hq, D, nwg);
+  DecodeArgs a{};
+  a.q = q, a.kc = kcache, a.vc = vcache, a.q_stride = q_stride, a.table = table, a.ctx = ctx, a.Hkv = Hkv, a.GH = G;
+  a.log2bs = log2bs, a.max_blocks = max_blocks, a.num_blocks = num_blocks;
+  a.tcs = w.tcs, a.first_b = w.first, a.B = B, a.nwg = nwg, a.aligned = B <= 64 && nwg >= 2 * B;
+  a.scale = scale, a.scale_log2 = scale * kLog2e, a.ws_o = w.o, a.ws_ml = w.ml, a.mods = mods;
+  if (B > kInlineB) {
+    hipLaunchKernelGGL(attn_decode_mod_plan_kernel, dim3(1), dim3(1024), 0, s, a, w.tcs, w.first);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const dim3 grid((unsigned)nwg, (unsigned)(Hkv / HB), (unsigned)blocks);
+  hipError_t e;
+  if (bf16 && D == 128) e = launch_split_h<true, 128>(a, HB, grid, s);
+  else if (bf16) e = launch_split_h<true, 64>(a, HB, grid, s);
+  else if (D == 128) e = launch_split_h<false, 128>(a, HB, grid, s);
+  else e = launch_split_h<false, 64>(a, HB, grid, s);
+  if (e != hipSuccess) return e;
+  if (bf16) return D == 128 ? launch_combine<__bf16, 128>(a, o, Hq, kWaves / HB, s) : launch_combine<__bf16, 64>(a, o, Hq, kWaves / HB, s);
+  return D == 128 ? launch_combine<float, 128>(a, o, Hq, kWaves / HB, s) : launch_combine<float, 64>(a, o, Hq, kWaves / HB, s);
+}
+
+}  // namespace opscale

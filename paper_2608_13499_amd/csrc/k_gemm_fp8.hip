@@ -1,0 +1,521 @@
+// The linear of e4m3 operands (opscale_linear_fp8): with a scale for each token and
+// 128 of K (xs) and for each 128 x 128 of W (ws),
+//   y[m, n] = sum over blocks b of K of xs[b, m] ws[n / 128, b] sum_{k in b} x[m, k] W[n, k].
+//
+// The inner sums are one v_mfma_f32_16x16x128_f8f6f4 each (W as the A operand, x as
+// the B operand: an accumulator lane owns one row of y and four consecutive columns),
+// whose result the vector units scale and add: the sum over K is an fp32 fma chain.
+// That MFMA adds products in groups of eight consecutive k, each cut to 2^-13 of its
+// group's largest (measured: a product 2^14 below it is lost), and the sixteen groups
+// in fp32.  Against 64 bits that is 1e-4 of a result, a bf16 result's own rounding is
+// 1.7e-3.  For fp32 results (EXACT) the operands are widened in registers (exactly)
+// and multiplied as bf16, whose MFMA keeps the products whole, at half the rate.
+//
+// A slice is a block of K: 128 bytes of each row.  Rows past M and N and the K columns
+// past the end read as zeros (buffer range check, and a lane flag in the last slice).
+#include <algorithm>
+#include <type_traits>
+
+#include "gemm_schedule.h"
+#include "launch.h"
+#include "quant.h"
+
+namespace opscale {
+
+namespace {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kSlice = kFp8Block;
+
+template <int V>
+using Int = std::integral_constant<int, V>;
+template <int N, class F, int I = 0>
+__device__ __forceinline__ void static_for(F&& f) {
+  if constexpr (I < N) {
+    f(Int<I>{});
+    static_for<N, F, I + 1>(static_cast<F&&>(f));
+  }
+}
+
+// 32 bytes a lane: chunks fq and 4 + fq of a row's slice (any order of k, the same for both operands)
+struct Frag {
+  u32x4 c[2];
+};
+
+__device__ __forceinline__ bf16x8 widen(uint32_t lo, uint32_t hi) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// The sum over a slice of 16 rows of W and 16 of x.
+template <bool EXACT>
+__device__ __forceinline__ f32x4 block_product(const Frag& w, const Frag& x) {
+  if constexpr (EXACT) {
+    f32x4 s{};
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2)
+        s = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w.c[h][i], w.c[h][i + 1]), widen(x.c[h][i], x.c[h][i + 1]), s,
+                                                    0, 0, 0);
+    return s;
+  } else {
+    const i32x8 a = __builtin_shufflevector(__builtin_bit_cast(i32x4, w.c[0]), __builtin_bit_cast(i32x4, w.c[1]), 0, 1, 2,
+                                            3, 4, 5, 6, 7);
+    const i32x8 b = __builtin_shufflevector(__builtin_bit_cast(i32x4, x.c[0]), __builtin_bit_cast(i32x4, x.c[1]), 0, 1, 2,
+                                            3, 4, 5, 6, 7);
+    // (no scale operands: the unscaled instruction)
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, f32x4{}, 0, 0, 0, 0, 0, 0);
+  }
+}
+
+__device__ __forceinline__ Frag read_frag(const OPS_LDS char* p, const int (&off)[2]) {
+  Frag f;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) f.c[h] = *reinterpret_cast<const OPS_LDS u32x4*>(p + off[h]);
+  return f;
+}
+
+// Four consecutive columns of a row of y, plus bias.
+template <class OUT>
+__device__ __forceinline__ void store4(OUT* y, const OUT* bias, int64_t at, int n, f32x4 v) {
+  if constexpr (sizeof(OUT) == 2) {
+    if (bias) {
+      const u32x2 b = *reinterpret_cast<const u32x2*>(bias + n);
+      v[0] += bf_lo(b[0]), v[1] += bf_hi(b[0]), v[2] += bf_lo(b[1]), v[3] += bf_hi(b[1]);
+    }
+    *reinterpret_cast<u32x2*>(y + at) = u32x2{pack_bf2(v[0], v[1]), pack_bf2(v[2], v[3])};
+  } else {
+    if (bias) v += *reinterpret_cast<const f32x4*>(bias + n);
+    *reinterpret_cast<f32x4*>(y + at) = v;
+  }
+}
+
+struct LinearFp8Args {
+  const uint8_t *x, *w;
+  const float *xs, *ws;
+  const void* bias;
+  void* y;
+  float* part;  // not null: fp32 partials [split, M, N]
+  int M, N, K, nkb;
+  int tiles_n, group_m;  // column tiles; tile-rows that sweep them together
+  int chunk;             // slices of a split
+};
+
+}  // namespace
+
+// ------------------------------------------------------------ tiles of many rows --
+// BM x BN of y a workgroup, WGM x WGN waves, an LDS ring of STAGES slices filled by LDS
+// DMA: a stage holds the slices of x's and W's rows, then the rows' scales.
+template <int BM_, int BN_, int WGM_, int WGN_, int STAGES_>
+struct Fp8Tile {
+  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, STAGES = STAGES_;
+  static constexpr int kWaves = WGM * WGN, kThreads = 64 * kWaves;
+  static constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16;
+  static constexpr int kXLoads = BM / 8 / kWaves, kWLoads = BN / 8 / kWaves, kLoads = kXLoads + kWLoads + 1;
+  static constexpr int kStageBytes = (BM + BN) * kSlice + BM * 4, kLdsBytes = STAGES * kStageBytes;
+  static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BM % 64 == 0, "whole loads");
+  static_assert(kFp8Block % WN == 0 && BN % kFp8Block == 0, "a wave's columns lie in one block of W's scales");
+  static_assert((STAGES - 2) * kLoads <= 63, "vmcnt range");
+};
+
+template <class C, class OUT>
+__global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const LinearFp8Args a) {
+  constexpr bool EXACT = sizeof(OUT) == 4;
+  constexpr int BM = C::BM, BN = C::BN, TM = C::TM, TN = C::TN, S = C::STAGES;
+  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  OPS_LDS char* smem = (OPS_LDS char*)smem_raw;
+  const int M = a.M, N = a.N, K = a.K;
+
+  const int tiles_m = (M + BM - 1) / BM, tiles = tiles_m * a.tiles_n;
+  const int split = blockIdx.x / tiles;
+  const int tid = (int)xcd_remap(blockIdx.x - split * tiles, (uint32_t)tiles);
+  int m0, n0;
+  {
+    const int per = a.group_m * a.tiles_n, group = tid / per, first = group * a.group_m;
+    const int rows = min(tiles_m - first, a.group_m), in = tid - group * per;
+    m0 = (first + in % rows) * BM;
+    n0 = in / rows * BN;
+  }
+  const int kb0 = split * a.chunk, ns = min(a.chunk, a.nkb - kb0);
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int wm = wave % C::WGM, wn = wave / C::WGM;
+  const int fr = lane & 15, fq = lane >> 4;
+
+  // A load covers 8 rows; lane p writes chunk p % 8 of row p / 8, which holds chunk
+  // (p % 8) ^ (p / 8) of the row (gemm_bf16_kernel's layout: no bank conflicts).
+  const int c16 = ((lane & 7) ^ (lane >> 3)) * 16;
+  const int xrows = min(BM, M - m0), wrows = min(BN, N - n0);
+  const uint8_t* xp = a.x + (int64_t)m0 * K;
+  const uint8_t* wp = a.w + (int64_t)n0 * K;
+  uint32_t xo[C::kXLoads], wo[C::kWLoads];
+#pragma unroll
+  for (int g = 0; g < C::kXLoads; ++g) xo[g] = (uint32_t)(((g * C::kWaves + wave) * 8 + (lane >> 3)) * K + c16);
+#pragma unroll
+  for (int g = 0; g < C::kWLoads; ++g) wo[g] = (uint32_t)(((g * C::kWaves + wave) * 8 + (lane >> 3)) * K + c16);
+  const int sw = wave % (BM / 64);  // the rows whose scales this wave loads
+
+  // Slices past the last one are loaded too, on descriptors of no records: every step issues
+  // the same loads, which the counted wait relies on.
+  auto load = [&](int kt, int stage) {
+    const int k = (kb0 + kt) * kSlice;
+    const bool live = kt < ns;
+    OPS_LDS char* st = smem + stage * C::kStageBytes;
+    const uint32_t off = k + c16 < K ? 0u : kOobOffset;
+    const __amdgpu_buffer_rsrc_t xr = make_rsrc(xp + k, live ? (uint32_t)((xrows - 1) * K + K - k) : 0u);
+    const __amdgpu_buffer_rsrc_t wr = make_rsrc(wp + k, live ? (uint32_t)((wrows - 1) * K + K - k) : 0u);
+    const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.xs + (int64_t)(kb0 + kt) * M + m0, live ? (uint32_t)xrows * 4 : 0u);
+#pragma unroll
+    for (int g = 0; g < C::kXLoads; ++g)
+      buffer_load16_lds<kNoL1>(xr, st + (g * C::kWaves + wave) * 1024, xo[g] | off);
+#pragma unroll
+    for (int g = 0; g < C::kWLoads; ++g)
+      buffer_load16_lds<kNoL1>(wr, st + BM * kSlice + (g * C::kWaves + wave) * 1024, wo[g] | off);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, st + (BM + BN) * kSlice + sw * 256, 4, (sw * 64 + lane) * 4, 0, 0, 0);
+  };
+
+  f32x4 acc[TN][TM];
+#pragma unroll
+  for (int i = 0; i < TN; ++i)
+#pragma unroll
+    for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{};
+
+  int off[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) off[h] = fr * kSlice + (((4 * h + fq) ^ (fr & 7)) << 4);
+  const int x0 = wm * C::WM * kSlice, w0 = BM * kSlice + wn * C::WN * kSlice;
+  const int s0 = (BM + BN) * kSlice + (wm * C::WM + fr) * 4;
+  // W's scales of this wave's columns, a lane each for 64 slices
+  const float* wsp = a.ws + (int64_t)(min(n0 + wn * C::WN, N - 1) / kFp8Block) * a.nkb + kb0;
+  float wscales = 0.f;
+
+#pragma unroll
+  for (int s = 0; s < S - 1; ++s) load(s, s);
+  int stage = 0;
+  for (int kt = 0; kt < ns; ++kt) {
+    if ((kt & 63) == 0) wscales = kt + lane < ns ? wsp[kt + lane] : 0.f;
+    wait_vmcnt_le<(S - 2) * C::kLoads>();
+    barrier_keep_loads();
+    const int next = stage == 0 ? S - 1 : stage - 1;  // the stage of slice kt - 1
+    load(kt + S - 1, next);
+    const OPS_LDS char* st = smem + stage * C::kStageBytes;
+    const float wscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), kt & 63));
+    Frag w[TN];
+#pragma unroll
+    for (int i = 0; i < TN; ++i) w[i] = read_frag(st + w0 + i * 16 * kSlice, off);
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const Frag x = read_frag(st + x0 + j * 16 * kSlice, off);
+      const float f = *reinterpret_cast<const OPS_LDS float*>(st + s0 + j * 64) * wscale;
+#pragma unroll
+      for (int i = 0; i < TN; ++i) {
+        const f32x4 p = block_product<EXACT>(w[i], x);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(f, p[r], acc[i][j][r]);
+      }
+    }
+    stage = stage + 1 == S ? 0 : stage + 1;
+  }
+  wait_vmem();  // no LDS DMA may be in flight when the workgroup ends
+
+#pragma unroll
+  for (int j = 0; j < TM; ++j) {
+    const int m = m0 + wm * C::WM + 16 * j + fr;
+    if (m >= M) continue;
+#pragma unroll
+    for (int i = 0; i < TN; ++i) {
+      const int n = n0 + wn * C::WN + 16 * i + 4 * fq;
+      if (n >= N) continue;
+      if (a.part) *reinterpret_cast<f32x4*>(a.part + ((int64_t)split * M + m) * N + n) = acc[i][j];
+      else store4(static_cast<OUT*>(a.y), static_cast<const OUT*>(a.bias), (int64_t)m * N + n, n, acc[i][j]);
+    }
+  }
+}
+
+// --------------------------------------------------------------------- few rows --
+// Up to 16 TM rows: W's bytes are the time.  As gemm_decode_bf16_kernel: a workgroup
+// of NW waves takes 16 NW columns and all rows, each wave's W rows straight to
+// registers, a ring of kSlots slices, x and its scales through an LDS ring.
+namespace {
+constexpr int kSlots = 8, kAhead = 7, kStages = 4;
+static_assert(kAhead == kSlots - 1 && kSlots % kStages == 0, "ring shapes");
+}  // namespace
+
+// (x and w are not __restrict__: their loads would be moved across the fences)
+template <int TM, int NW, class OUT>
+__global__ __launch_bounds__(64 * NW, 1) void gemm_fp8_rows_kernel(const LinearFp8Args a) {
+  constexpr bool EXACT = sizeof(OUT) == 4;
+  constexpr int XL = (2 * TM + NW - 1) / NW;      // x loads of 8 rows, for every wave alike
+  constexpr int SEG = (16 * TM + 63) / 64;        // 64-row runs of scales
+  constexpr int kXBytes = XL * NW * 1024, kStageBytes = kXBytes + SEG * 256;
+  extern __shared__ __attribute__((aligned(16))) char smem_raw[];
+  OPS_LDS char* smem = (OPS_LDS char*)smem_raw;
+  const int M = a.M, N = a.N, K = a.K;
+
+  const uint32_t id = xcd_remap(blockIdx.x, gridDim.x);
+  const int split = (int)(id / (uint32_t)a.tiles_n), tn = (int)(id % (uint32_t)a.tiles_n);
+  const int kb0 = split * a.chunk, ns = min(a.chunk, a.nkb - kb0);
+  // column tiles start at different slices, or all would read the same few HBM channels
+  const int rot = a.tiles_n <= 65536 ? (int)((uint32_t)(tn * ns) / (uint32_t)a.tiles_n) : tn % ns;
+
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int fr = lane & 15, fq = lane >> 4;
+  const int n0 = (tn * NW + wave) * 16;
+  const int wrows = max(0, min(16, N - n0));
+  const uint8_t* wp = a.w + (int64_t)min(n0, N - 1) * K;
+  const uint32_t w_voff = (uint32_t)(fr * K + 16 * fq);
+  const float* wsp = a.ws + (int64_t)(min(n0, N - 1) / kFp8Block) * a.nkb;
+  const int c16 = ((lane & 7) ^ (lane >> 3)) * 16;
+  uint32_t x_voff[XL];
+#pragma unroll
+  for (int g = 0; g < XL; ++g) {
+    const int r = (g * NW + wave) * 8 + (lane >> 3);
+    x_voff[g] = r < M ? (uint32_t)(r * K + c16) : kOobOffset;
+  }
+  int off[2];
+#pragma unroll
+  for (int h = 0; h < 2; ++h) off[h] = fr * kSlice + (((4 * h + fq) ^ (fr & 7)) << 4);
+
+  Frag wf[kSlots];
+  float wsf[kSlots];
+  f32x4 acc[TM];
+#pragma unroll
+  for (int t = 0; t < TM; ++t) acc[t] = f32x4{};
+
+  // Slice s of the range, in this workgroup's order; those past the last one are loaded too,
+  // on descriptors of no records (zeros that no result takes).
+  auto slice = [&](int s) { return kb0 + (s + rot < ns ? s + rot : s + rot - ns); };
+  auto load_x = [&](int s, int stage) {
+    const int kb = slice(s), k = kb * kSlice;
+    const bool live = s < ns;
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(a.x + k, live ? (uint32_t)((M - 1) * K + K - k) : 0u);
+    const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.xs + (int64_t)kb * M, live ? (uint32_t)M * 4 : 0u);
+    const uint32_t out = k + c16 < K ? 0u : kOobOffset;
+    OPS_LDS char* st = smem + stage * kStageBytes;
+#pragma unroll
+    for (int g = 0; g < XL; ++g) buffer_load16_lds<kNoL1>(r, st + (g * NW + wave) * 1024, x_voff[g] | out);
+    const int seg = wave % SEG;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, st + kXBytes + seg * 256, 4, (seg * 64 + lane) * 4, 0, 0, 0);
+  };
+  auto load_w = [&](auto slot_c, int s) {
+    constexpr int slot = decltype(slot_c)::value;
+    const int kb = slice(s), k = kb * kSlice;
+    const bool live = s < ns && wrows > 0;
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(wp + k, live ? (uint32_t)((wrows - 1) * K + K - k) : 0u);
+    const __amdgpu_buffer_rsrc_t sr = make_rsrc(wsp + kb, live ? 4u : 0u);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      wf[slot].c[h] = buffer_load16(r, (w_voff + 64 * h) | (k + 16 * fq + 64 * h < K ? 0u : kOobOffset));
+    wsf[slot] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(sr, 0, 0, 0));
+  };
+  auto fence = [] { asm volatile("" ::: "memory"); };
+
+  auto step = [&](auto slot_c, int c) {
+    constexpr int slot = decltype(slot_c)::value;
+    constexpr int stage = slot % kStages;
+    // newer than x(c): the W loads of its own step, x and W of the two since
+    wait_vmcnt_le<3 * (kStages - 1) + (XL + 1) * (kStages - 2)>();
+    barrier_keep_loads();
+    load_x(c + kStages - 1, (stage + kStages - 1) % kStages);
+    fence();
+    load_w(Int<(slot + kAhead) % kSlots>{}, c + kAhead);
+    fence();
+    const OPS_LDS char* st = smem + stage * kStageBytes;
+    Frag x[TM];
+    float f[TM];
+#pragma unroll
+    for (int t = 0; t < TM; ++t) {
+      x[t] = read_frag(st + t * 16 * kSlice, off);
+      f[t] = *reinterpret_cast<const OPS_LDS float*>(st + kXBytes + (16 * t + fr) * 4);
+    }
+#pragma unroll
+    for (int t = 0; t < TM; ++t) {
+      const f32x4 p = block_product<EXACT>(wf[slot], x[t]);
+      const float g = f[t] * wsf[slot];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[t][r] = fmaf(g, p[r], acc[t][r]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  };
+
+  static_for<kAhead>([&](auto i_c) {
+    constexpr int i = decltype(i_c)::value, xs = i - kAhead + kStages - 1;
+    if constexpr (xs >= 0) {
+      load_x(xs, xs % kStages);
+      fence();
+    }
+    load_w(Int<i>{}, i);
+    fence();
+  });
+  // whole rounds of kSlots unconditional steps: every load is then issued as written
+  for (int base = 0; base < ns; base += kSlots)
+    static_for<kSlots>([&](auto s_c) { step(s_c, base + decltype(s_c)::value); });
+  wait_vmem();
+
+  const int n = n0 + 4 * fq;
+  if (n >= N) return;
+#pragma unroll
+  for (int t = 0; t < TM; ++t) {
+    const int m = 16 * t + fr;
+    if (m >= M) continue;
+    if (a.part) *reinterpret_cast<f32x4*>(a.part + ((int64_t)split * M + m) * N + n) = acc[t];
+    else store4(static_cast<OUT*>(a.y), static_cast<const OUT*>(a.bias), (int64_t)m * N + n, n, acc[t]);
+  }
+}
+
+// y = the splits' partials, in order, + bias; four columns a thread, kBatch splits' loads at a time.
+template <class OUT>
+__global__ __launch_bounds__(256) void fp8_reduce_kernel(const float* __restrict__ part, int splits,
+                                                         const OUT* __restrict__ bias, OUT* __restrict__ y, int64_t MN,
+                                                         int N) {
+  constexpr int kBatch = 8;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < MN / 4; i += (int64_t)gridDim.x * 256) {
+    f32x4 v = reinterpret_cast<const f32x4*>(part)[i];
+    for (int s0 = 1; s0 < splits; s0 += kBatch) {
+      f32x4 p[kBatch];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (s0 + j < splits) p[j] = reinterpret_cast<const f32x4*>(part + (int64_t)(s0 + j) * MN)[i];
+#pragma unroll
+      for (int j = 0; j < kBatch; ++j)
+        if (s0 + j < splits) v += p[j];
+    }
+    store4(y, bias, i * 4, (int)((i * 4) % N), v);
+  }
+}
+
+namespace {
+
+using Tile256 = Fp8Tile<256, 256, 2, 4, 2>;  // 8 waves of 128 x 64, 2 x 65 KB
+using Tile128 = Fp8Tile<128, 128, 2, 2, 2>;  // 4 waves of 64 x 64, 2 x 32.5 KB, two workgroups a CU
+
+constexpr int64_t kRowsMaxM = 128;
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Few rows: waves of a workgroup and slices of a split with the fewest W bytes a CU
+// (rounds x columns x slices, in whole rounds of the ring), splits of 8 slices at least.
+struct RowsShape {
+  int waves, splits, chunk;
+};
+RowsShape rows_shape(int64_t N, int64_t nkb, bool split_ok) {
+  RowsShape best{};
+  int64_t best_cost = 0;
+  for (int nw = kMaxStreamWaves; nw >= kMinStreamWaves; --nw) {
+    const int64_t tiles = cdiv(N, 16 * nw);
+    const int64_t most = split_ok ? std::max<int64_t>(1, std::min<int64_t>(kNumCUs / tiles, nkb / 8)) : 1;
+    const int64_t chunk = cdiv(nkb, most), splits = cdiv(nkb, chunk);
+    const int64_t cost = cdiv(tiles * splits, kNumCUs) * nw * cdiv(chunk, kSlots);
+    if (best_cost == 0 || cost < best_cost) best_cost = cost, best = {nw, (int)splits, (int)chunk};
+  }
+  return best;
+}
+
+// Tiles: the smaller ones where the larger leave more of the chip idle, and K split where
+// even those are fewer than the CUs.
+LinearFp8Plan tile_plan(int64_t M, int64_t N, int64_t nkb, bool split_ok) {
+  LinearFp8Plan p{};
+  const int64_t big = cdiv(M, 256) * cdiv(N, 256), small = cdiv(M, 128) * cdiv(N, 128);
+  const double t_big = 2.2 * cdiv(big, kNumCUs), t_small = 0.8 * cdiv(small, kNumCUs);
+  p.path = t_big <= t_small ? LinearFp8Plan::kTile256 : LinearFp8Plan::kTile128;
+  const int64_t tiles = p.path == LinearFp8Plan::kTile256 ? big : small;
+  int64_t splits = 1;
+  if (split_ok && tiles < kNumCUs) splits = std::max<int64_t>(1, std::min<int64_t>(2 * kNumCUs / tiles, nkb / 8));
+  p.chunk = (int)cdiv(nkb, splits);
+  p.splits = (int)cdiv(nkb, p.chunk);
+  return p;
+}
+
+}  // namespace
+
+LinearFp8Plan plan_linear_fp8(int64_t M, int64_t N, int64_t K, bool split_ok) {
+  const int64_t nkb = cdiv(K, kFp8Block);
+  LinearFp8Plan p{};
+  if (M <= kRowsMaxM) {
+    const RowsShape r = rows_shape(N, nkb, split_ok);
+    p.path = LinearFp8Plan::kRows;
+    p.waves = r.waves, p.splits = r.splits, p.chunk = r.chunk;
+  } else {
+    p = tile_plan(M, N, nkb, split_ok);
+  }
+  p.ws_bytes = p.splits > 1 ? (size_t)p.splits * M * N * sizeof(float) : 0;
+  return p;
+}
+
+namespace {
+
+template <class C, class OUT>
+hipError_t launch_tile(LinearFp8Args a, int splits, hipStream_t s) {
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_tile_kernel<C, OUT>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, C::kLdsBytes);
+  if (attr != hipSuccess) return attr;
+  const int64_t tiles_m = cdiv(a.M, C::BM);
+  a.tiles_n = (int)cdiv(a.N, C::BN);
+  // tile-rows whose x (16 MB of it) stays cached while they sweep the columns, four at least
+  a.group_m = (int)std::max<int64_t>(1, std::min<int64_t>(tiles_m, std::max<int64_t>(4, ((int64_t)16 << 20) / ((int64_t)C::BM * a.K))));
+  hipLaunchKernelGGL((gemm_fp8_tile_kernel<C, OUT>), dim3((unsigned)(tiles_m * a.tiles_n * splits)), dim3(C::kThreads),
+                     C::kLdsBytes, s, a);
+  return hipGetLastError();
+}
+
+template <int TM, int NW, class OUT>
+hipError_t launch_rows_kernel(LinearFp8Args a, int splits, hipStream_t s) {
+  constexpr int lds = kStages * ((2 * TM + NW - 1) / NW * NW * 1024 + (16 * TM + 63) / 64 * 256);
+  static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(gemm_fp8_rows_kernel<TM, NW, OUT>),
+                                                     hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  if (attr != hipSuccess) return attr;
+  a.tiles_n = (int)cdiv(a.N, 16 * NW);
+  hipLaunchKernelGGL((gemm_fp8_rows_kernel<TM, NW, OUT>), dim3((unsigned)((int64_t)a.tiles_n * splits)), dim3(64 * NW),
+                     lds, s, a);
+  return hipGetLastError();
+}
+
+template <int TM, class OUT>
+hipError_t launch_rows(const LinearFp8Args& a, int waves, int splits, hipStream_t s) {
+  switch (waves) {
+    case 5: return launch_rows_kernel<TM, 5, OUT>(a, splits, s);
+    case 6: return launch_rows_kernel<TM, 6, OUT>(a, splits, s);
+    case 7: return launch_rows_kernel<TM, 7, OUT>(a, splits, s);
+    default: return launch_rows_kernel<TM, 8, OUT>(a, splits, s);
+  }
+}
+
+template <class OUT>
+hipError_t launch_fp8(const LinearFp8Plan& p, const LinearFp8Args& a, hipStream_t s) {
+  hipError_t e;
+  if (p.path == LinearFp8Plan::kRows) {
+    if (a.M <= 16) e = launch_rows<1, OUT>(a, p.waves, p.splits, s);
+    else if (a.M <= 32) e = launch_rows<2, OUT>(a, p.waves, p.splits, s);
+    else if (a.M <= 64) e = launch_rows<4, OUT>(a, p.waves, p.splits, s);
+    else e = launch_rows<8, OUT>(a, p.waves, p.splits, s);
+  } else if (p.path == LinearFp8Plan::kTile256) {
+    e = launch_tile<Tile256, OUT>(a, p.splits, s);
+  } else {
+    e = launch_tile<Tile128, OUT>(a, p.splits, s);
+  }
+  if (e != hipSuccess || p.splits <= 1) return e;
+  const int64_t MN = (int64_t)a.M * a.N;
+  hipLaunchKernelGGL((fp8_reduce_kernel<OUT>), dim3((unsigned)std::min<int64_t>(cdiv(MN / 4, 256), 2048)), dim3(256), 0, s,
+                     a.part, p.splits, static_cast<const OUT*>(a.bias), static_cast<OUT*>(a.y), MN, a.N);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_linear_fp8(const LinearFp8Plan& p, const void* x, const float* xs, const void* w, const float* ws,
+                             const void* bias, void* y, int64_t M, int64_t N, int64_t K, bool bf16, void* work,
+                             hipStream_t s) {
+  LinearFp8Args a{};
+  a.x = static_cast<const uint8_t*>(x), a.w = static_cast<const uint8_t*>(w), a.xs = xs, a.ws = ws;
+  a.bias = bias, a.y = y, a.part = p.splits > 1 ? static_cast<float*>(work) : nullptr;
+  a.M = (int)M, a.N = (int)N, a.K = (int)K, a.nkb = (int)cdiv(K, kFp8Block), a.chunk = p.chunk;
+  return bf16 ? launch_fp8<__bf16>(p, a, s) : launch_fp8<float>(p, a, s);
+}
+
+}  // namespace opscale

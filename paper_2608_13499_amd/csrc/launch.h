@@ -123,6 +123,38 @@ hipError_t launch_attn_decode_mod(const void* q, int64_t q_stride, const void* k
                                   int32_t block_size, int32_t max_blocks, int64_t num_blocks, int32_t max_context_len,
                                   float scale, const opscale_attn_mods* m, bool bf16, void* ws, hipStream_t s);
 
+// Activations to e4m3 and cache rows to and from e2m1 (k_quant.hip); strides in elements.
+hipError_t launch_quantize_fp8(const void* x, int64_t x_stride, void* q, float* scales, int64_t M, int64_t K, bool bf16,
+                               hipStream_t s);
+hipError_t launch_kv_write_fp4(const void* k, const void* v, int64_t stride, void* kc, void* vc, const int32_t* slots,
+                               int64_t T, int32_t Hkv, int32_t D, int32_t block_size, int64_t num_blocks, bool bf16,
+                               hipStream_t s);
+hipError_t launch_kv_read_fp4(const void* kc, const void* vc, const int32_t* table, const int32_t* cu,
+                              const int32_t* first, void* k, void* v, int64_t stride, int32_t B, int64_t T, int32_t Hkv,
+                              int32_t D, int32_t block_size, int32_t max_blocks, int64_t num_blocks, bool bf16,
+                              hipStream_t s);
+
+// Decode attention over such a cache; workspace as launch_attn_decode_mod's.
+hipError_t launch_attn_decode_fp4(const void* q, int64_t q_stride, const void* kc, const void* vc, const int32_t* table,
+                                  const int32_t* ctx, void* o, int32_t B, int32_t Hq, int32_t Hkv, int32_t D,
+                                  int32_t block_size, int32_t max_blocks, int64_t num_blocks, int32_t max_context_len,
+                                  float scale, const opscale_attn_mods* m, bool bf16, void* ws, hipStream_t s);
+
+// The linear of e4m3 operands (k_gemm_fp8.hip); the workspace query and the launch take
+// the same plan.  split_ok == false plans no K split, which needs no workspace.
+struct LinearFp8Plan {
+  enum Path { kRows = 0, kTile256 = 1, kTile128 = 2 };
+  int path;
+  int waves;        // rows: waves of a workgroup
+  int splits;       // K ranges (fp32 partials [splits, M, N] where more than one)
+  int chunk;        // blocks of K of a range
+  size_t ws_bytes;
+};
+LinearFp8Plan plan_linear_fp8(int64_t M, int64_t N, int64_t K, bool split_ok);
+hipError_t launch_linear_fp8(const LinearFp8Plan& p, const void* x, const float* xs, const void* w, const float* ws,
+                             const void* bias, void* y, int64_t M, int64_t N, int64_t K, bool bf16, void* work,
+                             hipStream_t s);
+
 // Rotary embedding of the q and k heads in place (rows of q_stride /
 // k_stride elements, token t at position pos[t]).
 hipError_t launch_rope(void* q, void* k, int64_t q_stride, int64_t k_stride, const int32_t* pos, int64_t T,
