@@ -709,7 +709,7 @@ opscale_status check_linear_fp8(const void* x, const float* xs, const void* W, c
   const Range in[] = {{x, M * K}, {W, N * K}, {xs, 4 * nkb * M}, {ws, 4 * nkb * ((N + 127) / 128)}, {bias, N * s}};
   for (const Range& r : in)
     if (r.p && overlap(y, ny, r.p, r.n)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: y must not overlap an input", who);
-  *plan = opscale::plan_linear_fp8(M, N, K, work != nullptr);
+  *plan = opscale::plan_linear_fp8(M, N, K, dt == OPSCALE_BF16, work != nullptr);
   if (plan->ws_bytes > 0) {
     if (work_bytes < plan->ws_bytes)
       return fail(OPSCALE_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu needed", who, work_bytes, plan->ws_bytes);
@@ -1241,7 +1241,7 @@ opscale_status opscale_quantize_fp8(const void* x, int64_t x_row_stride, void* q
 
 size_t opscale_linear_fp8_workspace_size(int64_t M, int64_t N, int64_t K, opscale_dtype dt) {
   if (M <= 0 || N <= 0 || K <= 0 || !dtype_ok(dt)) return 0;
-  return opscale::plan_linear_fp8(M, N, K, true).ws_bytes;
+  return opscale::plan_linear_fp8(M, N, K, dt == OPSCALE_BF16, true).ws_bytes;
 }
 
 opscale_status opscale_linear_fp8(const void* x, const float* x_scales, const void* W, const float* w_scales,

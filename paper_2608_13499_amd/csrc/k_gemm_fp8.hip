@@ -96,6 +96,24 @@ __device__ __forceinline__ void store4(OUT* y, const OUT* bias, int64_t at, int 
   }
 }
 
+// Eight consecutive columns from n on of the row of y that begins at `row`; those past N (a multiple
+// of four) are left out.
+template <class OUT>
+__device__ __forceinline__ void store8(OUT* y, const OUT* bias, int64_t row, int n, int N, f32x4 lo, f32x4 hi) {
+  if (sizeof(OUT) == 2 && n + 8 <= N) {
+    if (bias) {
+      const u32x4 b = *reinterpret_cast<const u32x4*>(bias + n);
+      lo[0] += bf_lo(b[0]), lo[1] += bf_hi(b[0]), lo[2] += bf_lo(b[1]), lo[3] += bf_hi(b[1]);
+      hi[0] += bf_lo(b[2]), hi[1] += bf_hi(b[2]), hi[2] += bf_lo(b[3]), hi[3] += bf_hi(b[3]);
+    }
+    *reinterpret_cast<u32x4*>(y + row + n) =
+        u32x4{pack_bf2(lo[0], lo[1]), pack_bf2(lo[2], lo[3]), pack_bf2(hi[0], hi[1]), pack_bf2(hi[2], hi[3])};
+  } else if (sizeof(OUT) == 4) {
+    if (n < N) store4(y, bias, row + n, n, lo);
+    if (n + 4 < N) store4(y, bias, row + n + 4, n + 4, hi);
+  }
+}
+
 struct LinearFp8Args {
   const uint8_t *x, *w;
   const float *xs, *ws;
@@ -110,24 +128,29 @@ struct LinearFp8Args {
 }  // namespace
 
 // ------------------------------------------------------------ tiles of many rows --
-// BM x BN of y a workgroup, WGM x WGN waves, an LDS ring of STAGES slices filled by LDS
-// DMA: a stage holds the slices of x's and W's rows, then the rows' scales.
-template <int BM_, int BN_, int WGM_, int WGN_, int STAGES_>
+// BM x BN of y a workgroup, WGM x WGN waves.  LDS holds XS slices of x's rows, with the
+// rows' scales, and two of W's, filled by LDS DMA.
+template <int BM_, int BN_, int WGM_, int WGN_, int XS_>
 struct Fp8Tile {
-  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, STAGES = STAGES_;
+  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, XS = XS_;
   static constexpr int kWaves = WGM * WGN, kThreads = 64 * kWaves;
   static constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16;
-  static constexpr int kXLoads = BM / 8 / kWaves, kWLoads = BN / 8 / kWaves, kLoads = kXLoads + kWLoads + 1;
-  static constexpr int kStageBytes = (BM + BN) * kSlice + BM * 4, kLdsBytes = STAGES * kStageBytes;
+  static constexpr int kXLoads = BM / 8 / kWaves + 1, kWLoads = BN / 8 / kWaves;  // of a wave (the scales' among them)
+  static constexpr int kXBytes = BM * kSlice + BM * 4, kWBytes = BN * kSlice;
+  static constexpr int kLdsBytes = XS * kXBytes + 2 * kWBytes;
   static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BM % 64 == 0, "whole loads");
   static_assert(kFp8Block % WN == 0 && BN % kFp8Block == 0, "a wave's columns lie in one block of W's scales");
-  static_assert((STAGES - 2) * kLoads <= 63, "vmcnt range");
+  static_assert((XS == 2 || XS == 3) && (TM == 4 || TM == 6 || TM == 8) && TN % 2 == 0, "the order of the slice loop");
+  // Registers of x's fragments: where row j of them is held.  Each differs from the one before
+  // it, the last two from the third last and from 0, where the next slice's first goes.
+  static constexpr int kSlots = TM == 4 ? 4 : 3;
+  static constexpr int slot(int j) { return TM == 4 ? j : j < TM - 3 ? j % 3 : j - (TM - 3); }
 };
 
 template <class C, class OUT>
 __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const LinearFp8Args a) {
   constexpr bool EXACT = sizeof(OUT) == 4;
-  constexpr int BM = C::BM, BN = C::BN, TM = C::TM, TN = C::TN, S = C::STAGES;
+  constexpr int BM = C::BM, BN = C::BN, TM = C::TM, TN = C::TN, XS = C::XS;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   OPS_LDS char* smem = (OPS_LDS char*)smem_raw;
   const int M = a.M, N = a.N, K = a.K;
@@ -149,35 +172,42 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   const int fr = lane & 15, fq = lane >> 4;
 
   // A load covers 8 rows; lane p writes chunk p % 8 of row p / 8, which holds chunk
-  // (p % 8) ^ (p / 8) of the row (gemm_bf16_kernel's layout: no bank conflicts).
+  // (p % 8) ^ (row's place in its fragment mod 8) of the row: the fragment reads are free of bank
+  // conflicts.  x's fragment j is rows 16 j ..  + 15; a pair of W's interleaves runs of four of
+  // its 32 rows, so that a lane's two sums are eight consecutive columns of y.
   const int c16 = ((lane & 7) ^ (lane >> 3)) * 16;
+  const int wc16 = ((lane & 7) ^ ((lane >> 3 & 3) | (wave & 1) << 2)) * 16;
   const int xrows = min(BM, M - m0), wrows = min(BN, N - n0);
   const uint8_t* xp = a.x + (int64_t)m0 * K;
   const uint8_t* wp = a.w + (int64_t)n0 * K;
-  uint32_t xo[C::kXLoads], wo[C::kWLoads];
+  constexpr int kMost = C::kXLoads - 1 > C::kWLoads ? C::kXLoads - 1 : C::kWLoads;
+  uint32_t from[kMost];
 #pragma unroll
-  for (int g = 0; g < C::kXLoads; ++g) xo[g] = (uint32_t)(((g * C::kWaves + wave) * 8 + (lane >> 3)) * K + c16);
-#pragma unroll
-  for (int g = 0; g < C::kWLoads; ++g) wo[g] = (uint32_t)(((g * C::kWaves + wave) * 8 + (lane >> 3)) * K + c16);
+  for (int g = 0; g < kMost; ++g) from[g] = (uint32_t)(((g * C::kWaves + wave) * 8 + (lane >> 3)) * K);
   const int sw = wave % (BM / 64);  // the rows whose scales this wave loads
 
   // Slices past the last one are loaded too, on descriptors of no records: every step issues
-  // the same loads, which the counted wait relies on.
-  auto load = [&](int kt, int stage) {
+  // the same loads, which the counted waits rely on.
+  OPS_LDS char* const xbuf = smem;
+  OPS_LDS char* const wbuf = smem + XS * C::kXBytes;
+  auto load_x = [&](int kt, OPS_LDS char* to) {
     const int k = (kb0 + kt) * kSlice;
     const bool live = kt < ns;
-    OPS_LDS char* st = smem + stage * C::kStageBytes;
-    const uint32_t off = k + c16 < K ? 0u : kOobOffset;
+    const uint32_t at = k + c16 < K ? c16 : kOobOffset;
     const __amdgpu_buffer_rsrc_t xr = make_rsrc(xp + k, live ? (uint32_t)((xrows - 1) * K + K - k) : 0u);
-    const __amdgpu_buffer_rsrc_t wr = make_rsrc(wp + k, live ? (uint32_t)((wrows - 1) * K + K - k) : 0u);
     const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.xs + (int64_t)(kb0 + kt) * M + m0, live ? (uint32_t)xrows * 4 : 0u);
 #pragma unroll
-    for (int g = 0; g < C::kXLoads; ++g)
-      buffer_load16_lds<kNoL1>(xr, st + (g * C::kWaves + wave) * 1024, xo[g] | off);
+    for (int g = 0; g < C::kXLoads - 1; ++g)
+      buffer_load16_lds<kNoL1>(xr, to + (g * C::kWaves + wave) * 1024, from[g] + at);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, to + BM * kSlice + sw * 256, 4, (sw * 64 + lane) * 4, 0, 0, 0);
+  };
+  auto load_w = [&](int kt) {
+    const int k = (kb0 + kt) * kSlice;
+    const uint32_t at = k + wc16 < K ? wc16 : kOobOffset;
+    const __amdgpu_buffer_rsrc_t wr = make_rsrc(wp + k, kt < ns ? (uint32_t)((wrows - 1) * K + K - k) : 0u);
 #pragma unroll
     for (int g = 0; g < C::kWLoads; ++g)
-      buffer_load16_lds<kNoL1>(wr, st + BM * kSlice + (g * C::kWaves + wave) * 1024, wo[g] | off);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, st + (BM + BN) * kSlice + sw * 256, 4, (sw * 64 + lane) * 4, 0, 0, 0);
+      buffer_load16_lds<kNoL1>(wr, wbuf + (kt & 1) * C::kWBytes + (g * C::kWaves + wave) * 1024, from[g] + at);
   };
 
   f32x4 acc[TN][TM];
@@ -186,41 +216,116 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
 #pragma unroll
     for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{};
 
-  int off[2];
+  int off[2], woff[2];
 #pragma unroll
-  for (int h = 0; h < 2; ++h) off[h] = fr * kSlice + (((4 * h + fq) ^ (fr & 7)) << 4);
-  const int x0 = wm * C::WM * kSlice, w0 = BM * kSlice + wn * C::WN * kSlice;
-  const int s0 = (BM + BN) * kSlice + (wm * C::WM + fr) * 4;
-  // W's scales of this wave's columns, a lane each for 64 slices
+  for (int h = 0; h < 2; ++h) {
+    const int chunk = ((4 * h + fq) ^ (fr & 7)) << 4;
+    off[h] = fr * kSlice + chunk;
+    woff[h] = (8 * (fr >> 2) + (fr & 3)) * kSlice + chunk;
+  }
+  const int x0 = wm * C::WM * kSlice, w0 = wn * C::WN * kSlice, s0 = BM * kSlice + (wm * C::WM + fr) * 4;
   const float* wsp = a.ws + (int64_t)(min(n0 + wn * C::WN, N - 1) / kFp8Block) * a.nkb + kb0;
-  float wscales = 0.f;
 
-#pragma unroll
-  for (int s = 0; s < S - 1; ++s) load(s, s);
-  int stage = 0;
-  for (int kt = 0; kt < ns; ++kt) {
-    if ((kt & 63) == 0) wscales = kt + lane < ns ? wsp[kt + lane] : 0.f;
-    wait_vmcnt_le<(S - 2) * C::kLoads>();
+  // Slice kt: W's fragments are in registers from the start, so that behind a barrier (`left`) W's
+  // slice kt + 2 is sent for into their place.  The last two rows of x's fragments are read before
+  // the second barrier (`ready`); behind it their MFMAs run while the first fragments of slice
+  // kt + 1 are read into the registers that they free, and slice kt + XS of x is sent for.
+  Frag w[TN], x[C::kSlots];
+  float f[C::kSlots];
+  OPS_LDS char* xst = xbuf;
+  auto next_stage = [&](OPS_LDS char* st) { return st == xbuf + (XS - 1) * C::kXBytes ? xbuf : st + C::kXBytes; };
+  auto read_x = [&](int j) {
+    x[C::slot(j)] = read_frag(xst + x0 + j * 16 * kSlice, off);
+    f[C::slot(j)] = *reinterpret_cast<const OPS_LDS float*>(xst + s0 + j * 64);
+  };
+  auto read_w = [&](int kt, int i) {
+    w[i] = read_frag(wbuf + (kt & 1) * C::kWBytes + w0 + (32 * (i >> 1) + 4 * (i & 1)) * kSlice, woff);
+  };
+  // x's and W's next slices have arrived, in every wave; what was sent for after them need not have
+  auto ready = [&] {
+    wait_vmcnt_le<C::kWLoads + (XS - 2) * C::kXLoads>();
     barrier_keep_loads();
-    const int next = stage == 0 ? S - 1 : stage - 1;  // the stage of slice kt - 1
-    load(kt + S - 1, next);
-    const OPS_LDS char* st = smem + stage * C::kStageBytes;
-    const float wscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), kt & 63));
-    Frag w[TN];
+  };
+  // A product is scaled and added a group of products after its own: p holds a group, of TN
+  // (or two rows of x of TN / 2) products.
+  f32x4 p[2][TN];
+  auto add = [&](f32x4& to, const f32x4& from, float scale) {
 #pragma unroll
-    for (int i = 0; i < TN; ++i) w[i] = read_frag(st + w0 + i * 16 * kSlice, off);
+    for (int r = 0; r < 4; ++r) to[r] = fmaf(scale, from[r], to[r]);
+  };
+
+  if constexpr (XS == 3) load_x(0, xbuf);
+  load_w(0);
+  load_x(XS - 2, xbuf + (XS - 2) * C::kXBytes);
+  load_w(1);
+  ready();
+  load_x(XS - 1, xbuf + (XS - 1) * C::kXBytes);
+  read_x(0);
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const Frag x = read_frag(st + x0 + j * 16 * kSlice, off);
-      const float f = *reinterpret_cast<const OPS_LDS float*>(st + s0 + j * 64) * wscale;
+  for (int i = 0; i < TN; ++i) read_w(0, i);
+  auto pin = [] { __builtin_amdgcn_sched_barrier(0); };
+  constexpr int ja = TM - 2, jb = TM - 1, TH = TN / 2;
+  for (int kw = 0; kw < ns; kw += 64) {
+    const float wscales = kw + lane < ns ? wsp[kw + lane] : 0.f;  // W's scales of 64 slices, a lane each
+    const int end = min(ns, kw + 64);
+    for (int kt = kw; kt < end; ++kt) {
+      const float wscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), kt & 63));
+      float scale[C::kSlots];
 #pragma unroll
-      for (int i = 0; i < TN; ++i) {
-        const f32x4 p = block_product<EXACT>(w[i], x);
+      for (int j = 0; j < TM - 2; ++j) {
+        read_x(j + 1);
+        if (j == TM - 3) read_x(j + 2);
+        scale[C::slot(j)] = f[C::slot(j)] * wscale;
+        pin();
 #pragma unroll
-        for (int r = 0; r < 4; ++r) acc[i][j][r] = fmaf(f, p[r], acc[i][j][r]);
+        for (int i = 0; i < TN; ++i) {
+          p[j & 1][i] = block_product<EXACT>(w[i], x[C::slot(j)]);
+          pin();
+          if (j > 0) add(acc[i][j - 1], p[~j & 1][i], scale[C::slot(j - 1)]);
+          pin();
+        }
+        if (j == 0) {
+          barrier_keep_loads();  // (left)
+          load_w(kt + 2);
+          pin();
+        }
+      }
+      scale[C::slot(ja)] = f[C::slot(ja)] * wscale, scale[C::slot(jb)] = f[C::slot(jb)] * wscale;
+      ready();
+      pin();
+      load_x(kt + XS, xst);
+      xst = next_stage(xst);
+      pin();
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        constexpr int last = (TM - 3) & 1;  // p of row TM - 3, then of the halves
+#pragma unroll
+        for (int i = 0; i < TH; ++i) {
+          const int n = h * TH + i;
+          f32x4(&to)[TN] = p[h == 0 ? 1 - last : last];
+          const f32x4(&of)[TN] = p[h == 0 ? last : 1 - last];
+          to[2 * i] = block_product<EXACT>(w[n], x[C::slot(ja)]);
+          pin();
+          if (h == 0) add(acc[2 * i][TM - 3], of[2 * i], scale[C::slot(TM - 3)]);
+          else add(acc[i][ja], of[2 * i], scale[C::slot(ja)]);
+          pin();
+          to[2 * i + 1] = block_product<EXACT>(w[n], x[C::slot(jb)]);
+          pin();
+          if (h == 0) add(acc[2 * i + 1][TM - 3], of[2 * i + 1], scale[C::slot(TM - 3)]);
+          else add(acc[i][jb], of[2 * i + 1], scale[C::slot(jb)]);
+          pin();
+          if (n == 0) read_x(0);
+          read_w(kt + 1, n);
+          pin();
+        }
+        if (h == 1)
+#pragma unroll
+          for (int i = 0; i < TH; ++i) {
+            add(acc[TH + i][ja], p[last][2 * i], scale[C::slot(ja)]);
+            add(acc[TH + i][jb], p[last][2 * i + 1], scale[C::slot(jb)]);
+          }
       }
     }
-    stage = stage + 1 == S ? 0 : stage + 1;
   }
   wait_vmem();  // no LDS DMA may be in flight when the workgroup ends
 
@@ -229,11 +334,10 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
     const int m = m0 + wm * C::WM + 16 * j + fr;
     if (m >= M) continue;
 #pragma unroll
-    for (int i = 0; i < TN; ++i) {
-      const int n = n0 + wn * C::WN + 16 * i + 4 * fq;
-      if (n >= N) continue;
-      if (a.part) *reinterpret_cast<f32x4*>(a.part + ((int64_t)split * M + m) * N + n) = acc[i][j];
-      else store4(static_cast<OUT*>(a.y), static_cast<const OUT*>(a.bias), (int64_t)m * N + n, n, acc[i][j]);
+    for (int i = 0; i < TN; i += 2) {
+      const int n = n0 + wn * C::WN + 16 * i + 8 * fq;
+      if (a.part) store8<float>(a.part, nullptr, ((int64_t)split * M + m) * N, n, N, acc[i][j], acc[i + 1][j]);
+      else store8(static_cast<OUT*>(a.y), static_cast<const OUT*>(a.bias), (int64_t)m * N, n, N, acc[i][j], acc[i + 1][j]);
     }
   }
 }
@@ -392,8 +496,8 @@ __global__ __launch_bounds__(256) void fp8_reduce_kernel(const float* __restrict
 
 namespace {
 
-using Tile256 = Fp8Tile<256, 256, 2, 4, 2>;  // 8 waves of 128 x 64, 2 x 65 KB
-using Tile128 = Fp8Tile<128, 128, 2, 2, 2>;  // 4 waves of 64 x 64, 2 x 32.5 KB, two workgroups a CU
+using Tile256 = Fp8Tile<256, 256, 2, 4, 2>;  // 8 waves of 128 x 64, 130 KB
+using Tile128 = Fp8Tile<128, 128, 2, 2, 2>;  // 4 waves of 64 x 64, 65 KB: two workgroups a CU
 
 constexpr int64_t kRowsMaxM = 128;
 
@@ -419,11 +523,12 @@ RowsShape rows_shape(int64_t N, int64_t nkb, bool split_ok) {
 
 // Tiles: the smaller ones where the larger leave more of the chip idle, and K split where
 // even those are fewer than the CUs.
-LinearFp8Plan tile_plan(int64_t M, int64_t N, int64_t nkb, bool split_ok) {
+LinearFp8Plan tile_plan(int64_t M, int64_t N, int64_t nkb, bool bf16, bool split_ok) {
   LinearFp8Plan p{};
   const int64_t big = cdiv(M, 256) * cdiv(N, 256), small = cdiv(M, 128) * cdiv(N, 128);
   const double t_big = 2.2 * cdiv(big, kNumCUs), t_small = 0.8 * cdiv(small, kNumCUs);
-  p.path = t_big <= t_small ? LinearFp8Plan::kTile256 : LinearFp8Plan::kTile128;
+  // (fp32 results: the widened operands and the larger tile's sums are more than the registers)
+  p.path = bf16 && t_big <= t_small ? LinearFp8Plan::kTile256 : LinearFp8Plan::kTile128;
   const int64_t tiles = p.path == LinearFp8Plan::kTile256 ? big : small;
   int64_t splits = 1;
   if (split_ok && tiles < kNumCUs) splits = std::max<int64_t>(1, std::min<int64_t>(2 * kNumCUs / tiles, nkb / 8));
@@ -434,7 +539,7 @@ LinearFp8Plan tile_plan(int64_t M, int64_t N, int64_t nkb, bool split_ok) {
 
 }  // namespace
 
-LinearFp8Plan plan_linear_fp8(int64_t M, int64_t N, int64_t K, bool split_ok) {
+LinearFp8Plan plan_linear_fp8(int64_t M, int64_t N, int64_t K, bool bf16, bool split_ok) {
   const int64_t nkb = cdiv(K, kFp8Block);
   LinearFp8Plan p{};
   if (M <= kRowsMaxM) {
@@ -442,7 +547,7 @@ LinearFp8Plan plan_linear_fp8(int64_t M, int64_t N, int64_t K, bool split_ok) {
     p.path = LinearFp8Plan::kRows;
     p.waves = r.waves, p.splits = r.splits, p.chunk = r.chunk;
   } else {
-    p = tile_plan(M, N, nkb, split_ok);
+    p = tile_plan(M, N, nkb, bf16, split_ok);
   }
   p.ws_bytes = p.splits > 1 ? (size_t)p.splits * M * N * sizeof(float) : 0;
   return p;
@@ -495,7 +600,8 @@ hipError_t launch_fp8(const LinearFp8Plan& p, const LinearFp8Args& a, hipStream_
     else if (a.M <= 64) e = launch_rows<4, OUT>(a, p.waves, p.splits, s);
     else e = launch_rows<8, OUT>(a, p.waves, p.splits, s);
   } else if (p.path == LinearFp8Plan::kTile256) {
-    e = launch_tile<Tile256, OUT>(a, p.splits, s);
+    if constexpr (sizeof(OUT) == 2) e = launch_tile<Tile256, OUT>(a, p.splits, s);
+    else e = hipErrorInvalidValue;  // (not planned)
   } else {
     e = launch_tile<Tile128, OUT>(a, p.splits, s);
   }

@@ -150,7 +150,7 @@ struct LinearFp8Plan {
   int chunk;        // blocks of K of a range
   size_t ws_bytes;
 };
-LinearFp8Plan plan_linear_fp8(int64_t M, int64_t N, int64_t K, bool split_ok);
+LinearFp8Plan plan_linear_fp8(int64_t M, int64_t N, int64_t K, bool bf16, bool split_ok);
 hipError_t launch_linear_fp8(const LinearFp8Plan& p, const void* x, const float* xs, const void* w, const float* ws,
                              const void* bias, void* y, int64_t M, int64_t N, int64_t K, bool bf16, void* work,
                              hipStream_t s);
