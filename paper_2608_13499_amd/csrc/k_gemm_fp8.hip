@@ -122,25 +122,27 @@ struct LinearFp8Args {
   float* part;  // not null: fp32 partials [split, M, N]
   int M, N, K, nkb;
   int tiles_n, group_m;  // column tiles; tile-rows that sweep them together
-  int chunk;             // slices of a split
+  int chunk, splits;     // slices of a split
+  bool chained;          // tiles: several items a workgroup
 };
 
 }  // namespace
 
 // ------------------------------------------------------------ tiles of many rows --
-// BM x BN of y a workgroup, WGM x WGN waves.  LDS holds XS slices of x's rows, with the
-// rows' scales, and two of W's, filled by LDS DMA.
-template <int BM_, int BN_, int WGM_, int WGN_, int XS_>
+// BM x BN of y an item, 2 x WGN waves.  LDS holds two slices of x's and W's rows and four of their
+// scales, filled by LDS DMA.
+template <int BM_, int BN_, int WGN_>
 struct Fp8Tile {
-  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, XS = XS_;
+  static constexpr int BM = BM_, BN = BN_, WGM = 2, WGN = WGN_;
   static constexpr int kWaves = WGM * WGN, kThreads = 64 * kWaves;
   static constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16;
-  static constexpr int kXLoads = BM / 8 / kWaves + 1, kWLoads = BN / 8 / kWaves;  // of a wave (the scales' among them)
-  static constexpr int kXBytes = BM * kSlice + BM * 4, kWBytes = BN * kSlice;
-  static constexpr int kLdsBytes = XS * kXBytes + 2 * kWBytes;
-  static_assert(BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BM % 64 == 0, "whole loads");
+  static constexpr int kLoads = BN / 8 / kWaves;  // of a wave: of W's rows, and of x's
+  static constexpr int kScales = BM * 4 + 256;  // x's, then W's
+  static constexpr int kStageBytes = (BM + BN) * kSlice, kLdsBytes = 2 * kStageBytes + 4 * kScales;
+  static constexpr bool kChained = BM > 128;  // one workgroup a CU
+  static_assert(BM == BN && BN % (8 * kWaves) == 0 && BM / 64 < kWaves, "whole loads");
   static_assert(kFp8Block % WN == 0 && BN % kFp8Block == 0, "a wave's columns lie in one block of W's scales");
-  static_assert((XS == 2 || XS == 3) && (TM == 4 || TM == 6 || TM == 8) && TN % 2 == 0, "the order of the slice loop");
+  static_assert((TM == 4 || TM == 8) && TN == 4 && kLoads == 4, "the order of the slice loop");
   // Registers of x's fragments: where row j of them is held.  Each differs from the one before
   // it, the last two from the third last and from 0, where the next slice's first goes.
   static constexpr int kSlots = TM == 4 ? 4 : 3;
@@ -150,23 +152,17 @@ struct Fp8Tile {
 template <class C, class OUT>
 __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const LinearFp8Args a) {
   constexpr bool EXACT = sizeof(OUT) == 4;
-  constexpr int BM = C::BM, BN = C::BN, TM = C::TM, TN = C::TN, XS = C::XS;
+  constexpr int BM = C::BM, BN = C::BN, TM = C::TM, TN = C::TN;
   extern __shared__ __attribute__((aligned(16))) char smem_raw[];
   OPS_LDS char* smem = (OPS_LDS char*)smem_raw;
   const int M = a.M, N = a.N, K = a.K;
 
-  const int tiles_m = (M + BM - 1) / BM, tiles = tiles_m * a.tiles_n;
-  const int split = blockIdx.x / tiles;
-  const int tid = (int)xcd_remap(blockIdx.x - split * tiles, (uint32_t)tiles);
-  int m0, n0;
-  {
-    const int per = a.group_m * a.tiles_n, group = tid / per, first = group * a.group_m;
-    const int rows = min(tiles_m - first, a.group_m), in = tid - group * per;
-    m0 = (first + in % rows) * BM;
-    n0 = in / rows * BN;
-  }
-  const int kb0 = split * a.chunk, ns = min(a.chunk, a.nkb - kb0);
-
+  // This workgroup's chain of items (a tile and a range of K): id, id + kNumCUs, ... below id_end.
+  const int tiles_m = (M + BM - 1) / BM, tiles = tiles_m * a.tiles_n, items = tiles * a.splits;
+  const Chain ch = chain_of((int)(blockIdx.x / kNumCUs), (items + kNumCUs - 1) / kNumCUs, a.chained);
+  int id = __builtin_amdgcn_readfirstlane(ch.first * kNumCUs + (int)(blockIdx.x % kNumCUs));
+  const int id_end = __builtin_amdgcn_readfirstlane(min(items, (ch.first + ch.len) * kNumCUs));
+  if (id >= id_end) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int wm = wave % C::WGM, wn = wave / C::WGM;
   const int fr = lane & 15, fq = lane >> 4;
@@ -177,45 +173,80 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   // its 32 rows, so that a lane's two sums are eight consecutive columns of y.
   const int c16 = ((lane & 7) ^ (lane >> 3)) * 16;
   const int wc16 = ((lane & 7) ^ ((lane >> 3 & 3) | (wave & 1) << 2)) * 16;
-  const int xrows = min(BM, M - m0), wrows = min(BN, N - n0);
-  const uint8_t* xp = a.x + (int64_t)m0 * K;
-  const uint8_t* wp = a.w + (int64_t)n0 * K;
-  constexpr int kMost = C::kXLoads - 1 > C::kWLoads ? C::kXLoads - 1 : C::kWLoads;
-  uint32_t from[kMost];
+  uint32_t from[C::kLoads];  // of x's rows, and of W's
 #pragma unroll
-  for (int g = 0; g < kMost; ++g) from[g] = (uint32_t)(((g * C::kWaves + wave) * 8 + (lane >> 3)) * K);
-  const int sw = wave % (BM / 64);  // the rows whose scales this wave loads
+  for (int g = 0; g < C::kLoads; ++g) from[g] = (uint32_t)(((g * C::kWaves + wave) * 8 + (lane >> 3)) * K);
+  // The scales: each of the first BM / 64 waves loads those of 64 rows of x, the others those of W's
+  // BN / 128 blocks.
+  const bool x_scales = wave < BM / 64;
+  const int s_to = 2 * C::kStageBytes + (x_scales ? wave * 256 : BM * 4);
+  const uint32_t s_from = x_scales ? (uint32_t)(wave * 64 + lane) * 4 : lane < BN / kFp8Block ? (uint32_t)(lane * a.nkb) * 4 : kOobOffset;
 
-  // Slices past the last one are loaded too, on descriptors of no records: every step issues
-  // the same loads, which the counted waits rely on.
-  OPS_LDS char* const xbuf = smem;
-  OPS_LDS char* const wbuf = smem + XS * C::kXBytes;
-  auto load_x = [&](int kt, OPS_LDS char* to) {
-    const int k = (kb0 + kt) * kSlice;
-    const bool live = kt < ns;
-    const uint32_t at = k + c16 < K ? c16 : kOobOffset;
-    const __amdgpu_buffer_rsrc_t xr = make_rsrc(xp + k, live ? (uint32_t)((xrows - 1) * K + K - k) : 0u);
-    const __amdgpu_buffer_rsrc_t sr = make_rsrc(a.xs + (int64_t)(kb0 + kt) * M + m0, live ? (uint32_t)xrows * 4 : 0u);
-#pragma unroll
-    for (int g = 0; g < C::kXLoads - 1; ++g)
-      buffer_load16_lds<kNoL1>(xr, to + (g * C::kWaves + wave) * 1024, from[g] + at);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(sr, to + BM * kSlice + sw * 256, 4, (sw * 64 + lane) * 4, 0, 0, 0);
+  struct Item {
+    int m0, n0, split, ns;
   };
-  auto load_w = [&](int kt) {
-    const int k = (kb0 + kt) * kSlice;
-    const uint32_t at = k + wc16 < K ? wc16 : kOobOffset;
-    const __amdgpu_buffer_rsrc_t wr = make_rsrc(wp + k, kt < ns ? (uint32_t)((wrows - 1) * K + K - k) : 0u);
-#pragma unroll
-    for (int g = 0; g < C::kWLoads; ++g)
-      buffer_load16_lds<kNoL1>(wr, wbuf + (kt & 1) * C::kWBytes + (g * C::kWaves + wave) * 1024, from[g] + at);
+  auto item = [&](int i) {
+    // (scalar divisions run in vector registers: the results are taken out of them, or all that
+    // follows would stay there)
+    auto scalar = [](int v) { return (int)__builtin_amdgcn_readfirstlane(v); };
+    Item it;
+    it.split = scalar(i / tiles);
+    const int tid = (int)xcd_remap(i - it.split * tiles, (uint32_t)tiles);
+    const int per = a.group_m * a.tiles_n, group = scalar(tid / per), first = group * a.group_m;
+    const int rows = min(tiles_m - first, a.group_m), in = tid - group * per, tn = scalar(in / rows);
+    it.m0 = (first + in - tn * rows) * BM;
+    it.n0 = tn * BN;
+    it.ns = min(a.chunk, a.nkb - it.split * a.chunk);
+    return it;
+  };
+  // The slice that is loaded next, up to two ahead of the one in use and into the next item, which
+  // begins at `to`.  Past the chain's end the loads go on, on descriptors of no records: every step
+  // issues the same loads, which the counted waits rely on.
+  struct Slice {
+    uint64_t x, w, s;           // the tile's first rows at the slice; x's or W's scales there
+    uint32_t xrec, wrec, srec;  // bytes from there on
+    uint32_t k, left, step;     // left: slices of the item; step: to the next one (0 past the end)
+  } at, to;
+  const uint64_t s_step = (x_scales ? (uint64_t)M : 1) * 4;
+  auto begin = [&](const Item& it, bool live) {
+    Slice b;
+    const int kb = it.split * a.chunk, xrows = min(BM, M - it.m0), wrows = min(BN, N - it.n0);
+    b.k = kb * kSlice, b.left = live ? it.ns : 1u << 30;
+    b.x = (uint64_t)(a.x + (int64_t)it.m0 * K + b.k);
+    b.w = (uint64_t)(a.w + (int64_t)it.n0 * K + b.k);
+    b.s = (uint64_t)(x_scales ? a.xs + (int64_t)kb * M + it.m0 : a.ws + (int64_t)(it.n0 / kFp8Block) * a.nkb + kb);
+    b.xrec = live ? (uint32_t)(xrows * K) - b.k : 0u, b.wrec = live ? (uint32_t)(wrows * K) - b.k : 0u;
+    b.srec = live ? (x_scales ? xrows * 4 : ((wrows - 1) / kFp8Block * a.nkb + 1) * 4) : 0u;
+    b.step = live ? kSlice : 0;
+    return b;
+  };
+  auto advance = [&] {  // (without a branch: that would cost the slice loop its registers)
+    uint32_t over = at.left == 1 ? ~0u : 0u;
+    const uint64_t over64 = (uint64_t)over << 32 | over;
+    auto pick = [&](uint32_t n, uint32_t v) { return (n & over) | (v & ~over); };
+    auto pick64 = [&](uint64_t n, uint64_t v) { return (n & over64) | (v & ~over64); };
+    at.x = pick64(to.x, at.x + at.step), at.w = pick64(to.w, at.w + at.step), at.s = pick64(to.s, at.s + s_step);
+    at.xrec = pick(to.xrec, at.xrec - at.step), at.wrec = pick(to.wrec, at.wrec - at.step);
+    at.srec = pick(to.srec, at.srec), at.k = pick(to.k, at.k + at.step);
+    at.left = pick(to.left, at.left - 1), at.step = pick(to.step, at.step);
+  };
+  // one load each: rows of x and of W, and the scales
+  auto load_x = [&](int g, OPS_LDS char* st) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc((const void*)at.x, at.xrec);
+    const uint32_t lane_at = (int)at.k + c16 < K ? c16 : kOobOffset;
+    buffer_load16_lds<kNoL1>(r, st + (g * C::kWaves + wave) * 1024, from[g] + lane_at);
+  };
+  auto load_w = [&](int g, OPS_LDS char* st) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc((const void*)at.w, at.wrec);
+    const uint32_t lane_at = (int)at.k + wc16 < K ? wc16 : kOobOffset;
+    buffer_load16_lds<kNoL1>(r, st + BM * kSlice + (g * C::kWaves + wave) * 1024, from[g] + lane_at);
+  };
+  auto load_scales = [&](int slice) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc((const void*)at.s, at.srec);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, smem + s_to + (slice & 3) * C::kScales, 4, s_from, 0, 0, 0);
   };
 
   f32x4 acc[TN][TM];
-#pragma unroll
-  for (int i = 0; i < TN; ++i)
-#pragma unroll
-    for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{};
-
   int off[2], woff[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
@@ -223,27 +254,30 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
     off[h] = fr * kSlice + chunk;
     woff[h] = (8 * (fr >> 2) + (fr & 3)) * kSlice + chunk;
   }
-  const int x0 = wm * C::WM * kSlice, w0 = wn * C::WN * kSlice, s0 = BM * kSlice + (wm * C::WM + fr) * 4;
-  const float* wsp = a.ws + (int64_t)(min(n0 + wn * C::WN, N - 1) / kFp8Block) * a.nkb + kb0;
+  const int x0 = wm * C::WM * kSlice, w0 = (BM + wn * C::WN) * kSlice;
+  const int s0 = 2 * C::kStageBytes + (wm * C::WM + fr) * 4;
+  const int ws0 = 2 * C::kStageBytes + BM * 4 + wn * C::WN / kFp8Block * 4;
 
-  // Slice kt: W's fragments are in registers from the start, so that behind a barrier (`left`) W's
-  // slice kt + 2 is sent for into their place.  The last two rows of x's fragments are read before
-  // the second barrier (`ready`); behind it their MFMAs run while the first fragments of slice
-  // kt + 1 are read into the registers that they free, and slice kt + XS of x is sent for.
+  // A slice: W's fragments are in registers from the start, so that behind a barrier W's slice after
+  // the next is sent for into their place.  The last two rows of x's fragments are read before the
+  // second barrier; behind it their MFMAs run while the next slice's first fragments are read into
+  // the registers that they free, and x's slice after the next is sent for.  The loads are spread
+  // between the MFMAs: those of all waves at once would fill the address unit's queue, and a wave
+  // that waits there issues no MFMA.
   Frag w[TN], x[C::kSlots];
-  float f[C::kSlots];
-  OPS_LDS char* xst = xbuf;
-  auto next_stage = [&](OPS_LDS char* st) { return st == xbuf + (XS - 1) * C::kXBytes ? xbuf : st + C::kXBytes; };
+  float f[C::kSlots], wscale;
+  OPS_LDS char* st = smem;
+  int slices = 0;  // past, of all items
   auto read_x = [&](int j) {
-    x[C::slot(j)] = read_frag(xst + x0 + j * 16 * kSlice, off);
-    f[C::slot(j)] = *reinterpret_cast<const OPS_LDS float*>(xst + s0 + j * 64);
+    x[C::slot(j)] = read_frag(st + x0 + j * 16 * kSlice, off);
+    f[C::slot(j)] = *reinterpret_cast<const OPS_LDS float*>(smem + s0 + (slices & 3) * C::kScales + j * 64);
   };
-  auto read_w = [&](int kt, int i) {
-    w[i] = read_frag(wbuf + (kt & 1) * C::kWBytes + w0 + (32 * (i >> 1) + 4 * (i & 1)) * kSlice, woff);
-  };
-  // x's and W's next slices have arrived, in every wave; what was sent for after them need not have
+  auto read_w = [&](int i) { w[i] = read_frag(st + w0 + (32 * (i >> 1) + 4 * (i & 1)) * kSlice, woff); };
+  auto read_wscale = [&] { return *reinterpret_cast<const OPS_LDS float*>(smem + ws0 + (slices & 3) * C::kScales); };
+  auto other = [&] { return st == smem ? smem + C::kStageBytes : smem; };
+  // The next slice has arrived, in every wave (W's slice after it need not have).
   auto ready = [&] {
-    wait_vmcnt_le<C::kWLoads + (XS - 2) * C::kXLoads>();
+    wait_vmcnt_le<C::kLoads + 1>();
     barrier_keep_loads();
   };
   // A product is scaled and added a group of products after its own: p holds a group, of TN
@@ -253,29 +287,49 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
 #pragma unroll
     for (int r = 0; r < 4; ++r) to[r] = fmaf(scale, from[r], to[r]);
   };
-
-  if constexpr (XS == 3) load_x(0, xbuf);
-  load_w(0);
-  load_x(XS - 2, xbuf + (XS - 2) * C::kXBytes);
-  load_w(1);
-  ready();
-  load_x(XS - 1, xbuf + (XS - 1) * C::kXBytes);
-  read_x(0);
-#pragma unroll
-  for (int i = 0; i < TN; ++i) read_w(0, i);
   auto pin = [] { __builtin_amdgcn_sched_barrier(0); };
   constexpr int ja = TM - 2, jb = TM - 1, TH = TN / 2;
-  for (int kw = 0; kw < ns; kw += 64) {
-    const float wscales = kw + lane < ns ? wsp[kw + lane] : 0.f;  // W's scales of 64 slices, a lane each
-    const int end = min(ns, kw + 64);
-    for (int kt = kw; kt < end; ++kt) {
-      const float wscale = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(wscales), kt & 63));
+
+  Item it = item(id), next;
+  auto look_ahead = [&] {
+    const bool more = id + kNumCUs < id_end;
+    next = item(more ? id + kNumCUs : id);
+    to = begin(next, more);
+  };
+  at = begin(it, true);
+  look_ahead();
+#pragma unroll
+  for (int slice = 0; slice < 2; ++slice) {
+    if (slice == 0)
+#pragma unroll
+      for (int g = 0; g < C::kLoads; ++g) load_x(g, smem);
+    load_scales(slice);
+#pragma unroll
+    for (int g = 0; g < C::kLoads; ++g) load_w(g, smem + slice * C::kStageBytes);
+    if (slice == 0) advance();
+  }
+  ready();
+#pragma unroll
+  for (int g = 0; g < C::kLoads; ++g) load_x(g, other());
+  advance();
+  read_x(0);
+  wscale = read_wscale();
+#pragma unroll
+  for (int i = 0; i < TN; ++i) read_w(i);
+
+  for (;;) {
+#pragma unroll
+    for (int i = 0; i < TN; ++i)
+#pragma unroll
+      for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{};
+    for (int kt = 0; kt < it.ns; ++kt) {
       float scale[C::kSlots];
+      const float ws = wscale;
 #pragma unroll
       for (int j = 0; j < TM - 2; ++j) {
         read_x(j + 1);
         if (j == TM - 3) read_x(j + 2);
-        scale[C::slot(j)] = f[C::slot(j)] * wscale;
+        scale[C::slot(j)] = f[C::slot(j)] * ws;
         pin();
 #pragma unroll
         for (int i = 0; i < TN; ++i) {
@@ -283,19 +337,26 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
           pin();
           if (j > 0) add(acc[i][j - 1], p[~j & 1][i], scale[C::slot(j - 1)]);
           pin();
+          if (j > 0) {  // W's four loads and the scales', over the rows 1 to TM - 3
+            constexpr int kMfmas = TN * (TM - 3);
+            const int n = (j - 1) * TN + i;
+#pragma unroll
+            for (int g = 0; g < C::kLoads + 1; ++g)
+              if (n == g * kMfmas / (C::kLoads + 1)) {
+                if (g == 0) load_scales(slices + 2);
+                else load_w(g - 1, st);
+              }
+            pin();
+          }
         }
-        if (j == 0) {
-          barrier_keep_loads();  // (left)
-          load_w(kt + 2);
-          pin();
-        }
+        if (j == 0) barrier_keep_loads();
       }
-      scale[C::slot(ja)] = f[C::slot(ja)] * wscale, scale[C::slot(jb)] = f[C::slot(jb)] * wscale;
+      scale[C::slot(ja)] = f[C::slot(ja)] * ws, scale[C::slot(jb)] = f[C::slot(jb)] * ws;
       ready();
       pin();
-      load_x(kt + XS, xst);
-      xst = next_stage(xst);
-      pin();
+      OPS_LDS char* const left = st;
+      st = other();
+      ++slices;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         constexpr int last = (TM - 3) & 1;  // p of row TM - 3, then of the halves
@@ -314,8 +375,12 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
           if (h == 0) add(acc[2 * i + 1][TM - 3], of[2 * i + 1], scale[C::slot(TM - 3)]);
           else add(acc[i][jb], of[2 * i + 1], scale[C::slot(jb)]);
           pin();
-          if (n == 0) read_x(0);
-          read_w(kt + 1, n);
+          if (n == 0) {
+            read_x(0);
+            wscale = read_wscale();
+          }
+          read_w(n);
+          load_x(n, left);
           pin();
         }
         if (h == 1)
@@ -325,21 +390,28 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
             add(acc[TH + i][jb], p[last][2 * i + 1], scale[C::slot(jb)]);
           }
       }
+      advance();
     }
+
+    // The item's results; the next one's first slices are on their way, its first fragments here.
+#pragma unroll
+    for (int j = 0; j < TM; ++j) {
+      const int m = it.m0 + wm * C::WM + 16 * j + fr;
+      pin();
+      if (m >= M) continue;
+#pragma unroll
+      for (int i = 0; i < TN; i += 2) {
+        const int n = it.n0 + wn * C::WN + 16 * i + 8 * fq;
+        if (a.part) store8<float>(a.part, nullptr, ((int64_t)it.split * M + m) * N, n, N, acc[i][j], acc[i + 1][j]);
+        else store8(static_cast<OUT*>(a.y), static_cast<const OUT*>(a.bias), (int64_t)m * N, n, N, acc[i][j], acc[i + 1][j]);
+      }
+    }
+    id += kNumCUs;
+    if (id >= id_end) break;
+    it = next;
+    look_ahead();
   }
   wait_vmem();  // no LDS DMA may be in flight when the workgroup ends
-
-#pragma unroll
-  for (int j = 0; j < TM; ++j) {
-    const int m = m0 + wm * C::WM + 16 * j + fr;
-    if (m >= M) continue;
-#pragma unroll
-    for (int i = 0; i < TN; i += 2) {
-      const int n = n0 + wn * C::WN + 16 * i + 8 * fq;
-      if (a.part) store8<float>(a.part, nullptr, ((int64_t)split * M + m) * N, n, N, acc[i][j], acc[i + 1][j]);
-      else store8(static_cast<OUT*>(a.y), static_cast<const OUT*>(a.bias), (int64_t)m * N, n, N, acc[i][j], acc[i + 1][j]);
-    }
-  }
 }
 
 // --------------------------------------------------------------------- few rows --
@@ -496,8 +568,8 @@ __global__ __launch_bounds__(256) void fp8_reduce_kernel(const float* __restrict
 
 namespace {
 
-using Tile256 = Fp8Tile<256, 256, 2, 4, 2>;  // 8 waves of 128 x 64, 130 KB
-using Tile128 = Fp8Tile<128, 128, 2, 2, 2>;  // 4 waves of 64 x 64, 65 KB: two workgroups a CU
+using Tile256 = Fp8Tile<256, 256, 4>;  // 8 waves of 128 x 64, 130 KB
+using Tile128 = Fp8Tile<128, 128, 2>;  // 4 waves of 64 x 64, 65 KB: two workgroups a CU
 
 constexpr int64_t kRowsMaxM = 128;
 
@@ -562,10 +634,13 @@ hipError_t launch_tile(LinearFp8Args a, int splits, hipStream_t s) {
   if (attr != hipSuccess) return attr;
   const int64_t tiles_m = cdiv(a.M, C::BM);
   a.tiles_n = (int)cdiv(a.N, C::BN);
-  // tile-rows whose x (16 MB of it) stays cached while they sweep the columns, four at least
-  a.group_m = (int)std::max<int64_t>(1, std::min<int64_t>(tiles_m, std::max<int64_t>(4, ((int64_t)16 << 20) / ((int64_t)C::BM * a.K))));
-  hipLaunchKernelGGL((gemm_fp8_tile_kernel<C, OUT>), dim3((unsigned)(tiles_m * a.tiles_n * splits)), dim3(C::kThreads),
-                     C::kLdsBytes, s, a);
+  // tile-rows whose x (8 MB of it) stays cached while they sweep the columns, four at least
+  a.group_m = (int)std::max<int64_t>(1, std::min<int64_t>(tiles_m, std::max<int64_t>(4, ((int64_t)8 << 20) / ((int64_t)C::BM * a.K))));
+  a.splits = splits;
+  // (a chain's loads run two slices into the next item and look at the third: none is shorter)
+  a.chained = C::kChained && a.nkb - (splits - 1) * a.chunk >= 3;
+  const int64_t grid = chain_grid(tiles_m * a.tiles_n * splits, a.chained, true);
+  hipLaunchKernelGGL((gemm_fp8_tile_kernel<C, OUT>), dim3((unsigned)grid), dim3(C::kThreads), C::kLdsBytes, s, a);
   return hipGetLastError();
 }
 
