@@ -489,8 +489,8 @@ size_t opscale_linear_fp8_workspace_size(int64_t M, int64_t N, int64_t K, opscal
  * Scales and sums over the blocks are fp32.  bf16 results: the inner sums are those of
  * the fp8 matrix instructions, which cut each product to 2^-13 of the largest of its eight
  * (k = 8 i .. 8 i + 7); fp32 results: the products are whole and summed in fp32.
- * K a multiple of 16, up to 2^20; N * sizeof(dt) a multiple of 16; M, N below 2^30 and
- * M * N up to 2^40; x, W, y, bias and workspace 16-byte aligned.
+ * K a multiple of 16, up to 2^20; N * sizeof(dt) a multiple of 16, N up to 2^24; M below
+ * 2^30 and M * N up to 2^40; x, W, y, bias and workspace 16-byte aligned.
  * workspace: as opscale_linear's (NULL: no K split; otherwise at least
  * opscale_linear_fp8_workspace_size(M, N, K, dt) bytes, else OPSCALE_ERR_WORKSPACE).
  * Splits are summed in a fixed order: deterministic.

@@ -691,7 +691,7 @@ opscale_status check_linear_fp8(const void* x, const float* xs, const void* W, c
   const char* who = "linear_fp8";
   if (!dtype_ok(dt)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, (int)dt);
   const int s = esize(dt);
-  if (M < 0 || N <= 0 || K <= 0 || M >= (1 << 30) || N >= (1 << 30) || K > (1 << 20) || M > ((int64_t)1 << 40) / N)
+  if (M < 0 || N <= 0 || K <= 0 || M >= (1 << 30) || N > (1 << 24) || K > (1 << 20) || M > ((int64_t)1 << 40) / N)
     return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes M=%lld N=%lld K=%lld", who, (long long)M, (long long)N, (long long)K);
   if (K % 16 || N * s % 16)
     return fail(OPSCALE_ERR_INVALID_ARG, "%s: K and N times sizeof(dt) must be multiples of 16 (K=%lld N=%lld)", who,

@@ -96,21 +96,24 @@ __device__ __forceinline__ void store4(OUT* y, const OUT* bias, int64_t at, int 
   }
 }
 
-// Eight consecutive columns from n on of the row of y that begins at `row`; those past N (a multiple
-// of four) are left out.
+// Eight consecutive columns from n on, at byte `at` of a descriptor; those past N (a multiple of
+// eight in bf16, of four in fp32) go nowhere.
 template <class OUT>
-__device__ __forceinline__ void store8(OUT* y, const OUT* bias, int64_t row, int n, int N, f32x4 lo, f32x4 hi) {
-  if (sizeof(OUT) == 2 && n + 8 <= N) {
-    if (bias) {
+__device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t y, const OUT* bias, uint32_t at, int n, int N, f32x4 lo,
+                                       f32x4 hi) {
+  if constexpr (sizeof(OUT) == 2) {
+    if (bias && n < N) {
       const u32x4 b = *reinterpret_cast<const u32x4*>(bias + n);
       lo[0] += bf_lo(b[0]), lo[1] += bf_hi(b[0]), lo[2] += bf_lo(b[1]), lo[3] += bf_hi(b[1]);
       hi[0] += bf_lo(b[2]), hi[1] += bf_hi(b[2]), hi[2] += bf_lo(b[3]), hi[3] += bf_hi(b[3]);
     }
-    *reinterpret_cast<u32x4*>(y + row + n) =
-        u32x4{pack_bf2(lo[0], lo[1]), pack_bf2(lo[2], lo[3]), pack_bf2(hi[0], hi[1]), pack_bf2(hi[2], hi[3])};
-  } else if (sizeof(OUT) == 4) {
-    if (n < N) store4(y, bias, row + n, n, lo);
-    if (n + 4 < N) store4(y, bias, row + n + 4, n + 4, hi);
+    const u32x4 v{pack_bf2(lo[0], lo[1]), pack_bf2(lo[2], lo[3]), pack_bf2(hi[0], hi[1]), pack_bf2(hi[2], hi[3])};
+    __builtin_amdgcn_raw_buffer_store_b128(v, y, n < N ? at : kOobOffset, 0, 0);
+  } else {
+    if (bias && n < N) lo += *reinterpret_cast<const f32x4*>(bias + n);
+    if (bias && n + 4 < N) hi += *reinterpret_cast<const f32x4*>(bias + n + 4);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), y, n < N ? at : kOobOffset, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), y, n + 4 < N ? at + 16 : kOobOffset, 0, 0);
   }
 }
 
@@ -275,9 +278,15 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   auto read_w = [&](int i) { w[i] = read_frag(st + w0 + (32 * (i >> 1) + 4 * (i & 1)) * kSlice, woff); };
   auto read_wscale = [&] { return *reinterpret_cast<const OPS_LDS float*>(smem + ws0 + (slices & 3) * C::kScales); };
   auto other = [&] { return st == smem ? smem + C::kStageBytes : smem; };
-  // The next slice has arrived, in every wave (W's slice after it need not have).
+  // The next slice has arrived, in every wave.  Behind it in the queue are W's loads of the slice
+  // after it, and in an item's first slice the stores of the one before.
+  int behind = 0;  // 0: no stores; 1: of the result; 2: of partial sums
+  constexpr int kStores = TM * TN / 2;
   auto ready = [&] {
-    wait_vmcnt_le<C::kLoads + 1>();
+    if (behind == 0) wait_vmcnt_le<C::kLoads + 1>();
+    else if (behind == 1) wait_vmcnt_le<C::kLoads + 1 + kStores * (EXACT ? 2 : 1)>();
+    else wait_vmcnt_le<C::kLoads + 1 + kStores * 2>();
+    behind = 0;
     barrier_keep_loads();
   };
   // A product is scaled and added a group of products after its own: p holds a group, of TN
@@ -393,19 +402,28 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
       advance();
     }
 
-    // The item's results; the next one's first slices are on their way, its first fragments here.
+    // The item's results; the next one's first slices are on their way, its first fragments here.  Every
+    // lane stores as often, out of range past the edges: the waits behind count on it.
+    auto store = [&](auto out, const auto* bias, auto* y, int64_t row0) {
+      using T = decltype(out);
+      const int n_end = it.n0 + wn * C::WN;
 #pragma unroll
-    for (int j = 0; j < TM; ++j) {
-      const int m = it.m0 + wm * C::WM + 16 * j + fr;
-      pin();
-      if (m >= M) continue;
+      for (int j = 0; j < TM; ++j) {
+        pin();
+        const int m = it.m0 + wm * C::WM + 16 * j;
+        // (16 rows of up to 2^24 columns: below 2^31 bytes)
+        const __amdgpu_buffer_rsrc_t r =
+            make_rsrc(y + (row0 + m) * N, m < M ? (uint32_t)min(16, M - m) * (uint32_t)N * (uint32_t)sizeof(T) : 0u);
 #pragma unroll
-      for (int i = 0; i < TN; i += 2) {
-        const int n = it.n0 + wn * C::WN + 16 * i + 8 * fq;
-        if (a.part) store8<float>(a.part, nullptr, ((int64_t)it.split * M + m) * N, n, N, acc[i][j], acc[i + 1][j]);
-        else store8(static_cast<OUT*>(a.y), static_cast<const OUT*>(a.bias), (int64_t)m * N, n, N, acc[i][j], acc[i + 1][j]);
+        for (int i = 0; i < TN; i += 2) {
+          const int n = n_end + 16 * i + 8 * fq;
+          store8<T>(r, bias, (uint32_t)(fr * N + n) * (uint32_t)sizeof(T), n, N, acc[i][j], acc[i + 1][j]);
+        }
       }
-    }
+    };
+    if (a.part) store(0.f, (const float*)nullptr, a.part, (int64_t)it.split * M);
+    else store(OUT{}, static_cast<const OUT*>(a.bias), static_cast<OUT*>(a.y), 0);
+    behind = a.part ? 2 : 1;
     id += kNumCUs;
     if (id >= id_end) break;
     it = next;

@@ -50,8 +50,8 @@ def test_linear_fp8(lib):
     good = dict(x=G, xs=2 * G, W=3 * G, ws=4 * G, bias=5 * G, y=6 * G, M=256, N=512, K=4096, dt=1, work=7 * G, wb=1 << 30)
     call = caller(lib, "linear_fp8", good)
     refused(lib, "linear_fp8", call, 1, (
-        dict(dt=-1), dict(M=-1), dict(M=1 << 30), dict(N=0), dict(N=1 << 30), dict(K=0), dict(K=4104),
-        dict(K=(1 << 20) + 16), dict(N=508), dict(dt=0, N=510), dict(M=1 << 25, N=1 << 20), dict(x=None), dict(xs=None),
+        dict(dt=-1), dict(M=-1), dict(M=1 << 30), dict(N=0), dict(N=(1 << 24) + 8), dict(K=0), dict(K=4104),
+        dict(K=(1 << 20) + 16), dict(N=508), dict(dt=0, N=510), dict(M=1 << 25, N=1 << 16), dict(x=None), dict(xs=None),
         dict(W=None), dict(ws=None), dict(y=None), dict(x=G + 8), dict(W=3 * G + 1), dict(y=6 * G + 8),
         dict(bias=5 * G + 2), dict(xs=2 * G + 1), dict(ws=4 * G + 2), dict(y=G), dict(y=2 * G + 64), dict(y=3 * G),
         dict(y=4 * G), dict(y=5 * G)))
