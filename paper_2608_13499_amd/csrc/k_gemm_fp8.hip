@@ -563,6 +563,78 @@ __global__ __launch_bounds__(64 * NW, 1) void gemm_fp8_rows_kernel(const LinearF
   }
 }
 
+// ------------------------------------------------------- 16 rows, no second launch --
+// 16 columns and 16 rows (blockIdx.y) a workgroup, whose waves take every kWaves-th slice
+// each, kBatch of them on their way while kBatch are used; their sums meet in LDS, in
+// wave order.  Every 16 columns read x's rows and every 16 rows W's, so this is for few
+// of either, where the chain (launch, loads, one sum) is the time.
+namespace {
+constexpr int kFewWaves = 8, kBatch = 4;
+}
+
+template <class OUT>
+__global__ __launch_bounds__(64 * kFewWaves, 1) void gemm_fp8_few_kernel(const LinearFp8Args a) {
+  constexpr bool EXACT = sizeof(OUT) == 4;
+  __shared__ f32x4 sums[kFewWaves - 1][64];
+  const int M = a.M, N = a.N, K = a.K, nkb = a.nkb;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int fr = lane & 15, fq = lane >> 4;
+  const int n0 = (int)xcd_remap(blockIdx.x, gridDim.x) * 16, m0 = blockIdx.y * 16;
+  const int xrows = min(16, M - m0), wrows = min(16, N - n0);
+  // rows past the ends read as zeros (range check), and so do slices past the last one
+  const __amdgpu_buffer_rsrc_t xr = make_rsrc(a.x + (int64_t)m0 * K, (uint32_t)(xrows * K));
+  const __amdgpu_buffer_rsrc_t wr = make_rsrc(a.w + (int64_t)n0 * K, (uint32_t)(wrows * K));
+  const float* wsp = a.ws + (int64_t)(n0 / kFp8Block) * nkb;
+  const float* xsp = a.xs + m0 + min(fr, xrows - 1);
+  const uint32_t row = (uint32_t)(fr * K + 16 * fq);
+
+  Frag w[2][kBatch], x[2][kBatch];
+  float scale[2][kBatch];
+  auto load = [&](auto b_c, int first) {
+    constexpr int b = decltype(b_c)::value;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int kb = first + u * kFewWaves, k = kb * kSlice + 16 * fq;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const uint32_t at = k + 64 * h < K ? row + kb * kSlice + 64 * h : kOobOffset;
+        w[b][u].c[h] = buffer_load16(wr, at);
+        x[b][u].c[h] = buffer_load16(xr, at);
+      }
+      const int c = min(kb, nkb - 1);
+      scale[b][u] = xsp[(int64_t)c * M] * wsp[c];
+    }
+  };
+  f32x4 acc{};
+  auto use = [&](auto b_c, int first) {
+    constexpr int b = decltype(b_c)::value;
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const f32x4 p = block_product<EXACT>(w[b][u], x[b][u]);
+      // (past the last slice the products are zeros, the scale is not: 0 * NaN)
+      const float f = first + u * kFewWaves < nkb ? scale[b][u] : 0.f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) acc[r] = fmaf(f, p[r], acc[r]);
+    }
+  };
+  constexpr int STEP = kBatch * kFewWaves;
+  load(Int<0>{}, wave);
+  for (int s = wave; s < nkb; s += 2 * STEP) {
+    if (s + STEP < nkb) load(Int<1>{}, s + STEP);
+    use(Int<0>{}, s);
+    if (s + STEP >= nkb) break;
+    if (s + 2 * STEP < nkb) load(Int<0>{}, s + 2 * STEP);
+    use(Int<1>{}, s + STEP);
+  }
+  if (wave > 0) sums[wave - 1][lane] = acc;
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int i = 0; i < kFewWaves - 1; ++i) acc += sums[i][lane];
+  const int n = n0 + 4 * fq, m = m0 + fr;
+  if (m < M && n < N) store4(static_cast<OUT*>(a.y), static_cast<const OUT*>(a.bias), (int64_t)m * N + n, n, acc);
+}
+
 // y = the splits' partials, in order, + bias; four columns a thread, kBatch splits' loads at a time.
 template <class OUT>
 __global__ __launch_bounds__(256) void fp8_reduce_kernel(const float* __restrict__ part, int splits,
@@ -611,6 +683,13 @@ RowsShape rows_shape(int64_t N, int64_t nkb, bool split_ok) {
   return best;
 }
 
+// Few outputs: as long as the 16 x 16 blocks are about one and a half rounds of the CUs, one
+// launch of them is done before the other kernels' chains are (us, this one / the others': 1 x
+// 6144 x 4096, 384 blocks, 8.3 / 10.0; 8 x 4096 x 4096 5.7 / 9.0; 1 x 4096 x 14336 13.6 / 17.1; 128 x 256
+// x 688 3.0 / 9.5; 32 x 4096 x 4096, 512 blocks, 10.4 / 10.4; 4 x 10240 x 8192, 640 blocks, 22.6 / 21.2; 48 x
+// 4096 x 4096 14.8 / 11.7).
+bool few(int64_t M, int64_t N) { return cdiv(M, 16) * cdiv(N, 16) <= kNumCUs * 3 / 2; }
+
 // Tiles: the smaller ones where the larger leave more of the chip idle, and K split where
 // even those are fewer than the CUs.
 LinearFp8Plan tile_plan(int64_t M, int64_t N, int64_t nkb, bool bf16, bool split_ok) {
@@ -632,7 +711,10 @@ LinearFp8Plan tile_plan(int64_t M, int64_t N, int64_t nkb, bool bf16, bool split
 LinearFp8Plan plan_linear_fp8(int64_t M, int64_t N, int64_t K, bool bf16, bool split_ok) {
   const int64_t nkb = cdiv(K, kFp8Block);
   LinearFp8Plan p{};
-  if (M <= kRowsMaxM) {
+  if (few(M, N)) {
+    p.path = LinearFp8Plan::kFew;
+    p.splits = 1, p.chunk = (int)nkb;
+  } else if (M <= kRowsMaxM) {
     const RowsShape r = rows_shape(N, nkb, split_ok);
     p.path = LinearFp8Plan::kRows;
     p.waves = r.waves, p.splits = r.splits, p.chunk = r.chunk;
@@ -687,6 +769,11 @@ hipError_t launch_rows(const LinearFp8Args& a, int waves, int splits, hipStream_
 template <class OUT>
 hipError_t launch_fp8(const LinearFp8Plan& p, const LinearFp8Args& a, hipStream_t s) {
   hipError_t e;
+  if (p.path == LinearFp8Plan::kFew) {
+    hipLaunchKernelGGL((gemm_fp8_few_kernel<OUT>), dim3((unsigned)cdiv(a.N, 16), (unsigned)cdiv(a.M, 16)),
+                       dim3(64 * kFewWaves), 0, s, a);
+    return hipGetLastError();
+  }
   if (p.path == LinearFp8Plan::kRows) {
     if (a.M <= 16) e = launch_rows<1, OUT>(a, p.waves, p.splits, s);
     else if (a.M <= 32) e = launch_rows<2, OUT>(a, p.waves, p.splits, s);

@@ -147,10 +147,13 @@ def check_linear(ops, dtype, M, N, K, bias=False, seed=7, spread=0, workspace=No
     return y
 
 
-# few rows (each count of row blocks, K of one short block to many), tiles of 128 and 256, edges in M, N and K
-SHAPES = [(1, 8, 16), (1, 136, 128), (2, 512, 4096), (16, 96, 144), (17, 256, 688), (33, 264, 1040), (64, 128, 2048),
-          (65, 640, 272), (128, 256, 688), (127, 72, 1152), (129, 128, 128), (130, 136, 400), (200, 520, 1040),
-          (256, 256, 256), (300, 392, 2064), (513, 264, 144)]
+# Few outputs; few rows (each count of row blocks, K split and not); tiles (K split and not, edges in M
+# and N); K of one short block to many.
+SHAPES = [(1, 8, 16), (1, 136, 128), (2, 512, 4096), (16, 96, 144), (33, 264, 1040), (65, 640, 272), (127, 72, 1152),
+          (128, 256, 688), (300, 200, 4112),
+          (2, 6160, 400), (16, 6152, 2064), (17, 3208, 144), (33, 2072, 1040), (48, 2048, 2576), (65, 1240, 272),
+          (128, 792, 688), (127, 776, 2064),
+          (129, 704, 128), (130, 712, 400), (200, 520, 1040), (256, 512, 256), (300, 392, 2064), (513, 264, 144)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -160,7 +163,7 @@ def test_linear(ops, dtype, M, N, K):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("M,N,K", [(5, 200, 656), (40, 128, 4096), (140, 136, 2064), (258, 264, 400)])
+@pytest.mark.parametrize("M,N,K", [(5, 200, 656), (40, 2056, 656), (40, 128, 4096), (140, 712, 1040), (258, 392, 400)])
 def test_linear_bias_and_spread(ops, dtype, M, N, K):
     check_linear(ops, dtype, M, N, K, bias=True)
     check_linear(ops, dtype, M, N, K, spread=1)
@@ -204,8 +207,8 @@ def test_special_values(ops, dtype):
     """A NaN element or scale, an infinite scale: in their row or columns of a block, nowhere else."""
     import torch
     say(f"linear_fp8 {dtype}: NaN and infinity")
-    for M in (3, 150):
-        N, K = 264, 300 + 4
+    for M, N in ((3, 264), (40, 2056), (150, 712)):
+        K = 304
         xc, xs, wc, ws = operands(M, N, K, 13)
         want, off = reference(xc, xs, wc, ws, None, dtype)
         xc[1, 290], wc[200, 5] = 0x7f, 0xff
@@ -222,6 +225,7 @@ def test_special_values(ops, dtype):
         y = f64(ops.opscale_linear_fp8(e4(xc), cuda(torch.from_numpy(xs)), e4(wc), cuda(torch.from_numpy(ws)),
                                        dtype=torch_dtype(dtype)).cpu())
         assert not np.isfinite(y[:, 128:256]).any() and np.isfinite(np.delete(y, 2, 0)[:, :128]).all()
+        assert np.isfinite(np.delete(y, 2, 0)[:, 256:]).all()
 
 
 def test_unit_weights(ops):
@@ -231,8 +235,8 @@ def test_unit_weights(ops):
     K = 384
     w = torch.eye(K, device="cuda").to(torch.float8_e4m3fn)
     ws = torch.full((3, 3), 2.0, device="cuda")
-    x = cuda(gen(1, "x", (140, K), "f32"))
-    for m in (3, 140):
+    x = cuda(gen(1, "x", (270, K), "f32"))
+    for m in (3, 270):
         q, s = ops.opscale_quantize_fp8(x[:m])
         y = ops.opscale_linear_fp8(q, s, w, ws, dtype=torch.float32)
         torch.cuda.synchronize()
@@ -247,14 +251,14 @@ def test_empty_and_graph(ops):
     ws = torch.ones(2, 4, device="cuda")
     q, s = ops.opscale_quantize_fp8(torch.zeros(0, 512, device="cuda"))
     assert q.shape == (0, 512) and ops.opscale_linear_fp8(q, s, w, ws).shape == (0, 256)
-    for M in (5, 200):
-        xc, xs, wc, wsc = operands(M, 256, 2048, 17)
+    for M, N in ((5, 256), (48, 2048), (200, 512)):
+        xc, xs, wc, wsc = operands(M, N, 2048, 17)
         x = cuda(gen(17, "x", (M, 2048), "bf16"))
         w = torch.from_numpy(wc).cuda().view(torch.float8_e4m3fn)
         ws = cuda(torch.from_numpy(wsc))
-        ws_mem = torch.empty(ops.opscale_linear_fp8_workspace_size(M, 256, 2048), dtype=torch.uint8, device="cuda")
+        ws_mem = torch.empty(ops.opscale_linear_fp8_workspace_size(M, N, 2048), dtype=torch.uint8, device="cuda")
         q, s = ops.opscale_quantize_fp8(x)
-        y = torch.empty(M, 256, dtype=torch.bfloat16, device="cuda")
+        y = torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
 
         def chain():
             ops.opscale_quantize_fp8(x, q, s)

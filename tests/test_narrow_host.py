@@ -57,7 +57,7 @@ def test_linear_fp8(lib):
         dict(y=4 * G), dict(y=5 * G)))
     # the workspace, where K is split
     need = lib.opscale_linear_fp8_workspace_size(256, 512, 4096, 1)
-    assert need >= 2 * 256 * 512 * 4
+    assert need >= 2 * 256 * 512 * 4 and need % (256 * 512 * 4) == 0
     assert call(wb=need - 1) == 3 and "linear_fp8" in _err(lib)
     refused(lib, "linear_fp8", call, 1, (dict(work=7 * G + 4), dict(work=6 * G + 16), dict(work=G), dict(work=2 * G),
                                          dict(work=3 * G), dict(work=4 * G), dict(work=5 * G)))
