@@ -278,6 +278,25 @@ def test_decode_long(ops):
     check_decode(ops, "f32", [5000], 4, 1, 128, 16, dict(softcap=30.0))
 
 
+@pytest.mark.parametrize("Hq,Hkv,D", [(4, 1, 128), (17, 1, 64), (6, 2, 128), (9, 3, 128), (8, 4, 64), (8, 8, 128), (24, 24, 128)])
+@pytest.mark.parametrize("name", DECODE_RULES)
+def test_decode_split(ops, name, Hq, Hkv, D):
+    """Short sequences whose greatest length as told has them split over workgroups, and untold, whole."""
+    ctx = [900, 0, 1, 40, 257]
+    for max_ctx in (8192, 1024):
+        check_decode(ops, "bf16", ctx, Hq, Hkv, D, 16, decode_rules(name, ctx, Hq), max_ctx=max_ctx, holes=True)
+        check_decode(ops, "f32", ctx, Hq, Hkv, D, 32, decode_rules(name, ctx, Hq), max_ctx=max_ctx)
+
+
+@pytest.mark.parametrize("Hkv", [1, 2, 8])
+def test_decode_pages_ahead(ops, Hkv):
+    """First tiles at every place of a window of 64 page ids, and prefixes that end in every one."""
+    for w in (3960, 3991, 4000, 4070, 4100):
+        ctx = [8000, 5000, 1100 + w // 8]
+        check_decode(ops, "bf16", ctx, 2 * Hkv, Hkv, 64, 16, dict(window=w, prefix_lens=np.array([w % 1500, 1030, 7])))
+    check_decode(ops, "bf16", [20000], Hkv, Hkv, 64, 16, {})
+
+
 @pytest.mark.parametrize("cap", [1e-3, 0.5, 50.0, 1e6])
 def test_decode_caps(ops, cap):
     for std in (0.3, 4.0, 20.0):
