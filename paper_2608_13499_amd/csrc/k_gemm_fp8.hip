@@ -139,13 +139,13 @@ struct Fp8Tile {
   static constexpr int BM = BM_, BN = BN_, WGM = 2, WGN = WGN_;
   static constexpr int kWaves = WGM * WGN, kThreads = 64 * kWaves;
   static constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16;
-  static constexpr int kLoads = BN / 8 / kWaves;  // of a wave: of W's rows, and of x's
+  static constexpr int kLoadsX = BM / 8 / kWaves, kLoadsW = BN / 8 / kWaves;  // of a wave
   static constexpr int kScales = BM * 4 + 256;  // x's, then W's
   static constexpr int kStageBytes = (BM + BN) * kSlice, kLdsBytes = 2 * kStageBytes + 4 * kScales;
-  static constexpr bool kChained = BM > 128;  // one workgroup a CU
-  static_assert(BM == BN && BN % (8 * kWaves) == 0 && BM / 64 < kWaves, "whole loads");
+  static constexpr bool kChained = kLdsBytes > 80 * 1024;  // one workgroup a CU
+  static_assert(BM <= BN && BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BM / 64 < kWaves, "whole loads");
   static_assert(kFp8Block % WN == 0 && BN % kFp8Block == 0, "a wave's columns lie in one block of W's scales");
-  static_assert((TM == 4 || TM == 8) && TN == 4 && kLoads == 4, "the order of the slice loop");
+  static_assert((TM == 4 || TM == 8) && TN == 4 && kLoadsX <= 4 && kLoadsW == 4, "the order of the slice loop");
   // Registers of x's fragments: where row j of them is held.  Each differs from the one before
   // it, the last two from the third last and from 0, where the next slice's first goes.
   static constexpr int kSlots = TM == 4 ? 4 : 3;
@@ -176,9 +176,9 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   // its 32 rows, so that a lane's two sums are eight consecutive columns of y.
   const int c16 = ((lane & 7) ^ (lane >> 3)) * 16;
   const int wc16 = ((lane & 7) ^ ((lane >> 3 & 3) | (wave & 1) << 2)) * 16;
-  uint32_t from[C::kLoads];  // of x's rows, and of W's
+  uint32_t from[C::kLoadsW];  // of x's rows, and of W's
 #pragma unroll
-  for (int g = 0; g < C::kLoads; ++g) from[g] = (uint32_t)(((g * C::kWaves + wave) * 8 + (lane >> 3)) * K);
+  for (int g = 0; g < C::kLoadsW; ++g) from[g] = (uint32_t)(((g * C::kWaves + wave) * 8 + (lane >> 3)) * K);
   // The scales: each of the first BM / 64 waves loads those of 64 rows of x, the others those of W's
   // BN / 128 blocks.
   const bool x_scales = wave < BM / 64;
@@ -283,9 +283,9 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   int behind = 0;  // 0: no stores; 1: of the result; 2: of partial sums
   constexpr int kStores = TM * TN / 2;
   auto ready = [&] {
-    if (behind == 0) wait_vmcnt_le<C::kLoads + 1>();
-    else if (behind == 1) wait_vmcnt_le<C::kLoads + 1 + kStores * (EXACT ? 2 : 1)>();
-    else wait_vmcnt_le<C::kLoads + 1 + kStores * 2>();
+    if (behind == 0) wait_vmcnt_le<C::kLoadsW + 1>();
+    else if (behind == 1) wait_vmcnt_le<C::kLoadsW + 1 + kStores * (EXACT ? 2 : 1)>();
+    else wait_vmcnt_le<C::kLoadsW + 1 + kStores * 2>();
     behind = 0;
     barrier_keep_loads();
   };
@@ -311,15 +311,15 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   for (int slice = 0; slice < 2; ++slice) {
     if (slice == 0)
 #pragma unroll
-      for (int g = 0; g < C::kLoads; ++g) load_x(g, smem);
+      for (int g = 0; g < C::kLoadsX; ++g) load_x(g, smem);
     load_scales(slice);
 #pragma unroll
-    for (int g = 0; g < C::kLoads; ++g) load_w(g, smem + slice * C::kStageBytes);
+    for (int g = 0; g < C::kLoadsW; ++g) load_w(g, smem + slice * C::kStageBytes);
     if (slice == 0) advance();
   }
   ready();
 #pragma unroll
-  for (int g = 0; g < C::kLoads; ++g) load_x(g, other());
+  for (int g = 0; g < C::kLoadsX; ++g) load_x(g, other());
   advance();
   read_x(0);
   wscale = read_wscale();
@@ -350,8 +350,8 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
             constexpr int kMfmas = TN * (TM - 3);
             const int n = (j - 1) * TN + i;
 #pragma unroll
-            for (int g = 0; g < C::kLoads + 1; ++g)
-              if (n == g * kMfmas / (C::kLoads + 1)) {
+            for (int g = 0; g < C::kLoadsW + 1; ++g)
+              if (n == g * kMfmas / (C::kLoadsW + 1)) {
                 if (g == 0) load_scales(slices + 2);
                 else load_w(g - 1, st);
               }
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
             wscale = read_wscale();
           }
           read_w(n);
-          load_x(n, left);
+          if (n < C::kLoadsX) load_x(n, left);
           pin();
         }
         if (h == 1)
@@ -659,6 +659,7 @@ __global__ __launch_bounds__(256) void fp8_reduce_kernel(const float* __restrict
 namespace {
 
 using Tile256 = Fp8Tile<256, 256, 4>;  // 8 waves of 128 x 64, 130 KB
+using Tile128x256 = Fp8Tile<128, 256, 4>;  // 8 waves of 64 x 64, 99 KB
 using Tile128 = Fp8Tile<128, 128, 2>;  // 4 waves of 64 x 64, 65 KB: two workgroups a CU
 
 constexpr int64_t kRowsMaxM = 128;
@@ -690,19 +691,42 @@ RowsShape rows_shape(int64_t N, int64_t nkb, bool split_ok) {
 // 4096 x 4096 14.8 / 11.7).
 bool few(int64_t M, int64_t N) { return cdiv(M, 16) * cdiv(N, 16) <= kNumCUs * 3 / 2; }
 
-// Tiles: the smaller ones where the larger leave more of the chip idle, and K split where
-// even those are fewer than the CUs.
+// Tiles: the shape, and the ranges of K where the tiles are fewer than the CUs, that are done
+// first by what each takes, in us: a slice of K over a round of the CUs, a launch's first loads
+// and last stores, and for ranges of K the sums' way through memory and the second launch.
+// (Measured / estimated, 256 x 256, 128 x 256 and 128 x 128: 1024 x 6144 x 4096 50 / 53, 37 / 37, 41 / 46;
+// 256 x 28672 x 4096 54, 46, 50; 2048 x 6144 x 4096 56 / 53, 73 / 70, 72 / 72; 1024 x 4096 x 4096 49, 34, 30 / 29;
+// 8871 x 6144 x 4096 215, 245, 275; 200 x 4096 x 4096 on 128 x 128 in one range 26 / 29, two 23 / 23.)
 LinearFp8Plan tile_plan(int64_t M, int64_t N, int64_t nkb, bool bf16, bool split_ok) {
+  struct Shape {
+    LinearFp8Plan::Path path;
+    int bm, bn;
+    double slice, half;  // a round, and one of 128 x 128 tiles that fills half the places (two a CU)
+    int places;
+  };
+  static constexpr Shape kShapes[] = {{LinearFp8Plan::kTile256, 256, 256, 1.55, 1.55, kNumCUs},
+                                      {LinearFp8Plan::kTile128x256, 128, 256, 1.05, 1.05, kNumCUs},
+                                      {LinearFp8Plan::kTile128, 128, 128, 1.35, 0.80, 2 * kNumCUs}};
+  constexpr double kEnds = 3.0, kSecond = 4.0, kSumBytes = 4e6;  // (bytes a us)
   LinearFp8Plan p{};
-  const int64_t big = cdiv(M, 256) * cdiv(N, 256), small = cdiv(M, 128) * cdiv(N, 128);
-  const double t_big = 2.2 * cdiv(big, kNumCUs), t_small = 0.8 * cdiv(small, kNumCUs);
-  // (fp32 results: the widened operands and the larger tile's sums are more than the registers)
-  p.path = bf16 && t_big <= t_small ? LinearFp8Plan::kTile256 : LinearFp8Plan::kTile128;
-  const int64_t tiles = p.path == LinearFp8Plan::kTile256 ? big : small;
-  int64_t splits = 1;
-  if (split_ok && tiles < kNumCUs) splits = std::max<int64_t>(1, std::min<int64_t>(2 * kNumCUs / tiles, nkb / 8));
-  p.chunk = (int)cdiv(nkb, splits);
-  p.splits = (int)cdiv(nkb, p.chunk);
+  double best = 0.0;
+  for (const Shape& s : kShapes) {
+    // (fp32 results: the widened operands and the larger tiles' sums are more than the registers, or
+    // leave them no second workgroup)
+    if (!bf16 && s.path != LinearFp8Plan::kTile128) continue;
+    const int64_t tiles = cdiv(M, s.bm) * cdiv(N, s.bn);
+    const int64_t most = split_ok && tiles < kNumCUs ? std::max<int64_t>(1, std::min<int64_t>(2 * kNumCUs / tiles, nkb / 8)) : 1;
+    for (int64_t splits = 1; splits <= most; ++splits) {
+      const int64_t chunk = cdiv(nkb, splits), items = tiles * cdiv(nkb, chunk);
+      const int64_t rounds = items / s.places, rest = items % s.places;
+      const double per = rounds * s.slice + (rest == 0 ? 0.0 : rest <= kNumCUs ? s.half : s.slice);
+      const double t = kEnds + chunk * per + (splits > 1 ? kSecond + 8.0 * splits * M * N / kSumBytes : 0.0);
+      if (best != 0.0 && t >= best) continue;
+      best = t;
+      p.path = s.path;
+      p.chunk = (int)chunk, p.splits = (int)cdiv(nkb, chunk);
+    }
+  }
   return p;
 }
 
@@ -779,9 +803,12 @@ hipError_t launch_fp8(const LinearFp8Plan& p, const LinearFp8Args& a, hipStream_
     else if (a.M <= 32) e = launch_rows<2, OUT>(a, p.waves, p.splits, s);
     else if (a.M <= 64) e = launch_rows<4, OUT>(a, p.waves, p.splits, s);
     else e = launch_rows<8, OUT>(a, p.waves, p.splits, s);
-  } else if (p.path == LinearFp8Plan::kTile256) {
-    if constexpr (sizeof(OUT) == 2) e = launch_tile<Tile256, OUT>(a, p.splits, s);
-    else e = hipErrorInvalidValue;  // (not planned)
+  } else if (p.path != LinearFp8Plan::kTile128) {
+    if constexpr (sizeof(OUT) == 2)
+      e = p.path == LinearFp8Plan::kTile256 ? launch_tile<Tile256, OUT>(a, p.splits, s)
+                                            : launch_tile<Tile128x256, OUT>(a, p.splits, s);
+    else
+      e = hipErrorInvalidValue;  // (not planned)
   } else {
     e = launch_tile<Tile128, OUT>(a, p.splits, s);
   }

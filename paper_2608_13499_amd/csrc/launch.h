@@ -143,7 +143,7 @@ hipError_t launch_attn_decode_fp4(const void* q, int64_t q_stride, const void* k
 // The linear of e4m3 operands (k_gemm_fp8.hip); the workspace query and the launch take
 // the same plan.  split_ok == false plans no K split, which needs no workspace.
 struct LinearFp8Plan {
-  enum Path { kRows = 0, kTile256 = 1, kTile128 = 2, kFew = 3 };
+  enum Path { kRows = 0, kTile256 = 1, kTile128x256 = 2, kTile128 = 3, kFew = 4 };
   int path;
   int waves;        // rows: waves of a workgroup
   int splits;       // K ranges (fp32 partials [splits, M, N] where more than one)
