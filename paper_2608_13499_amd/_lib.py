@@ -804,12 +804,16 @@ def opscale_quantize_fp8(x, q=None, scales=None, stream=None, timed: bool = Fals
     nkb = (K + 127) // 128
     if q is None:
         q = x.new_empty((M, K), dtype=_e4m3)
+        qp = q.data_ptr()
+    else:
+        qp = _cache("q", q, (M, K), _e4m3, dev)
     if scales is None:
         scales = x.new_empty((nkb, M), dtype=_f32)
+        sp = scales.data_ptr()
+    else:
+        sp = _cache("scales", scales, (nkb, M), _f32, dev)
     t = Timing() if timed else None
-    _check(lib.opscale_quantize_fp8(x.data_ptr(), xs, _cache("q", q, (M, K), _e4m3, dev),
-                                    _cache("scales", scales, (nkb, M), _f32, dev), M, K, dt, _stream(stream),
-                                    ctypes.byref(t) if t else None))
+    _check(lib.opscale_quantize_fp8(x.data_ptr(), xs, qp, sp, M, K, dt, _stream(stream), ctypes.byref(t) if t else None))
     return ((q, scales), t) if timed else (q, scales)
 
 
@@ -900,12 +904,14 @@ def opscale_kv_read_fp4(k_cache, v_cache, block_table, cu_seqlens, total_tokens:
             import torch
             dtype = torch.bfloat16
         k, v = k_cache.new_empty(shape, dtype=dtype), k_cache.new_empty(shape, dtype=dtype)
-    elif dtype is not None and dtype != k.dtype:
-        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"k is {k.dtype}, dtype {dtype}")
+        ks = Hkv * D
+    else:
+        if dtype is not None and dtype != k.dtype:
+            raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"k is {k.dtype}, dtype {dtype}")
+        ks = _rows("k", k, shape, k.dtype, dev)
+        if ks != _rows("v", v, shape, k.dtype, dev):
+            raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "k and v must share a row stride")
     dt = _dt(k)
-    ks, vs = _rows("k", k, shape, k.dtype, dev), _rows("v", v, shape, k.dtype, dev)
-    if ks != vs:
-        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "k and v must share a row stride")
     if block_table.dim() != 2:
         raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "block_table must be [B, max_blocks_per_seq]")
     B, cols = block_table.shape
