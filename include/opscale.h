@@ -469,7 +469,7 @@ opscale_status opscale_attn_decode_mod(const void* q, int64_t q_row_stride, cons
  *   q[m, k] = e4m3(x[m, k] 2^-e),  scales[k / 128, m] = 2^e.
  * x: [M, K], rows of x_row_stride elements; q: [M, K] bytes, dense; scales: fp32
  * [ceil(K / 128), M].  A block that holds an infinity or NaN has the scale NaN (its codes
- * then have no meaning).  K a multiple of 16, up to 2^20; x and q 16-byte aligned, x_row_stride a multiple
+ * then have no meaning).  K a multiple of 16, up to 2^20, ceil(M / 16) ceil(K / 512) < 2^24; x and q 16-byte aligned, x_row_stride a multiple
  * of 16 bytes; nothing overlaps.
  */
 opscale_status opscale_quantize_fp8(const void* x, int64_t x_row_stride, void* q, float* scales, int64_t M, int64_t K,
@@ -513,7 +513,7 @@ opscale_status opscale_linear_fp8(const void* x, const float* x_scales, const vo
  * opscale_reshape_and_cache to such a cache: the K and V rows of token t (k, v: [T, Hkv,
  * D], rows of kv_row_stride elements) go to slot slot_mapping[t], quantised.  A token
  * whose slot is outside [0, num_blocks * block_size) is skipped (padding).  num_blocks *
- * block_size < 2^31.  The caches overlap nothing else.  Tokens sharing a slot race.
+ * block_size < 2^31, T < 2^28.  The caches overlap nothing else.  Tokens sharing a slot race.
  */
 opscale_status opscale_kv_write_fp4(const void* k, const void* v, int64_t kv_row_stride, void* k_cache, void* v_cache,
                                     const int32_t* slot_mapping, int64_t T, int32_t Hkv, int32_t D, int32_t block_size,
@@ -525,7 +525,7 @@ opscale_status opscale_kv_write_fp4(const void* k, const void* v, int64_t kv_row
  * cu_seqlens: DEVICE int32 [B + 1], cu_seqlens[0] = 0, non-decreasing, cu_seqlens[B] <=
  * total_tokens (the rows past it are left as they were); first_keys: DEVICE int32 [B], or
  * NULL (0); block_table: DEVICE int32 [B, max_blocks_per_seq].
- * k, v: [total_tokens, Hkv, D], rows of kv_row_stride elements (both may be views into
+ * k, v: [total_tokens, Hkv, D], total_tokens < 2^28, rows of kv_row_stride elements (both may be views into
  * one tensor); they overlap nothing else.  A key below 0, past max_blocks_per_seq pages, or
  * whose page is outside [0, num_blocks) reads as zeros.  Values past bf16's or fp32's range
  * do not arise from opscale_kv_write_fp4.

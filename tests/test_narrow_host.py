@@ -42,7 +42,8 @@ def test_quantize_fp8(lib):
     refused(lib, "quantize_fp8", call, 1, (
         dict(dt=2), dict(M=-1), dict(M=1 << 31), dict(K=0), dict(K=4088), dict(K=(1 << 20) + 16), dict(xs=4080),
         dict(xs=4100), dict(x=None), dict(q=None), dict(s=None), dict(x=G + 8), dict(q=2 * G + 4), dict(s=3 * G + 2),
-        dict(q=G), dict(s=G + 256), dict(s=2 * G + 16), dict(M=(1 << 31) - 1, K=1 << 20, xs=1 << 20)))
+        dict(q=G), dict(s=G + 256), dict(s=2 * G + 16), dict(M=(1 << 31) - 1, K=1 << 20, xs=1 << 20),
+        dict(M=1 << 28, K=16, xs=16)))
     assert call(M=0) == 0 and call(M=0, x=None, q=None, s=None) == 0
 
 
@@ -80,7 +81,7 @@ def test_kv_write_fp4(lib):
     good = dict(k=G, v=G + 2048, kvs=6144, **CACHE, slots=5 * G, T=64, Hkv=8, D=128, bs=16, nb=512, dt=1)
     call = caller(lib, "kv_write_fp4", good)
     refused(lib, "kv_write_fp4", call, 1, (
-        dict(dt=5), dict(T=-1), dict(T=1 << 31), dict(Hkv=0), dict(Hkv=1 << 14), dict(D=0), dict(bs=8), dict(bs=48),
+        dict(dt=5), dict(T=-1), dict(T=1 << 28), dict(Hkv=0), dict(Hkv=1 << 14), dict(D=0), dict(bs=8), dict(bs=48),
         dict(bs=2048), dict(nb=0), dict(nb=1 << 27), dict(kvs=1016), dict(kvs=6148), dict(k=None), dict(v=None),
         dict(kc=None), dict(vc=None), dict(slots=None), dict(k=G + 2), dict(v=G + 4), dict(kc=3 * G + 8),
         dict(vc=4 * G + 1), dict(slots=5 * G + 2), dict(kc=G), dict(vc=G + 2048), dict(kc=4 * G), dict(vc=5 * G)))
@@ -93,7 +94,7 @@ def test_kv_read_fp4(lib):
                 nb=512, dt=1)
     call = caller(lib, "kv_read_fp4", good)
     refused(lib, "kv_read_fp4", call, 1, (
-        dict(dt=5), dict(B=-1), dict(T=-1), dict(T=1 << 31), dict(Hkv=-2), dict(bs=4), dict(bs=24), dict(mb=0), dict(nb=0),
+        dict(dt=5), dict(B=-1), dict(T=-1), dict(T=1 << 28), dict(Hkv=-2), dict(bs=4), dict(bs=24), dict(mb=0), dict(nb=0),
         dict(nb=(1 << 32) + 1), dict(kvs=1000), dict(kvs=2052), dict(kc=None), dict(vc=None), dict(tab=None),
         dict(cu=None), dict(k=None), dict(v=None), dict(k=G + 8), dict(v=G + 4), dict(tab=5 * G + 1), dict(cu=6 * G + 2),
         dict(first=7 * G + 3), dict(v=G), dict(v=G + 2032), dict(k=3 * G), dict(v=4 * G), dict(k=5 * G), dict(v=6 * G),
