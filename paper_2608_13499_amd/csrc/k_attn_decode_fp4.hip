@@ -117,12 +117,12 @@ __global__ __launch_bounds__(512, 2) void attn_decode_fp4_kernel(const Fp4Args a
   // V's keys: slot j of lane group grp is row v_row + 8 (j / 4) + j % 4 of run v_run.
   const int v_run = grp & 1, v_row = 4 * (grp >> 1);
   // DMA sources within a run of 16 rows.  K: chunk lane % CPR of row lane / CPR, swizzled.  V: row r
-  // of run u in place 4 (r % 4) + (r / 4) % 2 + 2 (u ^ r / 8), so that the four groups' reads of a
-  // key slot each lie in different banks.
+  // of run u in place 4 (r % 4) + (u ^ r / 8) + 2 ((r / 4) % 2), so that the reads of a key slot by
+  // groups 0 and 1, and by 2 and 3, lie side by side.
   constexpr int CPR = D / 32;  // 16-byte chunks of a row
   const int lr = lane / CPR, lc = lane % CPR;
   const uint32_t k_from = (uint32_t)(lr * P::kRow + (D == 128 ? lc ^ k_swz(lr) : lc) * 16);
-  const uint32_t v_from = (uint32_t)(((lr >> 2 & 3) + 4 * (lr & 1) + 8 * (lr >> 1 & 1)) * P::kRow + lc * 16);
+  const uint32_t v_from = (uint32_t)(((lr >> 2 & 3) + 4 * (lr >> 1 & 1) + 8 * (lr & 1)) * P::kRow + lc * 16);
   const uint32_t v_from1 = v_from ^ (8 * P::kRow);  // (run 1)
   // Scale bytes: 16 lanes for each of (run 0: K, V; run 1: K, V), dword col % 4 of group col / 4.
   const int s_group = min(col >> 2, P::kGroups - 1);
@@ -132,8 +132,8 @@ __global__ __launch_bounds__(512, 2) void attn_decode_fp4_kernel(const Fp4Args a
   const int ks_at = R::kScales + ((grp * KD / kFp4Group) * 16 + col);
   const int vs_at = R::kScales + 128 * v_run + 64 + ((col * DT / kFp4Group) * 16 + v_row);
   const int k_at = D == 128 ? col * P::kRow + ((grp ^ k_swz(col)) << 4) : col * P::kRow + grp * 8;
-  const int v_at = R::kV + v_run * R::kRun + ((grp >> 1) + 2 * v_run) * P::kRow + col * (DT / 2);
-  const int v_at1 = R::kV + v_run * R::kRun + ((grp >> 1) + 2 * (v_run ^ 1)) * P::kRow + col * (DT / 2);
+  const int v_at = R::kV + v_run * R::kRun + (2 * (grp >> 1) + v_run) * P::kRow + col * (DT / 2);
+  const int v_at1 = R::kV + v_run * R::kRun + (2 * (grp >> 1) + (v_run ^ 1)) * P::kRow + col * (DT / 2);
 
   const bool plain = !(a.mods.softcap > 0.f) && !a.mods.slopes;
   float slope2 = 0.f;  // of head `col`
