@@ -30,7 +30,10 @@
 namespace opscale {
 
 namespace {
-constexpr int kRing = 4;  // tiles in a wave's ring
+// Tiles in a wave's ring: the one in use and the next.  More of them on their way cost (us, two /
+// three / four: 256 sequences of 128 to 8192 keys, 32 + 8 heads of 128, 205 / 211 / 219; one of 700 keys
+// 7.8 / - / 8.9, whose first loads they hold up).
+constexpr int kRing = 2;
 // Places of P in the sparse operand, two bits each: 0 and 2 of every four, or 1 and 3.
 constexpr int kEven = 0x8888, kOdd = 0xDDDD;
 using bf16x2 = __bf16 __attribute__((ext_vector_type(2)));
@@ -573,11 +576,17 @@ hipError_t launch_attn_decode_fp4(const void* q, int64_t q_stride, const void* k
   const AttnMods mods = make_attn_mods(m, scale);
   const int G = Hq / Hkv, blocks = (G + 15) / 16;
   const bool direct = whole_sequences(B, Hkv, blocks, max_context_len, mods.window, mods.prefix);
-  const int HB = direct ? 1 : decode_heads_per_workgroup(Hkv), groups = Hkv / HB * blocks;
-  // (a workgroup's rings leave no room for a second one on its CU: 4 sequences of a 4096-key
-  // window and a prefix of 100, 4 KV heads, 512 workgroups 22.0 us, 256 15.7)
-  const int nwg = direct ? B : std::min(mod_workgroups(B, max_context_len, mods.window, mods.prefix, groups, kWaves / HB),
-                                        std::max(1, kMaxWorkgroups / groups));
+  int HB = direct ? 1 : decode_heads_per_workgroup(Hkv), groups, nwg;
+  for (;; HB /= 2) {
+    groups = Hkv / HB * blocks;
+    // (one workgroup a CU, or the first of them would be done before the last begin: 4 sequences of a
+    // 4096-key window and a prefix of 100, 4 KV heads, 512 workgroups 22.0 us, 256 15.7)
+    nwg = direct ? B : std::min(mod_workgroups(B, max_context_len, mods.window, mods.prefix, groups, kWaves / HB),
+                                std::max(1, kMaxWorkgroups / groups));
+    // few sequences, which would leave CUs idle: fewer heads a workgroup (one of 30000 keys, 8 KV heads,
+    // eight a workgroup 27.2 us, two 15.9; 120000 78 / 33; two of 30000 28.2 / 21.4)
+    if (HB == 1 || nwg >= kMaxWorkgroups / groups) break;
+  }
   const DecodeWs w = decode_ws(ws, B, Hq, D, nwg);
   Fp4Args a{};
   a.o = o, a.direct = direct;
