@@ -36,7 +36,8 @@ __device__ __forceinline__ uint32_t to_e2m1(const float (&x)[8], float scale) {
 
 // A workgroup takes 16 rows (four a wave, sixteen lanes each, so that the scales of a
 // block of K, which lie side by side for the rows, are written 64 bytes at a time)
-// and BLOCKS blocks of K.
+// and BLOCKS blocks of K.  8871 x 14336 in bf16, 385 MB: 63 us, 6.1 TB/s (70 with x left in
+// the caches, 64 with q's stores past them too: what comes next reads q); 1 x 4096 3.3 us, a launch.
 template <bool BF16, int BLOCKS>
 __global__ __launch_bounds__(kThreads) void quantize_fp8_kernel(const void* __restrict__ x, int64_t x_stride,
                                                                 uint8_t* __restrict__ q, float* __restrict__ scales,
@@ -50,7 +51,7 @@ __global__ __launch_bounds__(kThreads) void quantize_fp8_kernel(const void* __re
     const int64_t k = (int64_t)(kb0 + i) * kFp8Block + lane * 8;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-    if (row && k < K) load8<BF16>(x, m * x_stride + k, v[i]);
+    if (row && k < K) load8<BF16, true>(x, m * x_stride + k, v[i]);
   }
 #pragma unroll
   for (int i = 0; i < BLOCKS; ++i) {
@@ -65,7 +66,8 @@ __global__ __launch_bounds__(kThreads) void quantize_fp8_kernel(const void* __re
 
 // A workgroup takes a run of tokens (16 for heads of 128) and one head of K or V: a
 // prompt's tokens lie in consecutive slots, and their codes and scale bytes then leave
-// one compute die's L2 in whole lines.
+// one compute die's L2 in whole lines.  4448 tokens of 8 heads of 128 in consecutive slots, 23 MB:
+// 7.1 us; 256 tokens of one slot a page 3.0.
 template <bool BF16, int D>
 __global__ __launch_bounds__(kThreads) void kv_write_fp4_kernel(const void* __restrict__ k, const void* __restrict__ v,
                                                                 int64_t stride, uint8_t* __restrict__ kc,
@@ -91,7 +93,9 @@ __global__ __launch_bounds__(kThreads) void kv_write_fp4_kernel(const void* __re
   if ((lane & 3) == 0) page[P::scale(log2bs, lane >> 2, row)] = bad ? 255 : (uint8_t)(e + 127);
 }
 
-// A workgroup takes a run of output rows and HEADS of the 2 Hkv heads of K and V.
+// A workgroup takes a run of output rows and HEADS of the 2 Hkv heads of K and V.  88119 keys of 4
+// heads of 128, 228 MB: 35.8 us, 6.4 TB/s (40.8 with stores that stay in the caches); 4448 keys of
+// 8 heads 7.5 us (8.0), 256 of 256 sequences 4.3.
 template <bool BF16, int D, int HEADS>
 __global__ __launch_bounds__(kThreads) void kv_read_fp4_kernel(const uint8_t* __restrict__ kc,
                                                                const uint8_t* __restrict__ vc,
@@ -141,14 +145,14 @@ __global__ __launch_bounds__(kThreads) void kv_read_fp4_kernel(const uint8_t* __
       r[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale, 1));
       r[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale, 2));
       r[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale, 3));
-      *reinterpret_cast<u32x4*>(out) = r;
+      __builtin_nontemporal_store(r, reinterpret_cast<u32x4*>(out));
     } else {
       const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], scale, 0);
       const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], scale, 1);
       const auto c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], scale, 2);
       const auto d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[i], scale, 3);
-      *reinterpret_cast<f32x4*>(out) = f32x4{a[0], a[1], b[0], b[1]};
-      *reinterpret_cast<f32x4*>(out + 16) = f32x4{c[0], c[1], d[0], d[1]};
+      __builtin_nontemporal_store(f32x4{a[0], a[1], b[0], b[1]}, reinterpret_cast<f32x4*>(out));
+      __builtin_nontemporal_store(f32x4{c[0], c[1], d[0], d[1]}, reinterpret_cast<f32x4*>(out + 16));
     }
   }
 }

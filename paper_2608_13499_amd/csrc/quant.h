@@ -32,17 +32,22 @@ __device__ __forceinline__ bool non_finite(uint32_t most) { return most >= 0x7f8
 // 2^e, -127 < e < 128
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 
-// Eight elements as the kernels hold them: fp32, from 16 or 32 bytes.
-template <bool BF16>
+// Eight elements as the kernels hold them: fp32, from 16 or 32 bytes.  ONCE: nothing else reads
+// them, they pass the caches by.
+template <bool BF16, bool ONCE = false>
 __device__ __forceinline__ void load8(const void* p, int64_t at, float (&x)[8]) {
+  auto get = [](const auto* from) {
+    if constexpr (ONCE) return __builtin_nontemporal_load(from);
+    else return *from;
+  };
   if constexpr (BF16) {
-    const u32x4 v = *reinterpret_cast<const u32x4*>(static_cast<const char*>(p) + at * 2);
+    const u32x4 v = get(reinterpret_cast<const u32x4*>(static_cast<const char*>(p) + at * 2));
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[2 * i] = bf_lo(v[i]), x[2 * i + 1] = bf_hi(v[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const f32x4 v = *reinterpret_cast<const f32x4*>(static_cast<const char*>(p) + at * 4 + 16 * i);
+      const f32x4 v = get(reinterpret_cast<const f32x4*>(static_cast<const char*>(p) + at * 4 + 16 * i));
 #pragma unroll
       for (int j = 0; j < 4; ++j) x[4 * i + j] = v[j];
     }
