@@ -98,7 +98,7 @@ __device__ __forceinline__ void store4(OUT* y, const OUT* bias, int64_t at, int 
 
 // Eight consecutive columns from n on, at byte `at` of a descriptor; those past N (a multiple of
 // eight in bf16, of four in fp32) go nowhere.
-template <class OUT>
+template <class OUT, int POLICY>
 __device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t y, const OUT* bias, uint32_t at, int n, int N, f32x4 lo,
                                        f32x4 hi) {
   if constexpr (sizeof(OUT) == 2) {
@@ -108,12 +108,12 @@ __device__ __forceinline__ void store8(__amdgpu_buffer_rsrc_t y, const OUT* bias
       hi[0] += bf_lo(b[2]), hi[1] += bf_hi(b[2]), hi[2] += bf_lo(b[3]), hi[3] += bf_hi(b[3]);
     }
     const u32x4 v{pack_bf2(lo[0], lo[1]), pack_bf2(lo[2], lo[3]), pack_bf2(hi[0], hi[1]), pack_bf2(hi[2], hi[3])};
-    __builtin_amdgcn_raw_buffer_store_b128(v, y, n < N ? at : kOobOffset, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(v, y, n < N ? at : kOobOffset, 0, POLICY);
   } else {
     if (bias && n < N) lo += *reinterpret_cast<const f32x4*>(bias + n);
     if (bias && n + 4 < N) hi += *reinterpret_cast<const f32x4*>(bias + n + 4);
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), y, n < N ? at : kOobOffset, 0, 0);
-    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), y, n + 4 < N ? at + 16 : kOobOffset, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, lo), y, n < N ? at : kOobOffset, 0, POLICY);
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, hi), y, n + 4 < N ? at + 16 : kOobOffset, 0, POLICY);
   }
 }
 
@@ -142,6 +142,10 @@ struct Fp8Tile {
   static constexpr int kLoadsX = BM / 8 / kWaves, kLoadsW = BN / 8 / kWaves;  // of a wave
   static constexpr int kScales = BM * 4 + 256;  // x's, then W's
   static constexpr int kStageBytes = (BM + BN) * kSlice, kLdsBytes = 2 * kStageBytes + 4 * kScales;
+  // The result past the caches (nontemporal, sc1), where it is a launch's last word: 1023 x 6144 x 4096 40 /
+  // 34 us.  Where the next tile's MFMAs hide it that costs (8871 x 28672 x 4096 912 / 920), and fp32's
+  // stores, which fill a line in two goes, lose (2048 x 6144 x 4096 109 / 132).
+  static constexpr int kStorePolicy = BM < 256 ? 18 : 0;
   static constexpr bool kChained = kLdsBytes > 80 * 1024;  // one workgroup a CU
   static_assert(BM <= BN && BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BM / 64 < kWaves, "whole loads");
   static_assert(kFp8Block % WN == 0 && BN % kFp8Block == 0, "a wave's columns lie in one block of W's scales");
@@ -404,7 +408,7 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
 
     // The item's results; the next one's first slices are on their way, its first fragments here.  Every
     // lane stores as often, out of range past the edges: the waits behind count on it.
-    auto store = [&](auto out, const auto* bias, auto* y, int64_t row0) {
+    auto store = [&](auto out, const auto* bias, auto* y, int64_t row0, auto policy) {
       using T = decltype(out);
       const int n_end = it.n0 + wn * C::WN;
 #pragma unroll
@@ -417,12 +421,12 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
 #pragma unroll
         for (int i = 0; i < TN; i += 2) {
           const int n = n_end + 16 * i + 8 * fq;
-          store8<T>(r, bias, (uint32_t)(fr * N + n) * (uint32_t)sizeof(T), n, N, acc[i][j], acc[i + 1][j]);
+          store8<T, decltype(policy)::value>(r, bias, (uint32_t)(fr * N + n) * (uint32_t)sizeof(T), n, N, acc[i][j], acc[i + 1][j]);
         }
       }
     };
-    if (a.part) store(0.f, (const float*)nullptr, a.part, (int64_t)it.split * M);
-    else store(OUT{}, static_cast<const OUT*>(a.bias), static_cast<OUT*>(a.y), 0);
+    if (a.part) store(0.f, (const float*)nullptr, a.part, (int64_t)it.split * M, Int<0>{});
+    else store(OUT{}, static_cast<const OUT*>(a.bias), static_cast<OUT*>(a.y), 0, Int<EXACT ? 0 : C::kStorePolicy>{});
     behind = a.part ? 2 : 1;
     id += kNumCUs;
     if (id >= id_end) break;
