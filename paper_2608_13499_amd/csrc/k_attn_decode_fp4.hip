@@ -6,8 +6,9 @@
 // its query heads (the columns of the MFMA; more go to further workgroups).  A wave
 // step is a tile of 32 keys, two runs of 16 consecutive slots, each in one page (a page
 // has 16 slots or more).  Their codes and scale bytes come by LDS DMA into a ring of
-// the wave's own, kRing - 1 tiles ahead, so that nothing but a counted wait stands
-// between a tile and the next; no barrier in the loop.
+// the wave's own, kRing - 1 tiles ahead, so that nothing but a wait of its own stands
+// between a tile and the next; no barrier in the loop.  Masks and modifiers are computed
+// in tiles that need them only.
 //  * Scores S^T = K Q^T on MFMA 16x16x32: a lane holds a quarter row of a key, one
 //    scale for heads of 128, widened to bf16, which holds every value of the cache.
 //  * P V: a lane holds one dword of codes (D / 16 neighbouring elements) of eight keys.
@@ -18,6 +19,10 @@
 //    of the i-th is element (D / 16) col + i.  The instruction pairs A's lane group
 //    ga, place i with B's lane group 2 (ga % 2) + i / 4, key slot 4 (ga / 2) + i % 4:
 //    that places the keys of V in the lanes (v_run, v_row).
+// Bound by the cache's bytes where they are many: 256 sequences of 4331 keys, 32 + 8 heads of 128, 1.21 GB:
+// 200 us, 6.0 TB/s, of 128 to 8192 205; without the arithmetic the loads take 197.  They pass the caches by
+// (nontemporal; with four tiles in a ring 220 us, 233 without).  One sequence of 700 keys takes 7.8 us, of 30000 15.9 with the
+// merge: chains of lengths, page ids, first loads, 1.2 us a tile, and the merge.
 // bf16 takes its probabilities in two bf16 pieces, as decode with modifiers does.  fp32
 // queries are three bf16 pieces, exactly, and their probabilities too: the products with
 // the cache's values are whole, and summed in fp32.
@@ -555,10 +560,10 @@ hipError_t launch_combine(const DecodeArgs& a, void* o, int Hq, int waves, hipSt
 
 namespace {
 // A workgroup a (sequence, head), which writes the output, as long as all run at once and a
-// wave has four tiles at most: a tile more takes a wave 0.9 us, the merge's launch 4 (us, whole /
-// split: one sequence of 256 keys, 32 + 8 heads of 128 6.5 / 10.9, 700 8.9 / 11.4, 1500 12.2 /
-// 11.6, 2500 17.0 / 13.3; 8 of 700 9.6 / 12.9, 2500 17.7 / 16.4; fp32, one of 700, 8 + 1 heads 11.1 / 12.8,
-// 1500 15.3 / 12.9).  A window bounds the tiles only where there is no prefix.
+// wave has four tiles at most: a tile more takes a wave 1.2 us, the merge's launch 4 (us, whole /
+// split, 32 + 8 heads of 128: one sequence of 256 keys 5.6 / 9.8, 700 7.8 / 10.3, 1000 9.1 / 10.6, 1500 11.4 /
+// 10.4; 8 of 1000 9.5 / 12.8, 1500 11.8 / 13.3, 2500 16.7 / 15.1; fp32, 8 + 1 heads, one of 700 10.0 / 11.4, 1000
+// 11.3 / 11.6, 1500 14.3 / 11.5).  A window bounds the tiles only where there is no prefix.
 bool whole_sequences(int64_t B, int Hkv, int blocks, int max_context_len, int window, bool prefix) {
   int64_t tiles = ((int64_t)std::max(1, max_context_len) + kTile - 1) / kTile;
   if (window > 0 && !prefix) tiles = std::min<int64_t>(tiles, window / kTile + 2);
