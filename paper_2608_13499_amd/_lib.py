@@ -1089,11 +1089,17 @@ def opscale_cu_stream_mask(stream: int, words: int):
 
 
 def opscale_cu_probe(out, spins: int = 4, stream=None):
-    """Launch the placement probe: out is an int32 [n, 2] GPU tensor (XCD, HW_ID per workgroup)."""
+    """Launch the placement probe: out is an int32 [n, 2] GPU tensor (XCD, HW_ID per workgroup).  On
+    another stream than the current one it runs behind the current one's work."""
     _dev(out)
     if out.dim() != 2 or out.shape[1] != 2 or not out.is_contiguous() or out.element_size() != 4:
         raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "out must be a contiguous 4-byte [n, 2] tensor")
-    _check(load().opscale_cu_probe(_stream(stream), _ptr(out), out.shape[0], spins))
+    handle = _stream(stream)
+    if handle != _stream(None):  # (a masked stream does not wait for the fill of a new `out` by itself)
+        import torch
+        on = torch.cuda.ExternalStream(handle, device=out.device) if handle else torch.cuda.default_stream(out.device)
+        on.wait_stream(torch.cuda.current_stream(out.device))
+    _check(load().opscale_cu_probe(handle, _ptr(out), out.shape[0], spins))
     return out
 
 
