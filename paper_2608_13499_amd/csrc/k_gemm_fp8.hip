@@ -138,16 +138,16 @@ struct LinearFp8Args {
 // at the slices' two barriers and counted waits.  8871 x 4096 x 14336 takes 510 us, 1023 x 6144 x 4096 36,
 // 200 x 4096 x 4096 20 with its second launch; fp32 2048 x 6144 x 4096 109.
 //
-// BM x BN of y an item, 2 x WGN waves.  LDS holds two slices of x's and W's rows and four of their
-// scales, filled by LDS DMA.
-template <int BM_, int BN_, int WGN_>
+// BM x BN of y an item, 2 x WGN waves.  LDS holds RING slices of x's and W's rows and four of their
+// scales, filled by LDS DMA two slices ahead.
+template <int BM_, int BN_, int WGN_, int RING_>
 struct Fp8Tile {
   static constexpr int BM = BM_, BN = BN_, WGM = 2, WGN = WGN_;
   static constexpr int kWaves = WGM * WGN, kThreads = 64 * kWaves;
   static constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16;
   static constexpr int kLoadsX = BM / 8 / kWaves, kLoadsW = BN / 8 / kWaves;  // of a wave
   static constexpr int kScales = BM * 4 + 256;  // x's, then W's
-  static constexpr int kStageBytes = (BM + BN) * kSlice, kLdsBytes = 2 * kStageBytes + 4 * kScales;
+  static constexpr int kStageBytes = (BM + BN) * kSlice, kRing = RING_, kLdsBytes = kRing * kStageBytes + 4 * kScales;
   // The result past the caches (nontemporal, sc1), where it is a launch's last word: 1023 x 6144 x 4096 40 /
   // 34 us.  Where the next tile's MFMAs hide it that costs (8871 x 28672 x 4096 912 / 920), and fp32's
   // stores, which fill a line in two goes, lose (2048 x 6144 x 4096 109 / 132).
@@ -192,7 +192,7 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   // The scales: each of the first BM / 64 waves loads those of 64 rows of x, the others those of W's
   // BN / 128 blocks.
   const bool x_scales = wave < BM / 64;
-  const int s_to = 2 * C::kStageBytes + (x_scales ? wave * 256 : BM * 4);
+  const int s_to = C::kRing * C::kStageBytes + (x_scales ? wave * 256 : BM * 4);
   const uint32_t s_from = x_scales ? (uint32_t)(wave * 64 + lane) * 4 : lane < BN / kFp8Block ? (uint32_t)(lane * a.nkb) * 4 : kOobOffset;
 
   struct Item {
@@ -268,15 +268,16 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
     woff[h] = (8 * (fr >> 2) + (fr & 3)) * kSlice + chunk;
   }
   const int x0 = wm * C::WM * kSlice, w0 = (BM + wn * C::WN) * kSlice;
-  const int s0 = 2 * C::kStageBytes + (wm * C::WM + fr) * 4;
-  const int ws0 = 2 * C::kStageBytes + BM * 4 + wn * C::WN / kFp8Block * 4;
+  const int s0 = C::kRing * C::kStageBytes + (wm * C::WM + fr) * 4;
+  const int ws0 = C::kRing * C::kStageBytes + BM * 4 + wn * C::WN / kFp8Block * 4;
 
   // A slice: W's fragments are in registers from the start, so that behind a barrier W's slice after
   // the next is sent for into their place.  The last two rows of x's fragments are read before the
   // second barrier; behind it their MFMAs run while the next slice's first fragments are read into
   // the registers that they free, and x's slice after the next is sent for.  The loads are spread
   // between the MFMAs: those of all waves at once would fill the address unit's queue, and a wave
-  // that waits there issues no MFMA.
+  // that waits there issues no MFMA.  With three slices in LDS the one after the next has a place of
+  // its own and the first barrier falls away (1024 x 8192 x 4096 42 / 40 us; 256 x 256 tiles have no room).
   Frag w[TN], x[C::kSlots];
   float f[C::kSlots], wscale;
   OPS_LDS char* st = smem;
@@ -287,7 +288,15 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   };
   auto read_w = [&](int i) { w[i] = read_frag(st + w0 + (32 * (i >> 1) + 4 * (i & 1)) * kSlice, woff); };
   auto read_wscale = [&] { return *reinterpret_cast<const OPS_LDS float*>(smem + ws0 + (slices & 3) * C::kScales); };
-  auto other = [&] { return st == smem ? smem + C::kStageBytes : smem; };
+  auto after = [&](OPS_LDS char* at) {
+    if constexpr (C::kRing == 2) return at == smem ? smem + C::kStageBytes : smem;
+    else return at == smem + (C::kRing - 1) * C::kStageBytes ? smem : at + C::kStageBytes;
+  };
+  // where the slice two behind the one at `at` goes
+  auto ahead = [&](OPS_LDS char* at) {
+    if constexpr (C::kRing == 2) return at;
+    else return after(after(at));
+  };
   // The next slice has arrived, in every wave.  Behind it in the queue are W's loads of the slice
   // after it, and in an item's first slice the stores of the one before.
   int behind = 0;  // 0: no stores; 1: of the result; 2: of partial sums
@@ -329,7 +338,7 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   }
   ready();
 #pragma unroll
-  for (int g = 0; g < C::kLoadsX; ++g) load_x(g, other());
+  for (int g = 0; g < C::kLoadsX; ++g) load_x(g, smem + C::kStageBytes);
   advance();
   read_x(0);
   wscale = read_wscale();
@@ -342,6 +351,7 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
 #pragma unroll
       for (int j = 0; j < TM; ++j) acc[i][j] = f32x4{};
     for (int kt = 0; kt < it.ns; ++kt) {
+      OPS_LDS char* const dest = ahead(st);
       float scale[C::kSlots];
       const float ws = wscale;
 #pragma unroll
@@ -363,18 +373,17 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
             for (int g = 0; g < C::kLoadsW + 1; ++g)
               if (n == g * kMfmas / (C::kLoadsW + 1)) {
                 if (g == 0) load_scales(slices + 2);
-                else load_w(g - 1, st);
+                else load_w(g - 1, dest);
               }
             pin();
           }
         }
-        if (j == 0) barrier_keep_loads();
+        if (C::kRing == 2 && j == 0) barrier_keep_loads();
       }
       scale[C::slot(ja)] = f[C::slot(ja)] * ws, scale[C::slot(jb)] = f[C::slot(jb)] * ws;
       ready();
       pin();
-      OPS_LDS char* const left = st;
-      st = other();
+      st = after(st);
       ++slices;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -399,7 +408,7 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
             wscale = read_wscale();
           }
           read_w(n);
-          if (n < C::kLoadsX) load_x(n, left);
+          if (n < C::kLoadsX) load_x(n, dest);
           pin();
         }
         if (h == 1)
@@ -670,9 +679,9 @@ __global__ __launch_bounds__(256) void fp8_reduce_kernel(const float* __restrict
 
 namespace {
 
-using Tile256 = Fp8Tile<256, 256, 4>;  // 8 waves of 128 x 64, 130 KB
-using Tile128x256 = Fp8Tile<128, 256, 4>;  // 8 waves of 64 x 64, 99 KB
-using Tile128 = Fp8Tile<128, 128, 2>;  // 4 waves of 64 x 64, 65 KB: two workgroups a CU
+using Tile256 = Fp8Tile<256, 256, 4, 2>;  // 8 waves of 128 x 64, 130 KB
+using Tile128x256 = Fp8Tile<128, 256, 4, 3>;  // 8 waves of 64 x 64, 147 KB
+using Tile128 = Fp8Tile<128, 128, 2, 2>;  // 4 waves of 64 x 64, 65 KB: two workgroups a CU
 
 constexpr int64_t kRowsMaxM = 128;
 

@@ -173,9 +173,10 @@ def test_linear_bias_and_spread(ops, dtype, M, N, K):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("M,N,K", [(1000, 520, 144), (770, 1288, 272), (2, 57344, 128), (4, 4096, 14336)])
+@pytest.mark.parametrize("M,N,K", [(1000, 520, 144), (770, 1288, 272), (2, 57344, 128), (4, 4096, 14336), (1023, 4616, 400),
+                                   (1000, 3080, 12304), (1023, 8712, 400), (8200, 12296, 400)])
 def test_linear_large(ops, dtype, M, N, K):
-    """Several tiles a dimension; a row or two of wide and of deep weights."""
+    """Several tiles of each shape a dimension, several a workgroup; a row or two of wide and of deep weights."""
     import torch
     say(f"linear_fp8 {dtype} {M} x {N} x {K}, sampled")
     xc, xs, wc, ws = operands(M, N, K, 11)
