@@ -513,7 +513,7 @@ opscale_status opscale_linear_fp8(const void* x, const float* x_scales, const vo
  * opscale_reshape_and_cache to such a cache: the K and V rows of token t (k, v: [T, Hkv,
  * D], rows of kv_row_stride elements) go to slot slot_mapping[t], quantised.  A token
  * whose slot is outside [0, num_blocks * block_size) is skipped (padding).  num_blocks *
- * block_size < 2^31, T < 2^28.  The caches overlap nothing else.  Tokens sharing a slot race.
+ * block_size < 2^31; T < 2^28 (heads of 128: up to 2^28 - 16).  The caches overlap nothing else.  Tokens sharing a slot race.
  */
 opscale_status opscale_kv_write_fp4(const void* k, const void* v, int64_t kv_row_stride, void* k_cache, void* v_cache,
                                     const int32_t* slot_mapping, int64_t T, int32_t Hkv, int32_t D, int32_t block_size,
@@ -525,8 +525,8 @@ opscale_status opscale_kv_write_fp4(const void* k, const void* v, int64_t kv_row
  * cu_seqlens: DEVICE int32 [B + 1], cu_seqlens[0] = 0, non-decreasing, cu_seqlens[B] <=
  * total_tokens (the rows past it are left as they were); first_keys: DEVICE int32 [B], or
  * NULL (0); block_table: DEVICE int32 [B, max_blocks_per_seq].
- * k, v: [total_tokens, Hkv, D], total_tokens < 2^28, rows of kv_row_stride elements (both may be views into
- * one tensor); they overlap nothing else.  A key below 0, past max_blocks_per_seq pages, or
+ * k, v: [total_tokens, Hkv, D], total_tokens < 2^28 (heads of 128: up to 2^28 - 16), rows of
+ * kv_row_stride elements (both may be views into one tensor); they overlap nothing else.  A key below 0, past max_blocks_per_seq pages, or
  * whose page is outside [0, num_blocks) reads as zeros.  Values past bf16's or fp32's range
  * do not arise from opscale_kv_write_fp4.
  */

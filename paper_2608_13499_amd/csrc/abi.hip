@@ -479,6 +479,13 @@ opscale_status check_decode_mod(const void* q, int64_t qs, const void* kc, const
                              max_ctx, scale, m, dt, ws, ws_bytes, (int64_t)D * esize(dt));
 }
 
+constexpr int64_t kMaxGroups256 = 1 << 24;  // workgroups of 256 threads: a launch has fewer than 2^32 threads
+
+// Tokens of a call on such a cache, 2048 / D a workgroup (D 64 or 128).
+bool fp4_tokens_ok(int64_t T, int32_t D) {
+  return T >= 0 && T < ((int64_t)1 << 28) && T <= 2048 / D * (kMaxGroups256 - 1);
+}
+
 // Heads, pages and sizes of such a cache.
 opscale_status check_fp4_cache(const char* who, int32_t Hkv, int32_t D, int32_t bs) {
   if (Hkv <= 0 || D <= 0 || (int64_t)Hkv * D > (1 << 20))
@@ -664,14 +671,11 @@ opscale_status check_block_tables(const int32_t* ctx, const int32_t* fresh, int3
   return OPSCALE_OK;
 }
 
-constexpr int64_t kMaxGroups256 = 1 << 24;  // workgroups of 256 threads
-
 opscale_status check_quantize_fp8(const void* x, int64_t xs, const void* q, const float* scales, int64_t M, int64_t K,
                                   opscale_dtype dt) {
   const char* who = "quantize_fp8";
   if (!dtype_ok(dt)) return fail(OPSCALE_ERR_INVALID_ARG, "%s: unknown dtype %d", who, (int)dt);
   const int s = esize(dt);
-  // (a launch has fewer than 2^32 threads)
   if (M < 0 || K <= 0 || M >= kMaxDim || K > (1 << 20) || K % 16 || (M + 15) / 16 * ((K + 511) / 512) >= kMaxGroups256)
     return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes M=%lld K=%lld (K a multiple of 16, up to 2^20; ceil(M / 16) * "
                 "ceil(K / 512) below 2^24)", who, (long long)M, (long long)K);
@@ -733,8 +737,9 @@ opscale_status check_kv_write_fp4(const void* k, const void* v, int64_t kvs, con
   const opscale_status st = check_fp4_cache(who, Hkv, D, bs);
   if (st != OPSCALE_OK) return st;
   const int s = esize(dt);
-  if (T < 0 || T >= 16 * kMaxGroups256 || nb < 1 || nb >= kMaxDim / bs)
-    return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes T=%lld (below 2^28) num_blocks=%lld of %d", who, (long long)T, (long long)nb, bs);
+  if (!fp4_tokens_ok(T, D) || nb < 1 || nb >= kMaxDim / bs)
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes T=%lld (below 2^28, heads of 128 up to 2^28 - 16) num_blocks=%lld of %d",
+                who, (long long)T, (long long)nb, bs);
   if (T == 0) return OPSCALE_OK;
   if (kvs < (int64_t)Hkv * D || kvs * s % 16 || kvs > ((int64_t)1 << 32))
     return fail(OPSCALE_ERR_INVALID_ARG, "%s: kv_row_stride=%lld must cover the heads and be a multiple of 16 bytes", who,
@@ -757,8 +762,9 @@ opscale_status check_kv_read_fp4(const void* kc, const void* vc, const int32_t* 
   const opscale_status st = check_fp4_cache(who, Hkv, D, bs);
   if (st != OPSCALE_OK) return st;
   const int s = esize(dt);
-  if (B < 0 || T < 0 || T >= 16 * kMaxGroups256)
-    return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes B=%d total_tokens=%lld (below 2^28)", who, B, (long long)T);
+  if (B < 0 || !fp4_tokens_ok(T, D))
+    return fail(OPSCALE_ERR_INVALID_ARG, "%s: bad sizes B=%d total_tokens=%lld (below 2^28, heads of 128 up to 2^28 - 16)", who,
+                B, (long long)T);
   if (B == 0 || T == 0) return OPSCALE_OK;
   if (max_blocks < 1 || nb < 1 || nb > kMaxDim || nb * bs > ((int64_t)1 << 36))
     return fail(OPSCALE_ERR_INVALID_ARG, "%s: max_blocks_per_seq=%d num_blocks=%lld of %d", who, max_blocks, (long long)nb, bs);
