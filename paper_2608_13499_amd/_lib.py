@@ -823,6 +823,25 @@ def opscale_linear_fp8_workspace_size(M: int, N: int, K: int, dtype=None) -> int
     return load().opscale_linear_fp8_workspace_size(M, N, K, dt)
 
 
+def _linear_fp8_shapes(x, W):
+    """(M, N, K, blocks of K, blocks of N)."""
+    if x.dim() != 2 or W.dim() != 2 or W.shape[1] != x.shape[1]:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"x {tuple(x.shape)} and W {tuple(W.shape)} must be [M, K] and [N, K]")
+    (M, K), N = x.shape, W.shape[0]
+    return M, N, K, (K + 127) // 128, (N + 127) // 128
+
+
+def _linear_fp8_workspace(x, M, N, K, dt, workspace, stream, dev):
+    """The workspace to pass, with its bytes: given, allocated by torch (None), or none at all (False)."""
+    if workspace is None:
+        need = load().opscale_linear_fp8_workspace_size(M, N, K, dt)
+        return (_scratch(need, x, stream), need) if need else (None, 0)
+    if workspace is False:
+        return None, 0
+    _flat("workspace", workspace, workspace.numel(), workspace.dtype, dev)
+    return workspace, workspace.numel() * workspace.element_size()
+
+
 def opscale_linear_fp8(x, x_scales, W, w_scales, bias=None, dtype=None, y=None, workspace=None, stream=None,
                        timed: bool = False):
     """y[M, N] = x[M, K] W[N, K]^T (+ bias) of float8_e4m3fn operands, x_scales float32
@@ -831,10 +850,7 @@ def opscale_linear_fp8(x, x_scales, W, w_scales, bias=None, dtype=None, y=None, 
     tensor) is allocated by torch when None; False passes none."""
     lib = load()
     dev = _current_narrow()
-    if x.dim() != 2 or W.dim() != 2 or W.shape[1] != x.shape[1]:
-        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"x {tuple(x.shape)} and W {tuple(W.shape)} must be [M, K] and [N, K]")
-    (M, K), N = x.shape, W.shape[0]
-    nkb, nnb = (K + 127) // 128, (N + 127) // 128
+    M, N, K, nkb, nnb = _linear_fp8_shapes(x, W)
     if y is None:
         if dtype is None:
             import torch
@@ -843,14 +859,7 @@ def opscale_linear_fp8(x, x_scales, W, w_scales, bias=None, dtype=None, y=None, 
     elif dtype is not None and dtype != y.dtype:
         raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"y is {y.dtype}, dtype {dtype}")
     dt = _dt(y)
-    if workspace is None:
-        need = lib.opscale_linear_fp8_workspace_size(M, N, K, dt)
-        ws, nbytes = (_scratch(need, x, stream), need) if need else (None, 0)
-    elif workspace is False:
-        ws, nbytes = None, 0
-    else:
-        ws, nbytes = workspace, workspace.numel() * workspace.element_size()
-        _flat("workspace", ws, ws.numel(), ws.dtype, dev)
+    ws, nbytes = _linear_fp8_workspace(x, M, N, K, dt, workspace, stream, dev)
     t = Timing() if timed else None
     _check(lib.opscale_linear_fp8(_cache("x", x, (M, K), _e4m3, dev), _cache("x_scales", x_scales, (nkb, M), _f32, dev),
                                   _cache("W", W, (N, K), _e4m3, dev),
@@ -869,6 +878,14 @@ def _fp4_caches(k_cache, v_cache, dev):
     return nb, bs, Hkv, row * 32 // 17, _cache("k_cache", k_cache, shape, _u8, dev), _cache("v_cache", v_cache, shape, _u8, dev)
 
 
+def _kv_rows(k, v, shape, dev):
+    """The row stride that k and v [T, Hkv, D] share."""
+    stride = _rows("k", k, shape, k.dtype, dev)
+    if stride != _rows("v", v, shape, k.dtype, dev):
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "k and v must share a row stride")
+    return stride
+
+
 def opscale_kv_write_fp4(k, v, k_cache, v_cache, slot_mapping, stream=None, timed: bool = False):
     """Write k, v [T, Hkv, D] (token dimension may be strided) in 4 bits, with a scale for
     each 32 elements, into paged caches, uint8 [num_blocks, Hkv, block_size, D / 2 + D /
@@ -877,9 +894,7 @@ def opscale_kv_write_fp4(k, v, k_cache, v_cache, slot_mapping, stream=None, time
     dev, dt = _current_narrow(), _dt(k)
     nb, bs, Hkv, D, kc, vc = _fp4_caches(k_cache, v_cache, dev)
     shape = k.shape[0], Hkv, D
-    ks, vs = _rows("k", k, shape, k.dtype, dev), _rows("v", v, shape, k.dtype, dev)
-    if ks != vs:
-        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "k and v must share a row stride")
+    ks = _kv_rows(k, v, shape, dev)
     t = Timing() if timed else None
     _check(lib.opscale_kv_write_fp4(k.data_ptr(), v.data_ptr(), ks, kc, vc,
                                     _flat("slot_mapping", slot_mapping, shape[0], _i32, dev), shape[0], Hkv, D, bs, nb,
@@ -908,9 +923,7 @@ def opscale_kv_read_fp4(k_cache, v_cache, block_table, cu_seqlens, total_tokens:
     else:
         if dtype is not None and dtype != k.dtype:
             raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"k is {k.dtype}, dtype {dtype}")
-        ks = _rows("k", k, shape, k.dtype, dev)
-        if ks != _rows("v", v, shape, k.dtype, dev):
-            raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "k and v must share a row stride")
+        ks = _kv_rows(k, v, shape, dev)
     dt = _dt(k)
     if block_table.dim() != 2:
         raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "block_table must be [B, max_blocks_per_seq]")
@@ -1279,49 +1292,70 @@ def desc_attn_decode_mod(q, k_cache, v_cache, block_table, context_lens, out, ma
     return d
 
 
+# (of 8 and 4 bits: with the checks that the calls make)
 def desc_quantize_fp8(x, q, scales) -> OpDesc:
+    dev = _current_narrow()
     d = OpDesc(op=OP_QUANTIZE_FP8, dt=_dt(x))
-    M, K = x.shape
-    d.u.quantize_fp8 = _QuantizeFp8Args(_ptr(x), x.stride(0), _ptr(q), _ptr(scales), M, K)
+    M, K, xs = _matrix("x", x, x.dtype, dev)
+    d.u.quantize_fp8 = _QuantizeFp8Args(_ptr(x), xs, _cache("q", q, (M, K), _e4m3, dev),
+                                        _cache("scales", scales, ((K + 127) // 128, M), _f32, dev), M, K)
     return d
 
 
 def desc_linear_fp8(x, x_scales, W, w_scales, y, bias=None, workspace=None) -> OpDesc:
+    """`workspace` must stay alive while the descriptor is used (see
+    opscale_linear_fp8 for None / False)."""
+    dev = _current_narrow()
     d = OpDesc(op=OP_LINEAR_FP8, dt=_dt(y))
-    M, K = x.shape
-    d.u.linear_fp8 = _LinearFp8Args(_ptr(x), _ptr(x_scales), _ptr(W), _ptr(w_scales), _ptr(bias), _ptr(y), M, W.shape[0],
-                                    K, _ptr(workspace),
-                                    0 if workspace is None else workspace.numel() * workspace.element_size())
+    M, N, K, nkb, nnb = _linear_fp8_shapes(x, W)
+    ws, nbytes = _linear_fp8_workspace(x, M, N, K, d.dt, workspace, None, dev)
+    d.u.linear_fp8 = _LinearFp8Args(_cache("x", x, (M, K), _e4m3, dev), _cache("x_scales", x_scales, (nkb, M), _f32, dev),
+                                    _cache("W", W, (N, K), _e4m3, dev), _cache("w_scales", w_scales, (nnb, nkb), _f32, dev),
+                                    None if bias is None else _flat("bias", bias, N, y.dtype, dev),
+                                    _cache("y", y, (M, N), y.dtype, dev), M, N, K, _ptr(ws), nbytes)
+    d._keep = ws
     return d
 
 
 def desc_kv_write_fp4(k, v, k_cache, v_cache, slot_mapping) -> OpDesc:
+    dev = _current_narrow()
     d = OpDesc(op=OP_KV_WRITE_FP4, dt=_dt(k))
-    T, Hkv, D = k.shape
-    d.u.kv_write_fp4 = _CacheWriteArgs(_ptr(k), _ptr(v), k.stride(0), _ptr(k_cache), _ptr(v_cache), _ptr(slot_mapping), T,
-                                       Hkv, D, k_cache.shape[2], k_cache.shape[0])
+    nb, bs, Hkv, D, kc, vc = _fp4_caches(k_cache, v_cache, dev)
+    T = k.shape[0]
+    d.u.kv_write_fp4 = _CacheWriteArgs(_ptr(k), _ptr(v), _kv_rows(k, v, (T, Hkv, D), dev), kc, vc,
+                                       _flat("slot_mapping", slot_mapping, T, _i32, dev), T, Hkv, D, bs, nb)
     return d
 
 
 def desc_kv_read_fp4(k_cache, v_cache, block_table, cu_seqlens, k, v, first_keys=None) -> OpDesc:
+    dev = _current_narrow()
     d = OpDesc(op=OP_KV_READ_FP4, dt=_dt(k))
-    T, Hkv, D = k.shape
+    nb, bs, Hkv, D, kc, vc = _fp4_caches(k_cache, v_cache, dev)
+    T = k.shape[0]
+    if block_table.dim() != 2:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, "block_table must be [B, max_blocks_per_seq]")
     B, cols = block_table.shape
-    d.u.kv_read_fp4 = _KvReadFp4Args(_ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(cu_seqlens), _ptr(first_keys),
-                                     _ptr(k), _ptr(v), k.stride(0), B, T, Hkv, D, k_cache.shape[2], cols,
-                                     k_cache.shape[0])
+    d.u.kv_read_fp4 = _KvReadFp4Args(kc, vc, _flat("block_table", block_table, B * cols, _i32, dev),
+                                     _flat("cu_seqlens", cu_seqlens, B + 1, _i32, dev),
+                                     None if first_keys is None else _flat("first_keys", first_keys, B, _i32, dev),
+                                     _ptr(k), _ptr(v), _kv_rows(k, v, (T, Hkv, D), dev), B, T, Hkv, D, bs, cols, nb)
     return d
 
 
 def desc_attn_decode_fp4(q, k_cache, v_cache, block_table, context_lens, out, max_context_len, scale, workspace,
                          softcap=0.0, slopes=None, window=0, prefix_lens=None, doc_starts=None) -> OpDesc:
+    dev = _current_narrow()
     d = OpDesc(op=OP_ATTN_DECODE_FP4, dt=_dt(q))
-    B, Hq, D = q.shape
-    nb, Hkv, bs, _ = k_cache.shape
-    _heads_view("q", q, Hq, D)
-    d.u.attn_decode_fp4 = _DecodeModArgs(_ptr(q), q.stride(0), _ptr(k_cache), _ptr(v_cache), _ptr(block_table),
-                                         _ptr(context_lens), _ptr(out), B, Hq, Hkv, D, bs, block_table.shape[1], nb,
-                                         max_context_len, scale,
-                                         AttnMods(softcap, window, _ptr(slopes), _ptr(prefix_lens), _ptr(doc_starts)),
-                                         _ptr(workspace), workspace.numel() * workspace.element_size())
+    nb, bs, Hkv, D, kc, vc = _fp4_caches(k_cache, v_cache, dev)
+    if q.dim() != 3 or q.shape[2] != D or block_table.dim() != 2:
+        raise OpscaleError(OPSCALE_ERR_INVALID_ARG, f"q must be [B, Hq, {D}], block_table [B, max_blocks]")
+    shape = B, Hq, D = q.shape
+    qs, cols = _rows("q", q, shape, q.dtype, dev), block_table.shape[1]
+    mods = _mods(softcap, slopes, window, prefix_lens, doc_starts, Hq, B, B, dev)
+    d.u.attn_decode_fp4 = _DecodeModArgs(_ptr(q), qs, kc, vc, _flat("block_table", block_table, B * cols, _i32, dev),
+                                         _flat("context_lens", context_lens, B, _i32, dev),
+                                         _flat("out", out, B * Hq * D, q.dtype, dev), B, Hq, Hkv, D, bs, cols, nb,
+                                         max_context_len, scale, mods._obj,
+                                         _flat("workspace", workspace, workspace.numel(), workspace.dtype, dev),
+                                         workspace.numel() * workspace.element_size())
     return d
