@@ -10,6 +10,7 @@
 #include <string>
 #include <vector>
 
+#include "gemm_fp8_plan.h"
 #include "launch.h"
 #include "opscale.h"
 #include "status.h"

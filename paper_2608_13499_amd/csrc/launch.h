@@ -140,17 +140,8 @@ hipError_t launch_attn_decode_fp4(const void* q, int64_t q_stride, const void* k
                                   int32_t block_size, int32_t max_blocks, int64_t num_blocks, int32_t max_context_len,
                                   float scale, const opscale_attn_mods* m, bool bf16, void* ws, hipStream_t s);
 
-// The linear of e4m3 operands (k_gemm_fp8.hip); the workspace query and the launch take
-// the same plan.  split_ok == false plans no K split, which needs no workspace.
-struct LinearFp8Plan {
-  enum Path { kRows = 0, kTile256 = 1, kTile128x256 = 2, kTile128 = 3, kFew = 4 };
-  int path;
-  int waves;        // rows: waves of a workgroup
-  int splits;       // K ranges (fp32 partials [splits, M, N] where more than one)
-  int chunk;        // blocks of K of a range
-  size_t ws_bytes;
-};
-LinearFp8Plan plan_linear_fp8(int64_t M, int64_t N, int64_t K, bool bf16, bool split_ok);
+// The linear of e4m3 operands (k_gemm_fp8.hip) on a plan of gemm_fp8_plan.h.
+struct LinearFp8Plan;
 hipError_t launch_linear_fp8(const LinearFp8Plan& p, const void* x, const float* xs, const void* w, const float* ws,
                              const void* bias, void* y, int64_t M, int64_t N, int64_t K, bool bf16, void* work,
                              hipStream_t s);
