@@ -301,14 +301,16 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
     else return after(after(at));
   };
   // The next slice has arrived, in every wave.  Behind it in the queue are W's loads of the slice
-  // after it, and in an item's first slice the stores of the one before.
-  int behind = 0;  // 0: no stores; 1: of the result; 2: of partial sums
+  // after it, and in a chained item's first slice the stores of the one before: of bf16 results, one
+  // for eight columns.  (fp32 results and ranges of K are not chained; behind partial sums a wait
+  // that counts no stores would only be longer.)
+  static_assert(!(EXACT && C::kChained), "the stores that a wait counts");
+  bool behind = false;
   constexpr int kStores = TM * TN / 2;
   auto ready = [&] {
-    if (behind == 0) wait_vmcnt_le<C::kLoadsW + 1>();
-    else if (behind == 1) wait_vmcnt_le<C::kLoadsW + 1 + kStores * (EXACT ? 2 : 1)>();
-    else wait_vmcnt_le<C::kLoadsW + 1 + kStores * 2>();
-    behind = 0;
+    if (behind) wait_vmcnt_le<C::kLoadsW + 1 + kStores>();
+    else wait_vmcnt_le<C::kLoadsW + 1>();
+    behind = false;
     barrier_keep_loads();
   };
   // A product is scaled and added a group of products after its own: p holds a group, of TN
@@ -445,7 +447,7 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
     };
     if (a.part) store(0.f, (const float*)nullptr, a.part, (int64_t)it.split * M, Int<0>{});
     else store(OUT{}, static_cast<const OUT*>(a.bias), static_cast<OUT*>(a.y), 0, Int<EXACT ? 0 : C::kStorePolicy>{});
-    behind = a.part ? 2 : 1;
+    behind = !a.part;
     id += kNumCUs;
     if (id >= id_end) break;
     it = next;
@@ -696,8 +698,9 @@ hipError_t launch_tile(LinearFp8Args a, int splits, hipStream_t s) {
   // tile-rows whose x (8 MB of it) stays cached while they sweep the columns, four at least
   a.group_m = (int)std::max<int64_t>(1, std::min<int64_t>(tiles_m, std::max<int64_t>(4, ((int64_t)8 << 20) / ((int64_t)C::BM * a.K))));
   a.splits = splits;
-  // (a chain's loads run two slices into the next item and look at the third: none is shorter)
-  a.chained = C::kChained && a.nkb - (splits - 1) * a.chunk >= 3;
+  // (a chain's loads run two slices into the next item and look at the third: none is shorter.  Ranges of
+  // K are two rounds at most, which no chain joins.)
+  a.chained = C::kChained && splits == 1 && a.nkb >= 3;
   const int64_t grid = chain_grid(tiles_m * a.tiles_n * splits, a.chained, true);
   hipLaunchKernelGGL((gemm_fp8_tile_kernel<C, OUT>), dim3((unsigned)grid), dim3(C::kThreads), C::kLdsBytes, s, a);
   return hipGetLastError();
