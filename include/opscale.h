@@ -484,9 +484,12 @@ size_t opscale_linear_fp8_workspace_size(int64_t M, int64_t N, int64_t K, opscal
  *   y[m, n] = sum_b x_scales[b, m] w_scales[n / 128, b] sum_{k in block b} x[m, k] W[n, k] (+ bias[n]),
  * block b being elements 128 b .. 128 b + 127 of K.
  * x: [M, K] bytes with x_scales fp32 [ceil(K / 128), M], as opscale_quantize_fp8 leaves
- * them (any fp32 scales will do); W: [N, K] bytes with w_scales fp32 [ceil(N / 128),
+ * them, or with any other scales; W: [N, K] bytes with w_scales fp32 [ceil(N / 128),
  * ceil(K / 128)]; bias: [N] of dt, or NULL; y: [M, N] of dt, overlapping nothing else.
- * Scales and sums over the blocks are fp32.  bf16 results: the inner sums are those of
+ * The two scales of a block are multiplied first, in fp32: their product has to lie in its
+ * range.  Past it, a block gives what an infinite scale gives (infinities, and NaN where its
+ * sum is 0); below 2^-126 the product is rounded to a multiple of 2^-149.  Sums over the
+ * blocks are fp32.  bf16 results: the inner sums are those of
  * the fp8 matrix instructions, which cut each product to 2^-13 of the largest of its eight
  * (k = 8 i .. 8 i + 7); fp32 results: the products are whole and summed in fp32.
  * K a multiple of 16, up to 2^20; N * sizeof(dt) a multiple of 16, N up to 2^24; M below

@@ -846,7 +846,8 @@ def opscale_linear_fp8(x, x_scales, W, w_scales, bias=None, dtype=None, y=None, 
                        timed: bool = False):
     """y[M, N] = x[M, K] W[N, K]^T (+ bias) of float8_e4m3fn operands, x_scales float32
     [ceil(K / 128), M] (opscale_quantize_fp8) and w_scales float32 [ceil(N / 128),
-    ceil(K / 128)].  dtype: of y and bias (y's, or bfloat16).  `workspace` (a uint8 GPU
+    ceil(K / 128)], whose products lie in float32's range (past it they are infinite
+    scales).  dtype: of y and bias (y's, or bfloat16).  `workspace` (a uint8 GPU
     tensor) is allocated by torch when None; False passes none."""
     lib = load()
     dev = _current_narrow()
