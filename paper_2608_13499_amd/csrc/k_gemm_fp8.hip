@@ -305,12 +305,12 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   // for eight columns.  (fp32 results and ranges of K are not chained; behind partial sums a wait
   // that counts no stores would only be longer.)
   static_assert(!(EXACT && C::kChained), "the stores that a wait counts");
-  bool behind = false;
+  int behind = 0;  // 1: those stores
   constexpr int kStores = TM * TN / 2;
   auto ready = [&] {
-    if (behind) wait_vmcnt_le<C::kLoadsW + 1 + kStores>();
-    else wait_vmcnt_le<C::kLoadsW + 1>();
-    behind = false;
+    if (!C::kChained || behind == 0) wait_vmcnt_le<C::kLoadsW + 1>();
+    else wait_vmcnt_le<C::kLoadsW + 1 + kStores>();
+    behind = 0;
     barrier_keep_loads();
   };
   // A product is scaled and added a group of products after its own: p holds a group, of TN
@@ -447,7 +447,7 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
     };
     if (a.part) store(0.f, (const float*)nullptr, a.part, (int64_t)it.split * M, Int<0>{});
     else store(OUT{}, static_cast<const OUT*>(a.bias), static_cast<OUT*>(a.y), 0, Int<EXACT ? 0 : C::kStorePolicy>{});
-    behind = !a.part;
+    if (!a.part) behind = 1;
     id += kNumCUs;
     if (id >= id_end) break;
     it = next;
