@@ -57,9 +57,15 @@ inline bool few(int64_t M, int64_t N) { return cdiv(M, 16) * cdiv(N, 16) <= kNum
 // Tiles: the shape, and the ranges of K where the tiles are fewer than the CUs, that are done
 // first by what each takes, in us: a slice of K over a round of the CUs, a launch's first loads
 // and last stores, and for ranges of K the sums' way through memory and the second launch.
-// (Measured / estimated, 256 x 256, 128 x 256 and 128 x 128: 1024 x 6144 x 4096 50 / 53, 37 / 37, 41 / 46;
-// 256 x 28672 x 4096 54, 46, 50; 2048 x 6144 x 4096 56 / 53, 73 / 70, 72 / 72; 1024 x 4096 x 4096 49, 34, 30 / 29;
-// 8871 x 6144 x 4096 215, 245, 275; 200 x 4096 x 4096 on 128 x 128 in one range 26 / 29, two 23 / 23.)
+// (Measured / estimated, 256 x 256, 128 x 256 and 128 x 128, in ranges of K where those are faster:
+//   256 x 4096 x 4096    29 / 28    22 / 24    21 / 22      1024 x 4096 x 4096    41 / 49    30 / 37    28 / 29
+//   256 x 6144 x 4096    30 / 32    23 / 28    22 / 26      1024 x 8192 x 4096    49 / 53    36 / 37    43 / 46
+//   256 x 4096 x 14336   41 / 46    37 / 39    36 / 38      2048 x 6144 x 4096    55 / 53    64 / 70    68 / 72
+//   256 x 28672 x 4096   53 / 53    41 / 37    49 / 46      4096 x 6144 x 4096   105 / 102  107 / 104  124 / 133
+//   512 x 4096 x 14336   52 / 61    48 / 53    56 / 60      8871 x 6144 x 4096   220 / 201  240 / 238  277 / 305
+//   512 x 6144 x 4096    37 / 43    29 / 36    27 / 29      8871 x 4096 x 14336  501 / 524  516 / 591  588 / 697
+//   1023 x 6144 x 4096   49 / 53    32 / 37    39 / 46      8871 x 28672 x 4096  910 / 797 1069 / 1045 1253 / 1342
+// The estimates are up to 27 % off; the shape that they choose is the fastest of the three at each size.)
 inline LinearFp8Plan tile_plan(int64_t M, int64_t N, int64_t nkb, bool bf16, bool split_ok) {
   struct Shape {
     LinearFp8Plan::Path path;

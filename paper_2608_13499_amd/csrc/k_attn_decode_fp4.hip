@@ -20,9 +20,10 @@
 //    ga, place i with B's lane group 2 (ga % 2) + i / 4, key slot 4 (ga / 2) + i % 4:
 //    that places the keys of V in the lanes (v_run, v_row).
 // Bound by the cache's bytes where they are many: 256 sequences of 4331 keys, 32 + 8 heads of 128, 1.21 GB:
-// 200 us, 6.0 TB/s, of 128 to 8192 205; without the arithmetic the loads take 197.  They pass the caches by
-// (nontemporal; with four tiles in a ring 220 us, 233 without).  One sequence of 700 keys takes 7.8 us, of 30000 15.9 with the
-// merge: chains of lengths, page ids, first loads, 1.2 us a tile, and the merge.
+// 200 us at best, 6.0 TB/s, of 128 to 8192 205 (215 to 219 a call with the merge; in a kernel trace 204 to 259,
+// median 244); without the arithmetic the loads take 197.  They pass the caches by (nontemporal; with four tiles in
+// a ring 220 us, 233 without).  64 sequences of 2000 keys take 40 us, fp32 44; one of 700 keys 7.8, of 30000 15.9 with
+// the merge: chains of lengths, page ids, first loads, 1.2 us a tile, and the merge.
 // bf16 takes its probabilities in two bf16 pieces, as decode with modifiers does.  fp32
 // queries are three bf16 pieces, exactly, and their probabilities too: the products with
 // the cache's values are whole, and summed in fp32.

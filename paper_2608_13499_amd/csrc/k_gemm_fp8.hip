@@ -135,11 +135,14 @@ struct LinearFp8Args {
 }  // namespace
 
 // ------------------------------------------------------------ tiles of many rows --
-// Bound by the matrix cores, which 8871 x 28672 x 4096 keeps busy 56 % of 915 us (2280 TFLOP/s, at
-// 2.0 GHz; one library product of the size with a scale for the whole tensor takes 705): the waves of
-// a SIMD wait for issue 40 % of the time, the four fma that scale a product beside its MFMA, and 21 %
-// at the slices' two barriers and counted waits.  8871 x 4096 x 14336 takes 510 us, 1023 x 6144 x 4096 36,
-// 200 x 4096 x 4096 20 with its second launch; fp32 2048 x 6144 x 4096 109.
+// 8871 x 28672 x 4096 takes 910 to 980 us from card to card (2130 to 2290 TFLOP/s, at 2.0 GHz; one
+// library product of the size with a scale for the whole tensor 705) and keeps the matrix cores busy
+// 57 % of that.  The rest is issue and waiting: the waves of a SIMD wait for issue 40 % of the time, the
+// four fma that scale a product beside its MFMA, and 22 % at the slices' barriers and counted waits.  LDS
+// is as busy: of a slice of 256 x 256 its waves (128 x 64 of y each) read 196 KB and the loads write 64, 2050
+// clocks at 128 bytes each, beside 2048 of MFMAs; of 128 x 256 1400 clocks beside 1024.
+// 8871 x 4096 x 14336 takes 500 to 540 us, 1023 x 6144 x 4096 31 to 34 in a run of calls (35 by itself), 200 x 4096 x
+// 4096 19 with its second launch; fp32 2048 x 6144 x 4096 104 to 111, 8871 x 6144 x 4096 455.
 //
 // BM x BN of y an item, 2 x WGN waves.  LDS holds RING slices of x's and W's rows and four of their
 // scales, filled by LDS DMA two slices ahead.
@@ -151,9 +154,9 @@ struct Fp8Tile {
   static constexpr int kLoadsX = BM / 8 / kWaves, kLoadsW = BN / 8 / kWaves;  // of a wave
   static constexpr int kScales = BM * 4 + 256;  // x's, then W's
   static constexpr int kStageBytes = (BM + BN) * kSlice, kRing = RING_, kLdsBytes = kRing * kStageBytes + 4 * kScales;
-  // The result past the caches (nontemporal, sc1), where it is a launch's last word: 1023 x 6144 x 4096 40 /
-  // 34 us.  Where the next tile's MFMAs hide it that costs (8871 x 28672 x 4096 912 / 920), and fp32's
-  // stores, which fill a line in two goes, lose (2048 x 6144 x 4096 109 / 132).
+  // The result past the caches (nontemporal, sc1), where it is a launch's last word: 1024 x 8192 x 4096 39.8 /
+  // 36.7 us, 1023 x 6144 x 4096 32.0 / 31.1.  Where the next tile's MFMAs hide it that costs (8871 x 28672 x 4096
+  // 937 / 948), and fp32's stores, which fill a line in two goes, lose (2048 x 6144 x 4096 111 / 131).
   static constexpr int kStorePolicy = BM < 256 ? 18 : 0;
   static constexpr bool kChained = kLdsBytes > 80 * 1024;  // one workgroup a CU
   static_assert(BM <= BN && BM % (8 * kWaves) == 0 && BN % (8 * kWaves) == 0 && BM / 64 < kWaves, "whole loads");
@@ -280,7 +283,7 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
   // the registers that they free, and x's slice after the next is sent for.  The loads are spread
   // between the MFMAs: those of all waves at once would fill the address unit's queue, and a wave
   // that waits there issues no MFMA.  With three slices in LDS the one after the next has a place of
-  // its own and the first barrier falls away (1024 x 8192 x 4096 42 / 40 us; 256 x 256 tiles have no room).
+  // its own and the first barrier falls away (1024 x 8192 x 4096 39.0 / 36.7 us; 256 x 256 tiles have no room).
   Frag w[TN], x[C::kSlots];
   float f[C::kSlots], wscale;
   OPS_LDS char* st = smem;
@@ -457,10 +460,11 @@ __global__ __launch_bounds__(C::kThreads, 1) void gemm_fp8_tile_kernel(const Lin
 }
 
 // --------------------------------------------------------------------- few rows --
-// Up to 16 TM rows: W's bytes are the time (48 x 4096 x 14336, 59 MB of W: 16.6 us, and 4.0 for the
-// sum of the ranges; 48 x 28672 x 4096 29; 16 x 28672 x 4096 25, 4.7 TB/s).  As gemm_decode_bf16_kernel: a workgroup
-// of NW waves takes 16 NW columns and all rows, each wave's W rows straight to
-// registers, a ring of kSlots slices, x and its scales through an LDS ring.
+// Up to 16 TM rows: W's bytes are the time (48 x 4096 x 14336, 59 MB of W: 16.8 us, and 3.9 for the
+// sum of the ranges, 20 together with W from HBM, 17.7 where three W take turns in the last-level cache; 48 x 28672 x
+// 4096 25; 16 x 28672 x 4096 23.3, 5.0 TB/s).  As gemm_decode_bf16_kernel: a workgroup of NW waves takes
+// 16 NW columns and all rows, each wave's W rows straight to registers, a ring of kSlots slices, x and
+// its scales through an LDS ring.
 namespace {
 constexpr int kSlots = 8, kAhead = 7, kStages = 4;
 static_assert(kAhead == kSlots - 1 && kSlots % kStages == 0 && kSlots == fp8_plan::kRing, "ring shapes");
