@@ -135,7 +135,7 @@ struct LinearFp8Args {
 }  // namespace
 
 // ------------------------------------------------------------ tiles of many rows --
-// 8871 x 28672 x 4096 takes 910 to 980 us from card to card (2130 to 2290 TFLOP/s, at 2.0 GHz; one
+// 8871 x 28672 x 4096 takes 910 to 980 us from run to run (2130 to 2290 TFLOP/s, at 1.9 GHz or less; one
 // library product of the size with a scale for the whole tensor 705) and keeps the matrix cores busy
 // 57 % of that.  The rest is issue and waiting: the waves of a SIMD wait for issue 40 % of the time, the
 // four fma that scale a product beside its MFMA, and 22 % at the slices' barriers and counted waits.  LDS
